@@ -1,11 +1,12 @@
-"""Builds libdblp_agg.so (HIP kernels + C-ABI) for gfx950, in-tree."""
+"""Builds libdblp_agg.so (HIP kernels + C-ABI) for gfx950, in-tree: the receiver (dblp_agg.hip) and the worker's
+operators (dblp_worker.hip)."""
 from __future__ import annotations
 
 import os
 import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(_HERE, "csrc", "dblp_agg.hip")
+SRCS = [os.path.join(_HERE, "csrc", f) for f in ("dblp_agg.hip", "dblp_worker.hip")]
 LIB = os.path.join(_HERE, "libdblp_agg.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -14,7 +15,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
 
 
 def build(verbose: bool = False) -> str:
-    cmd = [HIPCC, *FLAGS, "-o", LIB, SRC]
+    cmd = [HIPCC, *FLAGS, "-o", LIB, *SRCS]
     if verbose:
         print(" ".join(cmd))
     subprocess.check_call(cmd)

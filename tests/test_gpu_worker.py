@@ -1,0 +1,533 @@
+"""GPU: the worker's operators against their definitions in 64 bits.
+
+Tolerances.  U = half a step of fp32, 2^-24; u = half a step of the output's type (torch.finfo(t).eps / 2), plus half of the
+type's smallest number where a result is that small.
+  dropout, embed   at most four fp32 roundings (product with the scale, the position term, the kept factor and its own rounding,
+                   the residual) of terms whose magnitudes add up to `mag`, then one to the type: u |y| + 4 U mag
+  embed_grad       n terms added one after the other in any grouping, each with three roundings of its own, then scale and base:
+                   (n + 6) U times the sum of the terms' magnitudes
+  lse              an exponential of x - m: its argument is rounded three times (difference, constant, product), the function is off by one
+                   step, so a term by (3 |x - m| + 2) U with |x - m| at most 104, beyond which it is zero; weighed by the terms
+                   themselves that is at most (3 min(spread, 104) + 2) U.  The sum is made of at most V / 64 + 64 additions in a row.
+                   Then fp32 once.
+  policy_loss      the error of lp is lse's; slope = grad_scale d loss / d lp moves by `bend` times that, and is rounded to fp32;
+                   the softmax is off by the exponential's error, the sum's and four roundings; then the type."""
+import pytest
+import torch
+
+import worker_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = dict(f32=torch.float32, bf16=torch.bfloat16, f16=torch.float16)
+TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
+FTZ = 2.0 ** -125                # an fp32 result below the normal numbers may be taken as zero
+
+
+def half_step(t):
+    return torch.finfo(t).eps / 2
+
+
+def close(got, want, slack, t):
+    got = got.cpu().double()
+    assert got.shape == want.shape
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)])
+    tol = half_step(t) * want.abs() * (1 + half_step(t)) + slack + TINY[t] / 2 + FTZ
+    # past the type's largest number a rounding gives infinity
+    bad = fine & ~((got - want).abs() <= tol) & ~((want.abs() + tol > torch.finfo(t).max) & torch.isinf(got))
+    assert not bad.any(), (int(bad.sum()), got[bad][:4], want[bad][:4], tol[bad][:4] if tol.shape == want.shape else tol)
+
+
+def same(a, b):
+    """Equal values; NaN where the other has NaN."""
+    return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(a.masked_fill(torch.isnan(a), 0.0), b.masked_fill(torch.isnan(b), 0.0))
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def matrix(g, rows, cols, t, stride=None, shift=0, fill=None):
+    """A [rows, cols] view with rows `stride` apart, `shift` elements past a 16-byte border, inside a buffer of its own."""
+    stride = cols if stride is None else stride
+    buf = torch.full((shift + max(rows, 1) * stride + 8,), -77.0, dtype=t, device="cuda")
+    m = buf[shift:].as_strided((rows, cols), (stride, 1))
+    if rows:
+        m.copy_(torch.randn(rows, cols, generator=g, device="cuda") if fill is None else torch.full((rows, cols), fill, device="cuda"))
+    return buf, m
+
+
+def untouched(buf, m):
+    """Whether everything of the buffer outside the matrix is as it was."""
+    left = buf.clone()
+    left.as_strided(m.shape, m.stride(), m.storage_offset()).fill_(-77.0)
+    return bool((left == -77.0).all())
+
+
+# (rows, columns, padding of the rows, shift): one value; odd widths and rows; whole groups; aligned rows; more than one block
+SHAPES = [(0, 8, 0, 0), (1, 1, 0, 0), (3, 7, 0, 1), (5, 8, 0, 0), (4, 13, 3, 2), (70, 257, 0, 0), (33, 768, 0, 0), (9, 1000, 8, 0), (2, 2500, 1, 3)]
+
+
+@pytest.mark.parametrize("p", [0.0, 1e-6, 0.1, 0.7, 1.0])
+@pytest.mark.parametrize("t", TYPES)
+def test_dropout(t, p):
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    for k, (rows, cols, pad, shift) in enumerate(SHAPES):
+        for residual in (False, True):
+            g = gen(17 * k + residual)
+            _, x = matrix(g, rows, cols, t, cols + pad, shift)
+            buf, y = matrix(g, rows, cols, t, cols + 2 * pad, shift, fill=5.0)
+            r = matrix(g, rows, cols, t, cols, 0)[1] if residual else None
+            if rows > 2:
+                x[0, 0], x[1, 1], x[2, 2] = float("inf"), float("nan"), -float("inf")
+            drop = dblp.Drop(0xFEDCBA9876543210 + k, (k << 33) + 5, p)
+            dblp.dropout(x, y, drop, residual=r)
+            gate = ref.gates(rows, cols, 0xFEDCBA9876543210 + k, (k << 33) + 5, p)
+            xd = ref.dropped(x.cpu().double(), gate)
+            rd = r.cpu().double() if residual else torch.zeros_like(xd)
+            mag = (xd.abs() + rd.abs()).nan_to_num(0.0, 0.0, 0.0)
+            close(y, xd + rd, 4 * U * mag, t)
+            assert untouched(buf, y)
+            if not residual:
+                assert not bool(y.signbit().cpu()[gate == 0].any())        # +0, also under an infinity or NaN
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_dropout_in_place_and_backward(t):
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    g, rows, cols = gen(3), 37, 101
+    drop = dblp.Drop(9, 1, 0.25)
+    x = torch.randn(rows, cols, generator=g, device="cuda").to(t)
+    r = torch.randn(rows, cols, generator=g, device="cuda").to(t)
+    want, want_r = torch.empty_like(x), torch.empty_like(x)
+    dblp.dropout(x, want, drop)
+    dblp.dropout(x, want_r, drop, residual=r)
+    over_x, over_r = x.clone(), r.clone()
+    dblp.dropout(over_x, over_x, drop)
+    dblp.dropout(x, over_r, drop, residual=over_r)
+    assert torch.equal(over_x, want) and torch.equal(over_r, want_r)
+    if t == torch.float32:
+        # it is linear: <drop(x + h) - drop(x), dy> = <h, gradient>, where the gradient is the same mask on dy; differences in fp64 of
+        # values with at most 2 U relative error each (factor and product), a thousand times their sum being more than the bound needs
+        dy, h = torch.randn(rows, cols, generator=g, device="cuda"), torch.randn(rows, cols, generator=g, device="cuda")
+        dx, moved = torch.empty_like(x), torch.empty_like(x)
+        dblp.dropout(dy, dx, drop)
+        dblp.dropout(x + h, moved, drop)
+        a, b = ((moved.double() - want.double()) * dy.double()).sum(), (h.double() * dx.double()).sum()
+        mag = ((moved.abs().double() + want.abs().double()) * dy.abs().double()).sum()
+        assert abs(float(a - b)) <= 6 * U * float(mag)
+
+
+def tokens_of(g, n, vocab, kind):
+    if kind == "one":
+        return torch.full((n,), vocab // 2, dtype=torch.int64, device="cuda")
+    if kind == "none":
+        return torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    tok = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    if kind == "skewed":
+        tok = tok * tok // vocab * tok // vocab // 4
+    if kind == "bad":
+        where = torch.rand(n, generator=g, device="cuda") < 0.4
+        wrong = torch.tensor([-1, vocab, vocab + 1, -100, 2**31, 2**32, 2**62, -2**63], device="cuda")
+        tok = torch.where(where, wrong[torch.randint(0, 8, (n,), generator=g, device="cuda")], tok)
+    return tok
+
+
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("table", TYPES)
+def test_embed(table, out):
+    import paper_2605_01989_amd as dblp
+    tt, ot = TYPES[table], TYPES[out]
+    for k, (n, dim, pad, shift) in enumerate(SHAPES):
+        for positions, p, kind in ((False, 0.0, "any"), (True, 0.2, "bad"), (True, 0.0, "bad"), (False, 0.5, "one"), (True, 1.0, "any"), (False, 0.0, "none")):
+            g = gen(100 + k)
+            vocab, n_pos, scale = 50 + k, 9, 3.7
+            _, tab = matrix(g, vocab, dim, tt, dim + pad, shift)
+            pos_tab = matrix(g, n_pos, dim, tt, dim, 0)[1] if positions else None
+            tok = tokens_of(g, n, vocab, kind)
+            pos = tokens_of(g, n, n_pos, kind) if positions else None
+            buf, y = matrix(g, n, dim, ot, dim + pad, shift, fill=5.0)
+            dblp.embed(tok, tab, y, scale=scale, positions=pos, pos_table=pos_tab, drop=dblp.Drop(5 + k, 6, p))
+            e = ref.rows_of(tab, tok) * float(torch.tensor(scale))
+            q = ref.rows_of(pos_tab, pos) if positions else torch.zeros_like(e)
+            gate = ref.gates(n, dim, 5 + k, 6, p)
+            close(y, ref.dropped(e + q, gate), 4 * U * gate * (e.abs() + q.abs()), ot)
+            assert untouched(buf, y)
+
+
+def test_embed_drops_what_is_not_finite_and_broadcasts():
+    import paper_2605_01989_amd as dblp
+    tab = torch.full((4, 64), float("nan"), device="cuda")
+    tab[1] = float("inf")
+    tok = torch.tensor([0, 1, 2, -1, 7], device="cuda")
+    y = torch.empty(5, 64, device="cuda")
+    dblp.embed(tok, tab, y, scale=float("inf"), drop=dblp.Drop(1, 2, 0.5))
+    gate = ref.gates(5, 64, 1, 2, 0.5)
+    assert bool((y.cpu()[gate == 0] == 0).all()) and bool((y[3:] == 0).all()) and bool(torch.isnan(y.cpu()[0][gate[0] != 0]).all())
+    # a table whose rows are all the same row (stride 0)
+    row = torch.randn(1, 64, device="cuda")
+    dblp.embed(torch.arange(5, device="cuda"), row.expand(5, 64), y)
+    assert torch.equal(y, row.expand(5, 64))
+
+
+# (tokens, vocabulary, width, kind): from nothing to several tiles of every stage, all places the same token, none at all,
+# tables of one row and of more rows than two digits of a sort hold
+GRADS = [(0, 7, 9, "any"), (1, 1, 1, "any"), (37, 5, 13, "any"), (300, 1000, 333, "bad"), (513, 40, 64, "one"), (700, 50, 40, "none"), (2100, 3000, 72, "skewed"),
+         (5000, 50257, 24, "skewed"), (9001, 300000, 16, "any"), (20000, 60, 17, "skewed"), (40000, 2, 8, "any"), (33000, 100, 520, "one"), (70001, 70000, 8, "bad")]
+
+
+@pytest.mark.parametrize("n, vocab, dim, kind", GRADS)
+def test_embed_grad(n, vocab, dim, kind):
+    import paper_2605_01989_amd as dblp
+    for k, (t, p, base) in enumerate([("f32", 0.0, None), ("bf16", 0.1, "place"), ("f16", 0.0, "apart"), ("f32", 0.3, "apart"), ("bf16", 0.0, None)]):
+        t = TYPES[t]
+        pad, shift = k % 3, k % 2
+        g = gen(n + k)
+        tok = tokens_of(g, n, vocab, kind)
+        _, dy = matrix(g, n, dim, t, dim + pad, shift)
+        buf, grad = matrix(g, vocab, dim, torch.float32, dim + pad, shift, fill=3.0)
+        b, bd = None, None
+        if base == "place":
+            grad.copy_(torch.randn(vocab, dim, generator=g, device="cuda"))
+            b, bd = grad, grad.clone()
+        elif base == "apart":
+            b = torch.randn(vocab, dim, generator=g, device="cuda")
+            bd = b
+        ws = torch.full((dblp.embed_grad_workspace(n, vocab, dim),), 0xA5, dtype=torch.uint8, device="cuda")
+        scale = 1.0 if k else 0.5
+        dblp.embed_grad(tok, dy, grad, ws, scale=scale, drop=dblp.Drop(3, 4, p), base=b)
+        want, mag, terms = ref.embed_grad(tok, dy, vocab, scale, ref.gates(n, dim, 3, 4, p), bd)
+        close(grad, want, (terms + 6) * U * mag, torch.float32)
+        assert untouched(buf, grad)
+        if b is not grad:
+            first = grad.clone()
+            ws.random_(generator=g)
+            dblp.embed_grad(tok, dy, grad, ws, scale=scale, drop=dblp.Drop(3, 4, p), base=b)
+            assert torch.equal(first, grad)                        # the same bits, whatever the workspace held
+
+
+def test_embed_grad_is_the_gradient_and_leaves_other_rows_alone():
+    """Differences of L = sum(embed(E) dy): L is linear in E, so L(E + h e) - L(E) = h gradient up to the roundings of the two sums'
+    terms, each of them one fp32 product (scale) and one more (kept factor)."""
+    import paper_2605_01989_amd as dblp
+    g, n, vocab, dim = gen(1), 60, 12, 20
+    tok, tab = tokens_of(g, n, vocab, "bad"), torch.randn(vocab, dim, generator=g, device="cuda")
+    dy, drop = torch.randn(n, dim, generator=g, device="cuda"), dblp.Drop(8, 8, 0.2)
+    grad, ws = torch.empty(vocab, dim, device="cuda"), torch.empty(dblp.embed_grad_workspace(n, vocab, dim), dtype=torch.uint8, device="cuda")
+    dblp.embed_grad(tok, dy, grad, ws, scale=2.5, drop=drop)
+
+    def loss(table):
+        y = torch.empty(n, dim, device="cuda")
+        dblp.embed(tok, table, y, scale=2.5, drop=drop)
+        return (y.double() * dy.double()).sum(), (y.double() * dy.double()).abs().sum()
+    at, mag = loss(tab)
+    for v, c in ((0, 0), (3, 7), (11, 19), (5, 12)):
+        h = torch.zeros_like(tab)
+        h[v, c] = 4.0
+        moved, mag2 = loss(tab + h)
+        assert abs(float(moved - at) / 4.0 - float(grad[v, c])) <= 4 * U * float(mag + mag2) + (n + 6) * U * float(grad[v, c].abs() + mag / 4)
+    # in place: rows without a token keep what they hold, NaN too
+    grad.fill_(float("nan"))
+    dblp.embed_grad(torch.tensor([2, -1, 2], device="cuda"), dy[:3].contiguous(), grad, ws, base=grad)
+    grad[2] = float("nan")
+    assert bool(torch.isnan(grad).all())
+    grad.fill_(1.0)
+    dblp.embed_grad(torch.tensor([2, -1, 2], device="cuda"), dy[:3].contiguous(), grad, ws, base=grad)
+    assert bool((grad[[0, 1, 3, 4, 5, 6, 7, 8, 9, 10, 11]] == 1).all()) and not bool((grad[2] == 1).all())
+
+
+# (rows, vocabulary, padding, shift): one value, odd widths, rows that a block takes in one, several and many pieces
+LOGITS = [(0, 5, 0, 0), (1, 1, 0, 0), (2, 7, 0, 1), (5, 100, 0, 0), (3, 1021, 3, 1), (40, 4096, 0, 0), (1, 50257, 0, 0), (7, 50257, 47, 0), (300, 5003, 0, 1), (2, 140001, 0, 1),
+          (1, 300000, 0, 0), (700, 515, 1, 0)]
+
+
+def make_logits(g, n, vocab, pad, shift, t):
+    buf, x = matrix(g, n, vocab, t, vocab + pad, shift)
+    x.mul_(3)
+    target = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    low = torch.finfo(t).min
+    for row in range(1, min(n, 7)):          # masked places: none, the lowest value, all but one, everything, everything the lowest, a huge one
+        if row == 1:
+            x[row, : vocab // 2] = -float("inf")
+        elif row == 2:
+            x[row, vocab // 2 :] = low
+        elif row == 3:
+            x[row] = -float("inf")
+            x[row, target[row]] = 2.0
+        elif row == 4:
+            x[row] = -float("inf")
+        elif row == 5:
+            x[row] = low
+        else:
+            x[row, vocab // 3] = 3.0e4
+    return buf, x, target
+
+
+def lse_error(x):
+    """Of lse, a number for each row."""
+    xd, V = x.cpu().double(), x.shape[1]
+    m = xd.max(1, keepdim=True).values
+    spread = torch.where(torch.isfinite(xd), m - xd, torch.zeros_like(xd)).nan_to_num(0.0, 0.0, 0.0).max(1).values.clamp(max=104.0) if V else torch.zeros(len(xd))
+    return (3 * spread + 2 + V / 64 + 64) * U
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n, vocab, pad, shift", LOGITS)
+def test_token_logprobs(n, vocab, pad, shift, t):
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    g = gen(n + vocab)
+    _, x, target = make_logits(g, n, vocab, pad, shift, t)
+    if n > 8:
+        target[8], target[7] = -1, vocab
+        x[8] = float("nan")
+        x[9 % n, 0] = float("nan") if n > 9 else x[0, 0]
+    ws = torch.full((dblp.logits_workspace(n, vocab),), 0xA5, dtype=torch.uint8, device="cuda")
+    logp, lse = torch.full((n,), 9.0, device="cuda"), torch.full((n,), 9.0, device="cuda")
+    dblp.token_logprobs(x, target, logp, ws, lse=lse)
+    if n == 0:
+        return
+    lp, l = ref.logprobs(x, target)
+    off = ((target < 0) | (target >= vocab)).cpu()
+    e = lse_error(x)
+    close(lse, torch.where(off, 0.0, l), e, torch.float32)
+    close(logp, torch.where(off, 0.0, lp), e, torch.float32)
+    only = torch.empty_like(logp)
+    dblp.token_logprobs(x, target, only, ws)
+    assert torch.equal(only.nan_to_num(7.0), logp.nan_to_num(7.0))
+
+
+def policy_inputs(g, x, target, none):
+    n = x.shape[0]
+    lp = ref.logprobs(x, target)[0].nan_to_num(0.0, 0.0, 0.0).cuda()
+    change = 0.3 * torch.randn(n, generator=g, device="cuda", dtype=torch.float64)
+    for border in (0.8, 1.3):                # the gradient jumps at a border: no ratio within rounding of one
+        b = torch.tensor(border, dtype=torch.float64).log().item()
+        change = torch.where((change - b).abs() < 2e-2, change + 0.05, change)
+    old, back = (lp - change).float(), (lp + 0.3 * torch.randn(n, generator=g, device="cuda", dtype=torch.float64)).float()
+    adv, w = torch.randn(n, generator=g, device="cuda"), torch.rand(n, generator=g, device="cuda") + 0.1
+    out = torch.rand(n, generator=g, device="cuda") < none
+    target = torch.where(out, torch.tensor([-1, x.shape[1], -100, 2**40], device="cuda")[torch.arange(n, device="cuda") % 4], target)
+    for v in (old, back, adv):
+        v[out] = float("nan")
+    if n > 9:
+        w[9], adv[9], old[9] = 0.0, float("nan"), float("inf")
+        x[9] = float("nan")
+    return target, adv, w, old, back
+
+
+def check_policy(got, want, x, t, grad_scale):
+    stats, logp, dlogits = got
+    e = lse_error(x)
+    close(logp, want["logp"], e, torch.float32)
+    move = (e + U * want["logp"].nan_to_num(0.0, 0.0, 0.0).abs())[:, None]
+    if dlogits is not None:
+        slope_error = want["bend"][:, None] * 2 * move + 2 * U * want["slope"].abs()[:, None]
+        p_error = want["prob"] * (2 * e[:, None] + 4 * U)
+        # a token of probability zero that was taken has an infinite KL: its row is infinite or, where the softmax is zero too, NaN
+        endless = want["on"] & ~torch.isfinite(want["slope"])
+        assert not bool(torch.isfinite(dlogits.cpu()[endless]).any())
+        for v in (slope_error, p_error, want["slope"], want["prob"], want["hit"], want["dlogits"]):
+            v[endless] = 0.0
+        dlogits = dlogits.clone()
+        dlogits[endless.cuda()] = 0.0
+        close(dlogits, want["dlogits"], slope_error * (want["hit"] + want["prob"]) + want["slope"].abs()[:, None] * p_error + 2 * U * want["dlogits"].abs(), t)
+        zero = ~want["on"]
+        assert bool((dlogits.cpu()[zero] == 0).all()) and not bool(dlogits.cpu()[zero].signbit().any())
+    if x.shape[0]:
+        worst = float(move.max())
+        close(stats[:3], want["stats"][:3], 2 * U * want["mags"] + 2 * worst * want["moves"], torch.float32)
+    assert torch.equal(stats[3:].cpu().double(), want["stats"][3:])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n, vocab, pad, shift", LOGITS)
+def test_policy_loss(n, vocab, pad, shift, t):
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    for k, (use_old, use_ref, none) in enumerate([(True, True, 0.3), (False, False, 0.0), (True, False, 0.0), (False, True, 1.0)]):
+        g = gen(n * 3 + vocab + k)
+        _, x, target = make_logits(g, n, vocab, pad, shift, t)
+        target, adv, w, old, back = policy_inputs(g, x, target, none)
+        old, back = old if use_old else None, back if use_ref else None
+        scale = 64.0 if k == 1 else 1.0
+        args = dict(old_logp=old, ref_logp=back, clip=(0.2, 0.3), kl_coef=0.1, grad_scale=scale)
+        want = ref.policy(x, target, adv, w, old, back, (0.2, 0.3), 0.1, scale)
+        ws = torch.full((dblp.logits_workspace(n, vocab),), 0xA5, dtype=torch.uint8, device="cuda")
+        stats, logp = torch.full((5,), 9.0, device="cuda"), torch.full((n,), 9.0, device="cuda")
+        buf, d = matrix(g, n, vocab, t, vocab + 2 * pad, shift ^ 1, fill=4.0)
+        dblp.policy_loss(x, target, adv, w, stats, ws, dlogits=d, logp=logp, **args)
+        check_policy((stats, logp, d), want, x, t, scale)
+        assert untouched(buf, d)
+        # without the gradient, and in place: the same numbers
+        only, only_lp = torch.empty_like(stats), torch.empty_like(logp)
+        dblp.policy_loss(x, target, adv, w, only, ws, logp=only_lp, **args)
+        check_policy((only, only_lp, None), want, x, t, scale)
+        over = torch.empty(n * (vocab + pad) + 1, dtype=t, device="cuda")[shift:].as_strided((n, vocab), (vocab + pad, 1))
+        over.copy_(x)
+        dblp.policy_loss(over, target, adv, w, only, ws, dlogits=over, **args)
+        assert same(over, d) and same(only, stats)
+
+
+def test_policy_loss_gradient_against_differences():
+    """Central differences of the loss with step h: off by h^2 / 6 times the third derivative (below 4 for these numbers: weights of
+    one, ratios and advantages of about one) and by the loss' rounding, U |loss| and lse's error, over h."""
+    import paper_2605_01989_amd as dblp
+    g, n, vocab, h = gen(5), 6, 17, 2.0 ** -5
+    x = torch.randn(n, vocab, generator=g, device="cuda")
+    target = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    target, adv, w, old, back = policy_inputs(g, x, target, 0.0)
+    ws = torch.empty(dblp.logits_workspace(n, vocab), dtype=torch.uint8, device="cuda")
+
+    def loss(logits, d=None):
+        stats = torch.empty(5, device="cuda")
+        dblp.policy_loss(logits, target, adv, w, stats, ws, old_logp=old, ref_logp=back, dlogits=d, clip=(0.2, 10.0), kl_coef=0.3)
+        return float(stats[0].double())
+    # wide borders: no token crosses one within the step (ratios are within exp(+-2) of each other)
+    d = torch.empty_like(x)
+    old = ref.logprobs(x, target)[0].float().cuda() - 0.05
+    loss(x, d)
+    for i in range(n):
+        for j in (0, int(target[i]), vocab - 1):
+            e = torch.zeros_like(x)
+            e[i, j] = h
+            got = (loss(x + e) - loss(x - e)) / (2 * h)
+            assert abs(got - float(d[i, j])) <= 4 * h * h / 6 + (20 * U + 4 * float(lse_error(x).max())) * n * 4 / h
+
+
+def test_cross_entropy_is_the_policy_loss_of_an_advantage_of_one():
+    import paper_2605_01989_amd as dblp
+    g, n, vocab = gen(6), 12, 333
+    x = torch.randn(n, vocab, generator=g, device="cuda")
+    target = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    one, w = torch.ones(n, device="cuda"), torch.full((n,), 1 / n, device="cuda")
+    stats, logp, d = torch.empty(5, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x)
+    dblp.policy_loss(x, target, one, w, stats, torch.empty(dblp.logits_workspace(n, vocab), dtype=torch.uint8, device="cuda"), dlogits=d, logp=logp)
+    want = (x.cpu().double().softmax(1) - torch.nn.functional.one_hot(target.cpu(), vocab).double()) / n
+    e = lse_error(x)
+    close(d, want, (2 * e[:, None] + 10 * U) / n, torch.float32)
+    ce = -x.cpu().double().log_softmax(1).gather(1, target.cpu()[:, None])[:, 0]
+    close(-logp, ce, e, torch.float32)
+
+
+def test_offsets_past_32_bits():
+    """Rows more than 2^32 bytes apart: 16-bit matrices of three rows, 2^31 + 24 elements from row to row."""
+    import paper_2605_01989_amd as dblp
+    stride, t, cols = 2**31 + 24, torch.bfloat16, 1000
+    big = torch.empty(2 * stride + cols, dtype=t, device="cuda")
+    far = big.as_strided((3, cols), (stride, 1))
+    g = gen(7)
+    x = torch.randn(3, cols, generator=g, device="cuda").to(t)
+    near, drop = torch.empty_like(x), dblp.Drop(1, 1, 0.3)
+    far.copy_(x)
+    dblp.dropout(far, near, drop)
+    want = near.clone()
+    dblp.dropout(x, far, drop)
+    assert torch.equal(far, want)
+    far.copy_(x)
+    tok = torch.tensor([2, 0, 1, 2], device="cuda")
+    y = torch.empty(4, cols, dtype=t, device="cuda")
+    dblp.embed(tok, far, y)
+    assert torch.equal(y, x[tok])
+    target, w = torch.tensor([5, 999, 0], device="cuda"), torch.ones(3, device="cuda")
+    ws = torch.empty(dblp.logits_workspace(3, cols), dtype=torch.uint8, device="cuda")
+    a, b = torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+    dblp.token_logprobs(x, target, a, ws)
+    dblp.token_logprobs(far, target, b, ws)
+    assert torch.equal(a, b)
+    stats, d = torch.empty(5, device="cuda"), torch.empty_like(x)
+    dblp.policy_loss(x, target, w, w, stats, ws, dlogits=d)
+    dblp.policy_loss(far, target, w, w, stats, ws, dlogits=far)
+    assert torch.equal(far, d)
+    far.copy_(x)
+    tok, grad, other = torch.tensor([1, 1, 0], device="cuda"), torch.empty(2, cols, device="cuda"), torch.empty(2, cols, device="cuda")
+    gws = torch.empty(dblp.embed_grad_workspace(3, 2, cols), dtype=torch.uint8, device="cuda")
+    dblp.embed_grad(tok, x, grad, gws)
+    dblp.embed_grad(tok, far, other, gws)
+    assert torch.equal(grad, other)
+
+
+def everything(dblp, s, d_draw, stream=None):
+    """All five operators on the buffers of `s`, enqueued one after the other."""
+    drop = dblp.Drop(77, 3, 0.2, d_draw)
+    dblp.embed(s["tok"], s["table"], s["h"], scale=2.0, positions=s["pos"], pos_table=s["pos_table"], drop=drop, stream=stream)
+    dblp.dropout(s["h"], s["y"], drop, residual=s["h"], stream=stream)
+    dblp.token_logprobs(s["logits"], s["target"], s["old"], s["ws"], stream=stream)
+    dblp.policy_loss(s["logits"], s["target"], s["adv"], s["w"], s["stats"], s["ws"], old_logp=s["old"], dlogits=s["dlogits"], stream=stream)
+    dblp.embed_grad(s["tok"], s["y"], s["grad"], s["gws"], drop=drop, stream=stream)
+
+
+def buffers(dblp, n=9000, vocab=3001, dim=72, seed=11):
+    g = gen(seed)
+    f = dict(device="cuda")
+    return dict(tok=tokens_of(g, n, vocab, "skewed"), table=torch.randn(vocab, dim, generator=g, **f), pos=torch.arange(n, **f) % 128, pos_table=torch.randn(128, dim, generator=g, **f),
+                h=torch.empty(n, dim, dtype=torch.bfloat16, **f), y=torch.empty(n, dim, dtype=torch.bfloat16, **f), logits=torch.randn(500, vocab, generator=g, **f),
+                target=torch.randint(0, vocab, (500,), generator=g, **f), old=torch.empty(500, **f), adv=torch.randn(500, generator=g, **f), w=torch.rand(500, generator=g, **f),
+                stats=torch.empty(5, **f), dlogits=torch.empty(500, vocab, **f), grad=torch.empty(vocab, dim, **f),
+                ws=torch.empty(dblp.logits_workspace(500, vocab), dtype=torch.uint8, **f), gws=torch.empty(dblp.embed_grad_workspace(n, vocab, dim), dtype=torch.uint8, **f))
+
+
+RESULTS = ("h", "y", "old", "stats", "dlogits", "grad")
+
+
+def test_recorded_into_a_graph_it_draws_anew_at_each_replay():
+    import paper_2605_01989_amd as dblp
+    s, e = buffers(dblp), buffers(dblp)
+    draw = torch.zeros(1, dtype=torch.int64, device="cuda")
+    everything(dblp, s, draw)                                   # (what a first call sets up is not recorded)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        everything(dblp, s, draw)
+    seen = []
+    for i in (0, 5, 6, 5):
+        draw.fill_(i)
+        for k in RESULTS:
+            s[k].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        everything(dblp, e, draw.clone())                       # eager work between the replays, on other buffers
+        for k in RESULTS:
+            assert torch.equal(s[k], e[k]), (i, k)
+        seen.append(s["h"].clone())
+    assert torch.equal(seen[1], seen[3]) and not torch.equal(seen[0], seen[1]) and not torch.equal(seen[1], seen[2])
+    # the counter on the device is added to the one in the arguments
+    y, z = torch.empty_like(s["h"]), torch.empty_like(s["h"])
+    draw.fill_(5)
+    dblp.dropout(s["h"], y, dblp.Drop(77, 3, 0.2, draw))
+    dblp.dropout(s["h"], z, dblp.Drop(77, 8, 0.2))
+    assert torch.equal(y, z)
+
+
+def test_on_another_stream_than_the_current_one():
+    import paper_2605_01989_amd as dblp
+    s, e = buffers(dblp), buffers(dblp)
+    everything(dblp, e, None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    everything(dblp, s, None, stream=side.cuda_stream)          # handed over raw
+    side.synchronize()
+    for k in RESULTS:
+        assert torch.equal(s[k], e[k]), k
+    assert torch.cuda.current_device() == 0
+
+
+def test_refusals_of_the_binding_on_the_gpu():
+    import paper_2605_01989_amd as dblp
+    x, y, drop = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda"), dblp.Drop(1, 1, 0.5)
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    v = torch.zeros(4, device="cuda")
+    for f in (lambda: dblp.dropout(x, y[:3], drop), lambda: dblp.dropout(x, y.half(), drop), lambda: dblp.dropout(x, y.cpu(), drop), lambda: dblp.dropout(x.T, y.T, drop),
+              lambda: dblp.embed(t.int(), x, y), lambda: dblp.embed(t, x, y, positions=t), lambda: dblp.embed_grad(t, x, y, ws[1:]), lambda: dblp.embed_grad(t, x, y.half(), ws),
+              lambda: dblp.embed_grad(t, x, y, ws[:16]), lambda: dblp.embed_grad(t, x, y, ws.cpu()), lambda: dblp.token_logprobs(x, t[:3], v, ws), lambda: dblp.token_logprobs(x, t, v.half(), ws),
+              lambda: dblp.policy_loss(x, t, v, v, v, ws), lambda: dblp.policy_loss(x, t, v, v, torch.zeros(5, device="cuda"), ws, clip=(2.0, 0.1))):
+        with pytest.raises(dblp.DblpError):
+            f()
+    dblp.dropout(x, y, drop)                                    # and the library goes on working
+    torch.cuda.synchronize()

@@ -1,0 +1,133 @@
+"""No-GPU checks of the worker's operators: the header and its binding agree, bad arguments are refused before the device
+is touched, and the tests' own generator has the published known answers."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_01989_amd as dblp
+import worker_reference as ref
+from paper_2605_01989_amd import binding, worker
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "dblp_worker.h")
+A, B = 1 << 20, 1 << 21            # addresses that are never read: every call here is refused
+
+
+def test_library_exports_what_the_header_declares():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(dblp_[a-z_0-9]+)\s*\(", text)))
+    assert sorted(worker.EXPORTS) == names and len(names) == 8
+    for n in names:
+        assert hasattr(dblp.lib(), n), n
+    defines = dict(re.findall(r"^#define\s+DBLP_([A-Z_0-9]+)\s+(\d+)", text, flags=re.M))
+    assert {k: int(v) for k, v in defines.items()} == dict(F32=worker.F32, BF16=worker.BF16, F16=worker.F16)
+
+
+@pytest.mark.parametrize("counter, key, answer", [
+    ((0, 0, 0, 0), (0, 0), (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)),
+    ((0xFFFFFFFF,) * 4, (0xFFFFFFFF,) * 2, (0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD)),
+    ((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0), (0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1)),
+])
+def test_generator_has_the_published_answers(counter, key, answer):
+    got = ref.philox([np.array([c]) for c in counter], key)
+    assert tuple(int(v[0]) for v in got) == answer
+
+
+def test_share_of_dropped_values():
+    g = ref.gates(500, 803, 12345, 7, 0.3)
+    n, p = g.numel(), round(65536 * 0.3) / 65536
+    assert abs(int((g == 0).sum()) - n * p) < 5 * (n * p * (1 - p)) ** 0.5
+    assert abs(float(g.mean()) - 1) < 5 * (p / (1 - p) / n) ** 0.5
+
+
+def test_workspaces():
+    assert dblp.embed_grad_workspace(0, 1, 1) > 0 and dblp.logits_workspace(0, 1) > 0
+    for bad in ((1 << 31, 1, 1), (1, 0, 1), (1, 1 << 31, 1), (1, 1, 0)):
+        assert dblp.embed_grad_workspace(*bad) == 0
+    for bad in ((1 << 31, 1), (1, 0), (1, 1 << 31)):
+        assert dblp.logits_workspace(*bad) == 0
+
+
+def _embed(**k):
+    a = dict(tokens=A, n=4, dim=8, table=A, stride=8, vocab=10, ttype=0, scale=1.0, pos=None, ptable=None, pstride=0, npos=0, drop=None, out=B, ostride=8, otype=0)
+    a.update(k)
+    return dblp.lib().dblp_embed(0, None, *a.values())
+
+
+def _grad(**k):
+    a = dict(tokens=A, n=4, dim=8, vocab=10, scale=1.0, drop=None, dy=A, dstride=8, type=0, base=None, bstride=0, grad=B, gstride=8, ws=A, bytes=1 << 30)
+    a.update(k)
+    return dblp.lib().dblp_embed_grad(0, None, *a.values())
+
+
+def _dropout(**k):
+    a = dict(rows=4, cols=8, x=A, xs=8, r=None, rs=0, drop=dblp.Drop(1, 2, 0.5), y=B, ys=8, type=0)
+    a.update(k)
+    return dblp.lib().dblp_dropout(0, None, *a.values())
+
+
+def _logprobs(**k):
+    a = dict(n=4, vocab=10, x=A, xs=10, type=0, targets=A, logp=B, lse=None, ws=A, bytes=1 << 30)
+    a.update(k)
+    return dblp.lib().dblp_token_logprobs(0, None, *a.values())
+
+
+def _policy(**k):
+    a = dict(n=4, vocab=10, x=A, xs=10, type=0, targets=A, adv=A, w=A, old=None, ref=None, lo=0.2, hi=0.2, kl=0.0, gs=1.0, d=B, ds=10, logp=None, stats=B, ws=A, bytes=1 << 30)
+    a.update(k)
+    return dblp.lib().dblp_policy_loss(0, None, *a.values())
+
+
+BIG = 1 << 31
+REFUSED = [
+    (_embed, [dict(ttype=3), dict(otype=-1), dict(dim=0), dict(vocab=0), dict(vocab=BIG), dict(n=BIG), dict(tokens=None), dict(table=None), dict(out=None),
+              dict(pos=A), dict(ptable=A), dict(pos=A, ptable=A, npos=0), dict(tokens=A + 4), dict(table=A + 2), dict(out=B + 1, otype=1), dict(ostride=7),
+              dict(drop=dblp.Drop(0, 0, -0.1)), dict(drop=dblp.Drop(0, 0, 1.1)), dict(drop=dblp.Drop(0, 0, float("nan")))]),
+    (_grad, [dict(type=9), dict(dim=0), dict(vocab=0), dict(n=BIG), dict(tokens=None), dict(dy=None), dict(grad=None), dict(dy=A + 1, type=2), dict(grad=B + 2), dict(base=B + 1),
+             dict(gstride=7), dict(base=B, bstride=16), dict(ws=None), dict(ws=A + 16), dict(bytes=0), dict(drop=dblp.Drop(0, 0, 2.0))]),
+    (_dropout, [dict(type=3), dict(cols=0), dict(rows=BIG), dict(x=None), dict(y=None), dict(drop=None), dict(x=A + 2), dict(r=A + 1, type=1), dict(ys=7), dict(y=A, ys=16),
+                dict(r=B, rs=16), dict(drop=dblp.Drop(0, 0, float("inf")))]),
+    (_logprobs, [dict(type=4), dict(vocab=0), dict(n=BIG), dict(x=None), dict(targets=None), dict(logp=None), dict(x=A + 1, type=1), dict(targets=A + 4), dict(lse=B + 2),
+                 dict(ws=None), dict(ws=A + 8), dict(bytes=0)]),
+    (_policy, [dict(type=4), dict(vocab=0), dict(n=BIG), dict(x=None), dict(targets=None), dict(adv=None), dict(w=None), dict(stats=None), dict(old=A + 1), dict(ref=A + 2),
+               dict(lo=-0.1), dict(lo=1.5), dict(hi=-1.0), dict(hi=float("inf")), dict(lo=float("nan")), dict(kl=float("nan")), dict(gs=float("inf")), dict(ds=9),
+               dict(d=A, ds=16), dict(ws=None), dict(bytes=0), dict(stats=B + 1)]),
+]
+
+
+@pytest.mark.parametrize("call, k", [(c, k) for c, ks in REFUSED for k in ks], ids=lambda v: v.__name__ if callable(v) else "-".join(v))
+def test_refusals(call, k):
+    worker._load()
+    assert call(**k) == binding.EINVAL
+    assert dblp.lib().dblp_worker_error().decode().split(":")[0] in ("embed", "embed_grad", "dropout", "token_logprobs", "policy_loss")
+
+
+def test_draw_counter_must_be_aligned():
+    worker._load()
+    d = dblp.Drop(1, 2, 0.5)
+    d.d_draw = A + 4
+    assert _dropout(drop=d) == binding.EINVAL and b"d_draw" in dblp.lib().dblp_worker_error()
+
+
+def test_nothing_to_do_needs_no_device():
+    worker._load()
+    assert _embed(n=0) == binding.OK and _dropout(rows=0) == binding.OK and _logprobs(n=0) == binding.OK
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    x = torch.zeros(4, 8)
+    with pytest.raises(dblp.DblpError) as e:
+        dblp.dropout(x, torch.zeros(4, 8), dblp.Drop(1, 2, 0.5))             # not on the GPU
+    assert e.value.code == binding.EINVAL
+    meta = torch.empty(4, 8, device="meta")
+    for bad in (torch.empty(4, 9, device="meta"), torch.empty(8, 4, device="meta").T, torch.empty(4, 8, dtype=torch.int32, device="meta"), torch.empty(32, device="meta"), x):
+        with pytest.raises(dblp.DblpError):
+            worker._matrix("m", bad, meta.device, 4, 8)
+    assert worker._matrix("m", meta, meta.device, 4, 8)[1] == 8
+    for bad in (torch.empty(5, device="meta"), torch.empty(4, device="meta", dtype=torch.float64), torch.empty(8, device="meta")[::2]):
+        with pytest.raises(dblp.DblpError):
+            worker._vector("v", bad, meta.device, 4, torch.float32)
+    assert ctypes.sizeof(worker.Drop) == 32
