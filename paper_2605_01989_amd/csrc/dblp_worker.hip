@@ -167,29 +167,42 @@ __global__ __launch_bounds__(256) void embed_groups(Groups s, Mask m, const int6
 }
 
 // ------------------------------------------------------------------------------------------
-// gradient of the embedding
+// gradient of the embedding: a table row's gradient is the sum over the places of its token, so the places are sorted by token
+// (stably: a row is summed in the order of its places) and the sorted list is cut into pieces of equal length
 // ------------------------------------------------------------------------------------------
-// grad = base, or zeros
-__global__ __launch_bounds__(256) void grad_begin(Groups s, const float* base, u64 base_stride, float* grad, u64 grad_stride) {
-    const u32 i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= s.n) return;
-    const u32 r = s.per_row.of(i), c = (i - r * s.per_row.d) * 8;
-    const u64 row = s.row0 + r;
+// Eight columns of a row of the result: base (or zero) + scale * sum.
+__device__ __forceinline__ void put_row(const float* base, u64 base_stride, float* grad, u64 grad_stride, u64 row, u32 c, u32 cols, float scale, const float (&sum)[8]) {
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (base) load_group<F32>(base + row * base_stride, c, s.cols, v);
-    store_group<F32>(grad + row * grad_stride, c, s.cols, v);
+    if (base) load_group<F32>(base + row * base_stride, c, cols, v);
+    for (int e = 0; e < 8; ++e) v[e] += scale * sum[e];
+    store_group<F32>(grad + row * grad_stride, c, cols, v);
 }
 
-// A block stands for one token place and some columns.  The block of a token's first place adds up the rows of all its
-// places, in order; the others end.
+struct Result { const float* base; u64 base_stride; float* grad; u64 grad_stride; u64 vocab; float scale; };
+
+// Group i of those rows of the result that have no token (`present` says which have one; null: all rows alike).
+__device__ __forceinline__ void fill_group(const Result& out, const Groups& s, u32 i, const uint8_t* present) {
+    const u32 r = s.per_row.of(i), c = (i - r * s.per_row.d) * 8;
+    const u64 row = s.row0 + r;
+    if (present && present[row]) return;
+    const float z[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    put_row(out.base, out.base_stride, out.grad, out.grad_stride, row, c, s.cols, 0.0f, z);
+}
+__global__ __launch_bounds__(256) void fill_rows(Groups s, Result out, const uint8_t* __restrict__ present) {
+    const u32 i = blockIdx.x * 256 + threadIdx.x;
+    if (i < s.n) fill_group(out, s, i, present);
+}
+
+// Few tokens: one launch.  A block stands for one token place and some columns; the block of a token's first place adds up the rows
+// of all its places, in order; the others end.  Every block looks through all tokens, so the work grows with their square.
 template <class T, bool DROP>
-__global__ __launch_bounds__(256) void grad_by_first(const int64_t* __restrict__ tokens, u32 n, u32 cols, u32 groups, u64 vocab, float scale, Mask m,
-                                                     const typename T::elem* __restrict__ dy, u64 dy_stride, float* grad, u64 grad_stride) {
+__global__ __launch_bounds__(256) void grad_by_first(const int64_t* __restrict__ tokens, u32 n, u32 cols, u32 groups, Result out, Mask m,
+                                                     const typename T::elem* __restrict__ dy, u64 dy_stride) {
     __shared__ u32 places[256];
     __shared__ u32 in_wave[4];
     const u32 t = blockIdx.x, tid = threadIdx.x, nt = blockDim.x;
     const u64 tok = (u64)tokens[t];
-    if (tok >= vocab) return;
+    if (tok >= out.vocab) return;
     int earlier = 0;
     for (u32 j = tid; j < t; j += nt) earlier |= (u64)tokens[j] == tok;
     if (__syncthreads_or(earlier)) return;
@@ -215,12 +228,282 @@ __global__ __launch_bounds__(256) void grad_by_first(const int64_t* __restrict__
             }
         __syncthreads();
     }
-    if (c >= cols) return;
-    float v[8];
-    float* row = grad + tok * grad_stride;
-    load_group<F32>(row, c, cols, v);
-    for (int e = 0; e < 8; ++e) v[e] += scale * sum[e];
-    store_group<F32>(row, c, cols, v);
+    if (c < cols) put_row(out.base, out.base_stride, out.grad, out.grad_stride, tok, c, cols, out.scale, sum);
+}
+
+// ---- the sort: least significant digit first, at most nine bits a pass ----
+#define BINS 512
+#define NO_TOKEN(vocab) ((u32)(vocab))          // key of a place without a token: behind all others
+
+__device__ __forceinline__ u32 key_of(int64_t token, u64 vocab) { return (u64)token < vocab ? (u32)token : NO_TOKEN(vocab); }
+
+// Lanes whose digit is this lane's.
+__device__ __forceinline__ u64 same_digit(u32 digit, u32 bits, bool there) {
+    u64 m = __ballot(there);
+    for (u32 b = 0; b < bits; ++b) {
+        const bool one = (digit >> b) & 1;
+        const u64 v = __ballot(one);
+        m &= one ? v : ~v;
+    }
+    return m;
+}
+// Place of this lane's item among its wave's items of the same digit so far, counted up in the wave's own counters.  The counter is
+// read by the lane that adds to it, and handed to the others.
+__device__ __forceinline__ u32 rank_digit(u32* counts, u32 digit, u32 bits, bool there) {
+    const u64 m = same_digit(digit, bits, there);
+    const u32 lane = threadIdx.x & 63, first = (u32)__ffsll((long long)m) - 1;
+    u32 old = 0;
+    if (there && lane == first) old = atomicAdd(&counts[digit], (u32)__popcll(m));
+    old = (u32)__shfl((int)old, (int)(there ? first : lane));
+    return old + (u32)__popcll(m & ((1ull << lane) - 1));
+}
+// Exclusive sum over the block's threads (NT a multiple of 64); `part`: one word for each wave.
+template <int NT>
+__device__ __forceinline__ u32 scan_block(u32 v, u32* part) {
+    const u32 lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    u32 s = v;
+    for (int d = 1; d < WAVE; d <<= 1) { const u32 o = __shfl_up(s, d); if ((int)lane >= d) s += o; }
+    __syncthreads();
+    if (lane == 63) part[w] = s;
+    __syncthreads();
+    u32 before = 0;
+    for (u32 i = 0; i < NT / WAVE; ++i) if (i < w) before += part[i];
+    return before + s - v;
+}
+
+struct SortShape { u32 n, passes, bits; u64 vocab; };        // bits: of a digit
+
+// All places of a short batch by one block, keys and places in LDS between the passes; the launch's other blocks write the result's rows
+// meanwhile (all of them: rows with a token are written again, they are few next to the table).
+#define SORT_BLOCK_ROWS 16
+#define SORT_BLOCK_MOST (1024 * SORT_BLOCK_ROWS)
+struct SortLds { u32 keys[SORT_BLOCK_MOST]; u16 places[SORT_BLOCK_MOST]; u32 counts[16][BINS]; u32 part[16]; };
+
+__global__ __launch_bounds__(1024) void sort_one_block(SortShape q, const int64_t* __restrict__ tokens, u32* __restrict__ keys_out, u32* __restrict__ places_out, u32* __restrict__ n_chains,
+                                                       Groups s, Result out) {
+    __shared__ SortLds L;
+    const u32 tid = threadIdx.x;
+    if (blockIdx.x) {
+        for (u32 i = (blockIdx.x - 1) * 1024 + tid; i < s.n; i += (gridDim.x - 1) * 1024) fill_group(out, s, i, nullptr);
+        return;
+    }
+    const u32 lane = tid & 63, w = tid >> 6;
+    const u32 rows = (q.n + 1023) / 1024;                // of 64 places, of each wave
+    if (tid == 0) *n_chains = 0;
+    u32 key[SORT_BLOCK_ROWS], place[SORT_BLOCK_ROWS], rank[SORT_BLOCK_ROWS];
+#pragma unroll
+    for (u32 r = 0; r < SORT_BLOCK_ROWS; ++r) {
+        const u32 i = (w * rows + r) * 64 + lane;
+        if (r < rows && i < q.n) { key[r] = key_of(tokens[i], q.vocab); place[r] = i; }
+    }
+    for (u32 pass = 0; pass < q.passes; ++pass) {
+        for (u32 i = tid; i < 16 * BINS; i += 1024) (&L.counts[0][0])[i] = 0;
+        __syncthreads();
+        const u32 shift = pass * q.bits, mask = (1u << q.bits) - 1;
+#pragma unroll
+        for (u32 r = 0; r < SORT_BLOCK_ROWS; ++r)
+            if (r < rows) {
+                const bool there = (w * rows + r) * 64 + lane < q.n;
+                rank[r] = rank_digit(L.counts[w], (key[r] >> shift) & mask, q.bits, there);
+            }
+        __syncthreads();
+        u32 sum = 0;
+        if (tid < BINS)
+            for (u32 i = 0; i < 16; ++i) { const u32 c = L.counts[i][tid]; L.counts[i][tid] = sum; sum += c; }
+        const u32 before = scan_block<1024>(sum, L.part);
+        if (tid < BINS)
+            for (u32 i = 0; i < 16; ++i) L.counts[i][tid] += before;
+        __syncthreads();
+        const bool last = pass + 1 == q.passes;
+#pragma unroll
+        for (u32 r = 0; r < SORT_BLOCK_ROWS; ++r)
+            if (r < rows && (w * rows + r) * 64 + lane < q.n) {
+                const u32 to = L.counts[w][(key[r] >> shift) & mask] + rank[r];
+                if (last) { keys_out[to] = key[r]; places_out[to] = place[r]; }
+                else { L.keys[to] = key[r]; L.places[to] = (u16)place[r]; }
+            }
+        if (last) break;
+        __syncthreads();
+#pragma unroll
+        for (u32 r = 0; r < SORT_BLOCK_ROWS; ++r) {
+            const u32 i = (w * rows + r) * 64 + lane;
+            if (r < rows && i < q.n) { key[r] = L.keys[i]; place[r] = L.places[i]; }
+        }
+    }
+}
+
+// Longer batches: at most SORT_TILES tiles, two launches a pass (count, move).  The first launch clears the marks of the rows that have a token, the
+// second sets them, the last two fill the rows that have none beside their own work.
+#define SORT_TILES 64
+#define SORT_STEP 1024                           // items that a block of 256 threads moves at once
+struct SortFrom { const int64_t* tokens; const u32 *keys, *places; };            // tokens in the first pass, keys and places later
+
+__device__ __forceinline__ u32 key_at(const SortFrom& f, u64 vocab, u32 i) { return f.tokens ? key_of(f.tokens[i], vocab) : f.keys[i]; }
+
+__global__ __launch_bounds__(256) void sort_count(SortShape q, SortFrom from, u32 shift, u32 tile, u32 tiles, u32* __restrict__ hist, u32* __restrict__ n_chains, u32* __restrict__ clear, u32 clear_words,
+                                                  Groups s, Result out, const uint8_t* __restrict__ present) {
+    __shared__ u32 counts[BINS];
+    const u32 tid = threadIdx.x;
+    if (blockIdx.x >= tiles) {
+        const u32 at = (blockIdx.x - tiles) * 256 + tid, step = (gridDim.x - tiles) * 256;
+        for (u32 i = at; i < clear_words; i += step) clear[i] = 0;
+        for (u32 i = at; i < s.n; i += step) fill_group(out, s, i, present);
+        return;
+    }
+    if (blockIdx.x == 0 && tid == 0) *n_chains = 0;
+    for (u32 b = tid; b < BINS; b += 256) counts[b] = 0;
+    __syncthreads();
+    const u32 mask = (1u << q.bits) - 1, lo = blockIdx.x * tile, hi = q.n - lo < tile ? q.n : lo + tile;
+    for (u32 i = lo + tid; i < hi; i += 256) atomicAdd(&counts[(key_at(from, q.vocab, i) >> shift) & mask], 1u);
+    __syncthreads();
+    for (u32 b = tid; b < BINS; b += 256) hist[blockIdx.x * BINS + b] = counts[b];
+}
+
+__global__ __launch_bounds__(256) void sort_move(SortShape q, SortFrom from, u32 shift, u32 tile, u32 tiles, const u32* __restrict__ hist, u32* __restrict__ keys_to, u32* __restrict__ places_to,
+                                                 uint8_t* __restrict__ mark, Groups s, Result out, const uint8_t* __restrict__ present) {
+    __shared__ u32 counts[4][BINS];
+    __shared__ u32 next[BINS];                   // where the next item of a digit goes
+    __shared__ u32 part[4];
+    const u32 tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (blockIdx.x >= tiles) {
+        for (u32 i = (blockIdx.x - tiles) * 256 + tid; i < s.n; i += (gridDim.x - tiles) * 256) fill_group(out, s, i, present);
+        return;
+    }
+    u32 total[2] = {0, 0}, mine[2] = {0, 0};
+#pragma unroll 8
+    for (u32 t = 0; t < tiles; ++t) {
+        const uint2 c = *(const uint2*)(hist + t * BINS + 2 * tid);
+        if (t < blockIdx.x) { mine[0] += c.x; mine[1] += c.y; }
+        total[0] += c.x; total[1] += c.y;
+    }
+    const u32 before = scan_block<256>(total[0] + total[1], part);
+    next[2 * tid] = before + mine[0];
+    next[2 * tid + 1] = before + total[0] + mine[1];
+    const u32 mask = (1u << q.bits) - 1, lo = blockIdx.x * tile, hi = q.n - lo < tile ? q.n : lo + tile;
+    for (u32 at = lo; at < hi; at += SORT_STEP) {
+        for (u32 i = tid; i < 4 * BINS; i += 256) (&counts[0][0])[i] = 0;
+        __syncthreads();
+        u32 key[4], place[4], rank[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const u32 i = at + (w * 4 + r) * 64 + lane;
+            if (i < hi) { key[r] = key_at(from, q.vocab, i); place[r] = from.tokens ? i : from.places[i]; }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) rank[r] = rank_digit(counts[w], (key[r] >> shift) & mask, q.bits, at + (w * 4 + r) * 64 + lane < hi);
+        __syncthreads();
+        for (u32 b = tid; b < BINS; b += 256) {
+            u32 sum = next[b];
+            for (int i = 0; i < 4; ++i) { const u32 c = counts[i][b]; counts[i][b] = sum; sum += c; }
+            next[b] = sum;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (at + (w * 4 + r) * 64 + lane < hi) {
+                const u32 to = counts[w][(key[r] >> shift) & mask] + rank[r];
+                keys_to[to] = key[r];
+                places_to[to] = place[r];
+                if (mark && key[r] != NO_TOKEN(q.vocab)) mark[key[r]] = 1;
+            }
+        __syncthreads();
+    }
+}
+
+// ---- the sums over the sorted places ----
+// A thread takes eight columns of a piece of LEN sorted places.  A run (the places of one token) is summed by the piece it begins in, also where it ends in the next one.
+// A run that covers the whole next piece is long: its pieces' sums go to `chain` (two rows a piece: [0] of a run that comes from before, [1] of one that goes on)
+// and are added up by the next launch.  The pieces know which it is from the keys at their borders.
+template <class T, bool DROP, int LEN>
+__global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys, const u32* __restrict__ places, u32 n, Groups s, Result out, Mask m, const typename T::elem* __restrict__ dy, u64 dy_stride,
+                                                   float* __restrict__ chain, u32* __restrict__ chains, u32* __restrict__ n_chains) {
+    const u32 i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= s.n) return;
+    const u32 groups = s.per_row.d, local = s.per_row.of(i), g = i - local * groups, c = g * 8;
+    const u32 piece = (u32)s.row0 + local, p0 = piece * LEN, p1 = n - p0 < LEN ? n : p0 + LEN;
+    const u32 none = NO_TOKEN(out.vocab), k0 = keys[p0];
+    if (k0 == none) return;
+    float* const slot = chain + ((u64)piece * 2 * groups + g) * 8;
+    u32 from = p0, to = p1;
+    bool first_to_chain = false, last_to_chain = false;
+    if (p0 && keys[p0 - 1] == k0) {
+        first_to_chain = (p0 > LEN && keys[p0 - LEN - 1] == k0) || (p1 - p0 == LEN && keys[p1 - 1] == k0);
+        if (!first_to_chain) {
+#pragma unroll
+            for (u32 j = 0; j < LEN; ++j) from += p0 + j < p1 && keys[p0 + j] == k0;
+        }
+    }
+    const u32 k1 = keys[p1 - 1];
+    if (p1 < n && k1 != none && keys[p1] == k1 && !(first_to_chain && k1 == k0)) {
+        last_to_chain = n - p1 >= LEN && keys[p1 + LEN - 1] == k1;
+        // a run that came from before and ends in this piece's last place is not this piece's to go on with: `from` is p1 then
+        if (!last_to_chain && from < p1) {
+#pragma unroll
+            for (u32 j = 0; j < LEN; ++j) to += p1 + j < n && keys[p1 + j] == k1;
+        }
+    }
+    const u64 draw = DROP ? draw_of(m) : 0;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (u32 at = from; at < to; at += 4) {
+        u32 k[5], row[4];
+        float v[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            k[j] = at + j < to ? keys[at + j] : none;
+            row[j] = at + j < to ? places[at + j] : 0;
+        }
+        k[4] = at + 4 < to ? keys[at + 4] : none;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (k[j] != none) load_group<T>(dy + (u64)row[j] * dy_stride, c, s.cols, v[j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (k[j] == none) continue;
+            if (DROP) gate8(m, draw, (u64)row[j] * groups + g, v[j]);
+            for (int e = 0; e < 8; ++e) sum[e] += v[j][e];
+            if (k[j + 1] == k[j]) continue;
+            if (first_to_chain && k[j] == k0) {
+                F32::put8(slot, sum);
+            } else if (last_to_chain && k[j] == k1) {
+                F32::put8(slot + (u64)groups * 8, sum);
+                if (g == 0) chains[atomicAdd(n_chains, 1u)] = piece;           // in any order: the chains have nothing to do with each other
+            } else {
+                put_row(out.base, out.base_stride, out.grad, out.grad_stride, k[j], c, s.cols, out.scale, sum);
+            }
+            for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+        }
+    }
+}
+
+// The long runs: a block takes a chain and 16 groups of columns; 16 threads share the pieces of each.
+__global__ __launch_bounds__(256) void grad_chains(const u32* __restrict__ keys, u32 n, u32 len, u32 cols, u32 groups, Result out, const float* __restrict__ chain, const u32* __restrict__ chains,
+                                                   const u32* __restrict__ n_chains) {
+    __shared__ float sh[16][16][8 + 1];
+    const u32 gl = threadIdx.x & 15, strand = threadIdx.x >> 4, g = blockIdx.y * 16 + gl, all = *n_chains;
+    for (u32 i = blockIdx.x; i < all; i += gridDim.x) {
+        const u32 piece = chains[i];
+        const u32 k = keys[(piece + 1) * len];             // the run covers the next piece
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (g < groups) {
+            if (strand == 0) F32::get8(chain + (((u64)piece * 2 + 1) * groups + g) * 8, sum);
+            for (u32 p = piece + 1 + strand; (u64)p * len < n && keys[p * len] == k; p += 16) {
+                float v[8];
+                F32::get8(chain + ((u64)p * 2 * groups + g) * 8, v);
+                for (int e = 0; e < 8; ++e) sum[e] += v[e];
+            }
+        }
+        for (int e = 0; e < 8; ++e) sh[strand][gl][e] = sum[e];
+        for (u32 half = 8; half; half >>= 1) {
+            __syncthreads();
+            if (strand < half)
+                for (int e = 0; e < 8; ++e) sh[strand][gl][e] += sh[strand + half][gl][e];
+        }
+        if (strand == 0 && g < groups) {
+            for (int e = 0; e < 8; ++e) sum[e] = sh[0][gl][e];
+            put_row(out.base, out.base_stride, out.grad, out.grad_stride, k, g * 8, cols, out.scale, sum);
+        }
+        __syncthreads();
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -479,9 +762,81 @@ extern "C" int dblp_embed(int device, void* stream, const int64_t* d_tokens, uin
     return launched(call);
 }
 
+// How the places of a batch are sorted and cut, and where its intermediate results lie in the workspace.
+struct GradPlan {
+    bool short_batch;            // one launch
+    u32 len, pieces, passes, bits, tile, tiles;
+    u64 keys[2], places[2], hist, present, chains, n_chains, chain, bytes;
+};
+#define GRAD_SHORT 512
+
+static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
+    GradPlan p = {};
+    p.short_batch = n <= GRAD_SHORT;
+    p.bytes = 256;
+    if (p.short_batch) return p;
+    const u64 groups = ((u64)dim + 7) / 8;
+    u32 bits = 0;
+    while ((vocab >> bits) != 0) ++bits;                 // keys run to vocab itself
+    p.passes = (bits + 8) / 9;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    p.len = n <= SORT_BLOCK_MOST ? 8 : 16;
+    p.pieces = (u32)((n + p.len - 1) / p.len);
+    p.tile = (u32)round_up((n + SORT_TILES - 1) / SORT_TILES, SORT_STEP);
+    p.tiles = (u32)((n + p.tile - 1) / p.tile);
+    u64 at = 0;
+    const auto take = [&](u64 bytes) { const u64 here = at; at += round_up(bytes, 256); return here; };
+    for (int i = 0; i < 2; ++i) { p.keys[i] = take(4 * n); p.places[i] = take(4 * n); }
+    p.hist = take(4ull * SORT_TILES * BINS);
+    p.present = take(vocab);
+    p.chains = take(4ull * p.pieces);
+    p.n_chains = take(4);
+    p.chain = take((u64)p.pieces * 2 * groups * 8 * 4);
+    p.bytes = at;
+    return p;
+}
+
 extern "C" uint64_t dblp_embed_grad_workspace(uint64_t n_tokens, uint64_t vocab, uint32_t dim) {
     if (n_tokens >= COUNT_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT || dim == 0 || dim >= COUNT_LIMIT) return 0;
-    return 256;
+    return grad_plan(n_tokens, vocab, dim).bytes;
+}
+
+// The launches that put the places in order and, unless the result is in place, write the rows that have no token.
+// Returns which of the two buffers holds the sorted keys and places.
+static int sort_places(const GradPlan& p, const int64_t* tokens, u32 n, u32 dim, const Result& out, uint8_t* ws, hipStream_t stream) {
+    const bool in_place = out.base == out.grad;
+    const SortShape q = {n, p.passes, p.bits, out.vocab};
+    u32* const n_chains = (u32*)(ws + p.n_chains);
+    const u32 per_row = (u32)((dim + 7ull) / 8);
+    const auto rows = [&](u64 row0, u64 count) { return Groups{row0, (u32)(count * per_row), dim, Divider::by(per_row)}; };
+    // one launch's share of the rows fits 31 bits of groups, or they are filled apart
+    const bool beside = !in_place && out.vocab * per_row < COUNT_LIMIT;
+    if (n <= SORT_BLOCK_MOST) {
+        const Groups s = rows(0, beside ? out.vocab : 0);
+        if (!in_place && !beside)
+            each_launch(out.vocab, dim, [&](Groups a) { hipLaunchKernelGGL(fill_rows, blocks_of(a), dim3(256), 0, stream, a, out, (const uint8_t*)nullptr); });
+        const u32 fillers = (u32)((s.n + 4095ull) / 4096);
+        hipLaunchKernelGGL(sort_one_block, dim3(1 + fillers), dim3(1024), 0, stream, q, tokens, (u32*)(ws + p.keys[0]), (u32*)(ws + p.places[0]), n_chains, s, out);
+        return 0;
+    }
+    uint8_t* const present = ws + p.present;
+    u32* const hist = (u32*)(ws + p.hist);
+    int to = 0;
+    for (u32 pass = 0; pass < p.passes; ++pass) {
+        const SortFrom from = {pass ? nullptr : tokens, pass ? (u32*)(ws + p.keys[to ^ 1]) : nullptr, pass ? (u32*)(ws + p.places[to ^ 1]) : nullptr};
+        const bool first = pass == 0, last = pass + 1 == p.passes;
+        const u64 half = out.vocab / 2;
+        const Groups lower = rows(0, beside && last && !first ? half : 0), upper = rows(half, beside && last && !first ? out.vocab - half : 0);
+        const u32 clear = first && !in_place ? (u32)(round_up(out.vocab, 256) / 4) : 0;
+        const auto fillers = [&](u64 groups, u64 words) { const u64 b = (groups + 1023) / 1024 + (words + 1023) / 1024; return (u32)b; };
+        hipLaunchKernelGGL(sort_count, dim3(p.tiles + fillers(lower.n, clear)), dim3(256), 0, stream, q, from, pass * p.bits, p.tile, p.tiles, hist, n_chains, (u32*)present, clear, lower, out, (const uint8_t*)present);
+        hipLaunchKernelGGL(sort_move, dim3(p.tiles + fillers(upper.n, 0)), dim3(256), 0, stream, q, from, pass * p.bits, p.tile, p.tiles, (const u32*)hist, (u32*)(ws + p.keys[to]), (u32*)(ws + p.places[to]),
+                           first && !in_place ? present : (uint8_t*)nullptr, upper, out, (const uint8_t*)present);
+        to ^= 1;
+    }
+    if (!in_place && (!beside || p.passes == 1))
+        each_launch(out.vocab, dim, [&](Groups a) { hipLaunchKernelGGL(fill_rows, blocks_of(a), dim3(256), 0, stream, a, out, (const uint8_t*)present); });
+    return to ^ 1;
 }
 
 extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens, uint64_t n_tokens, uint32_t dim, uint64_t vocab,
@@ -500,19 +855,34 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
     if (const int rc = take_drop(call, h_drop, &m)) return rc;
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
-    const u32 groups = (dim + 7) / 8;
-    if (d_base != d_grad)
-        each_launch(vocab, dim, [&](Groups s) {
-            hipLaunchKernelGGL(grad_begin, blocks_of(s), dim3(256), 0, (hipStream_t)stream, s, d_base, (u64)base_stride, d_grad, (u64)grad_stride);
+    const hipStream_t st = (hipStream_t)stream;
+    const Result out = {d_base, base_stride, d_grad, grad_stride, vocab, scale};
+    const GradPlan p = grad_plan(n_tokens, vocab, dim);
+    const u32 n = (u32)n_tokens, groups = (u32)((dim + 7ull) / 8);
+    if (p.short_batch) {
+        if (d_base != d_grad)
+            each_launch(vocab, dim, [&](Groups s) { hipLaunchKernelGGL(fill_rows, blocks_of(s), dim3(256), 0, st, s, out, (const uint8_t*)nullptr); });
+        if (n)
+            by_type(dy_type, [&](auto tt) {
+                typedef decltype(tt) T;
+                const u32 nt = groups >= 256 ? 256 : (groups + 63) / 64 * 64;
+                const auto kernel = m.limit ? grad_by_first<T, true> : grad_by_first<T, false>;
+                hipLaunchKernelGGL(kernel, dim3(n, (groups + nt - 1) / nt), dim3(nt), 0, st, d_tokens, n, dim, groups, out, m, (const typename T::elem*)d_dy, (u64)dy_stride);
+            });
+        return launched(call);
+    }
+    uint8_t* const ws = (uint8_t*)d_workspace;
+    const int at = sort_places(p, d_tokens, n, dim, out, ws, st);
+    u32 *const keys = (u32*)(ws + p.keys[at]), *const places = (u32*)(ws + p.places[at]), *const chains = (u32*)(ws + p.chains), *const n_chains = (u32*)(ws + p.n_chains);
+    float* const chain = (float*)(ws + p.chain);
+    by_type(dy_type, [&](auto tt) {
+        typedef decltype(tt) T;
+        each_launch(p.pieces, dim, [&](Groups s) {
+            const auto kernel = p.len == 8 ? (m.limit ? grad_pieces<T, true, 8> : grad_pieces<T, false, 8>) : (m.limit ? grad_pieces<T, true, 16> : grad_pieces<T, false, 16>);
+            hipLaunchKernelGGL(kernel, blocks_of(s), dim3(256), 0, st, (const u32*)keys, (const u32*)places, n, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride, chain, chains, n_chains);
         });
-    if (n_tokens)
-        by_type(dy_type, [&](auto tt) {
-            typedef decltype(tt) T;
-            const u32 nt = groups >= 256 ? 256 : (groups + 63) / 64 * 64;
-            const auto kernel = m.limit ? grad_by_first<T, true> : grad_by_first<T, false>;
-            hipLaunchKernelGGL(kernel, dim3((u32)n_tokens, (groups + nt - 1) / nt), dim3(nt), 0, (hipStream_t)stream, d_tokens, (u32)n_tokens, dim, groups, (u64)vocab, scale, m,
-                               (const typename T::elem*)d_dy, (u64)dy_stride, d_grad, (u64)grad_stride);
-        });
+    });
+    hipLaunchKernelGGL(grad_chains, dim3(p.pieces < 256 ? p.pieces : 256, (groups + 15) / 16), dim3(256), 0, st, (const u32*)keys, n, p.len, dim, groups, out, (const float*)chain, (const u32*)chains, (const u32*)n_chains);
     return launched(call);
 }
 
