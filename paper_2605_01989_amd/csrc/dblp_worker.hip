@@ -28,13 +28,27 @@ typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef float f8v __attribute__((ext_vector_type(8)));
 
+// Each type: `raw`, eight elements as they lie in memory, loaded apart from their conversion so that several loads can be in flight.
 struct F32 {
     typedef float elem;
+    struct raw { f4v a, b; };
     static __device__ __forceinline__ float get(const float* p) { return *p; }
     static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
-    static __device__ __forceinline__ void get8(const float* p, float (&v)[8]) {
-        const f4v a = *(const f4v_a4*)p, b = *(const f4v_a4*)(p + 4);
-        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    static __device__ __forceinline__ raw load(const float* p) { return {*(const f4v_a4*)p, *(const f4v_a4*)(p + 4)}; }
+    static __device__ __forceinline__ raw some(const float* p, u32 n) {
+        raw r = {};
+        for (u32 i = 0; i < 7; ++i) if (i < n) { if (i < 4) r.a[i] = p[i]; else r.b[i - 4] = p[i]; }
+        return r;
+    }
+    static __device__ __forceinline__ raw down(raw r, u32 by) {           // by 0..7 elements, zeros behind
+        float v[8];
+        open(r, v);
+        for (u32 step = 4; step; step >>= 1)
+            for (u32 i = 0; i < 8; ++i) { const float from = i + step < 8 ? v[i + step] : 0.0f; v[i] = (by & step) ? from : v[i]; }
+        return {{v[0], v[1], v[2], v[3]}, {v[4], v[5], v[6], v[7]}};
+    }
+    static __device__ __forceinline__ void open(const raw& r, float (&v)[8]) {
+        for (int i = 0; i < 4; ++i) { v[i] = r.a[i]; v[4 + i] = r.b[i]; }
     }
     static __device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
         const f4v a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
@@ -46,10 +60,23 @@ struct F32 {
 template <class E, class V8>
 struct Half {
     typedef E elem;
+    typedef u4v raw;
     static __device__ __forceinline__ float get(const E* p) { return (float)*p; }
     static __device__ __forceinline__ void put(E* p, float v) { *p = (E)v; }
-    static __device__ __forceinline__ void get8(const E* p, float (&v)[8]) {
-        const f8v f = __builtin_convertvector(__builtin_bit_cast(V8, (u4v)*(const u4v_a2*)p), f8v);
+    static __device__ __forceinline__ raw load(const E* p) { return *(const u4v_a2*)p; }
+    static __device__ __forceinline__ raw some(const E* p, u32 n) {
+        V8 r = {};
+        for (u32 i = 0; i < 7; ++i) if (i < n) r[i] = p[i];
+        return __builtin_bit_cast(u4v, r);
+    }
+    static __device__ __forceinline__ raw down(raw r, u32 by) {
+        if (by & 4) r = (u4v){r.z, r.w, 0u, 0u};
+        if (by & 2) r = (u4v){r.y, r.z, r.w, 0u};
+        if (by & 1) r = (u4v){r.x >> 16 | r.y << 16, r.y >> 16 | r.z << 16, r.z >> 16 | r.w << 16, r.w >> 16};
+        return r;
+    }
+    static __device__ __forceinline__ void open(const raw& r, float (&v)[8]) {
+        const f8v f = __builtin_convertvector(__builtin_bit_cast(V8, r), f8v);
         for (int i = 0; i < 8; ++i) v[i] = f[i];
     }
     static __device__ __forceinline__ void put8(E* p, const float (&v)[8]) {
@@ -60,12 +87,18 @@ struct Half {
 typedef Half<__bf16, bf8v> BF16;
 typedef Half<_Float16, h8v> F16;
 
-// Columns [c, c + 8) of a row of `cols`; those past the end read as zero and are not written.
-template <class T>
-__device__ __forceinline__ void load_group(const typename T::elem* row, u32 c, u32 cols, float (&v)[8]) {
-    if (c + 8 <= cols) { T::get8(row + c, v); return; }
-    for (u32 i = 0; i < 8; ++i) v[i] = c + i < cols ? T::get(row + c + i) : 0.0f;
+// Columns [c, c + 8) of a row of `cols`; those past the end read as zero and are not written.  WHOLE: cols is a multiple of eight.
+// Otherwise the last group of a row is read from the row's last eight elements and shifted down in registers: one load for every
+// group, without a branch that would have to wait for it (rows of fewer than eight elements apart).
+template <class T, bool WHOLE>
+__device__ __forceinline__ typename T::raw load_raw(const typename T::elem* row, u32 c, u32 cols) {
+    if (WHOLE) return T::load(row + c);
+    if (cols < 8) return T::some(row, cols);
+    const u32 at = c + 8 <= cols ? c : cols - 8;
+    return T::down(T::load(row + at), c - at);
 }
+template <class T>
+__device__ __forceinline__ void load_group(const typename T::elem* row, u32 c, u32 cols, float (&v)[8]) { T::open(load_raw<T, false>(row, c, cols), v); }
 template <class T>
 __device__ __forceinline__ void store_group(typename T::elem* row, u32 c, u32 cols, const float (&v)[8]) {
     if (c + 8 <= cols) { T::put8(row + c, v); return; }
@@ -124,46 +157,78 @@ __device__ __forceinline__ u64 draw_of(const Mask& m) { return m.draw + (m.d_dra
 // dropout and embedding: a thread takes eight columns of a row; groups of eight are numbered through the matrix
 // ------------------------------------------------------------------------------------------
 struct Groups { u64 row0; u32 n, cols; Divider per_row; };     // groups of this launch (below 2^31), first row of it
+#define GROUPS_EACH 2           // groups that a thread has in flight
 
-template <class T, bool RES>
+template <class T, bool RES, bool WHOLE>
 __global__ __launch_bounds__(256) void dropout_groups(Groups s, Mask m, const typename T::elem* x, u64 x_stride,
                                                       const typename T::elem* res, u64 res_stride, typename T::elem* y, u64 y_stride) {
-    const u32 i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= s.n) return;
-    const u32 r = s.per_row.of(i), c = (i - r * s.per_row.d) * 8;
-    const u64 row = s.row0 + r;
-    float v[8], w[8];
-    load_group<T>(x + row * x_stride, c, s.cols, v);
-    if (RES) load_group<T>(res + row * res_stride, c, s.cols, w);
-    gate8(m, draw_of(m), s.row0 * s.per_row.d + i, v);
-    if (RES) for (int k = 0; k < 8; ++k) v[k] += w[k];
-    store_group<T>(y + row * y_stride, c, s.cols, v);
+    const u32 i0 = blockIdx.x * (256 * GROUPS_EACH) + threadIdx.x;
+    typename T::raw a[GROUPS_EACH], b[GROUPS_EACH];
+    u32 c[GROUPS_EACH];
+    u64 row[GROUPS_EACH];
+#pragma unroll
+    for (int j = 0; j < GROUPS_EACH; ++j) {
+        const u32 i = i0 + j * 256, r = s.per_row.of(i);
+        c[j] = (i - r * s.per_row.d) * 8;
+        row[j] = s.row0 + r;
+        if (i >= s.n) continue;
+        a[j] = load_raw<T, WHOLE>(x + row[j] * x_stride, c[j], s.cols);
+        if (RES) b[j] = load_raw<T, WHOLE>(res + row[j] * res_stride, c[j], s.cols);
+    }
+    const u64 draw = draw_of(m);
+#pragma unroll
+    for (int j = 0; j < GROUPS_EACH; ++j) {
+        const u32 i = i0 + j * 256;
+        if (i >= s.n) continue;
+        float v[8], w[8];
+        T::open(a[j], v);
+        gate8(m, draw, s.row0 * s.per_row.d + i, v);
+        if (RES) {
+            T::open(b[j], w);
+            for (int k = 0; k < 8; ++k) v[k] += w[k];
+        }
+        store_group<T>(y + row[j] * y_stride, c[j], s.cols, v);
+    }
 }
 
-template <class S, class T, bool DROP>
+template <class S, class T, bool DROP, bool WHOLE>
 __global__ __launch_bounds__(256) void embed_groups(Groups s, Mask m, const int64_t* __restrict__ tokens, const typename S::elem* __restrict__ table, u64 table_stride, u64 vocab,
                                                     float scale, const int64_t* __restrict__ positions, const typename S::elem* __restrict__ pos_table, u64 pos_stride, u64 n_pos,
                                                     typename T::elem* __restrict__ out, u64 out_stride) {
-    const u32 i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= s.n) return;
-    const u32 r = s.per_row.of(i), c = (i - r * s.per_row.d) * 8;
-    const u64 row = s.row0 + r;
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const u64 tok = (u64)tokens[row];
-    if (tok < vocab) {
-        load_group<S>(table + tok * table_stride, c, s.cols, v);
-        for (int k = 0; k < 8; ++k) v[k] *= scale;
+    const u32 i0 = blockIdx.x * (256 * GROUPS_EACH) + threadIdx.x;
+    typename S::raw a[GROUPS_EACH], b[GROUPS_EACH];
+    u32 c[GROUPS_EACH];
+    u64 row[GROUPS_EACH], tok[GROUPS_EACH], at[GROUPS_EACH];
+#pragma unroll
+    for (int j = 0; j < GROUPS_EACH; ++j) {
+        const u32 i = i0 + j * 256, r = s.per_row.of(i);
+        c[j] = (i - r * s.per_row.d) * 8;
+        row[j] = s.row0 + r;
+        tok[j] = i < s.n ? (u64)tokens[row[j]] : vocab;
+        at[j] = i < s.n && positions ? (u64)positions[row[j]] : n_pos;
     }
-    if (positions) {
-        const u64 at = (u64)positions[row];
-        if (at < n_pos) {
-            float w[8];
-            load_group<S>(pos_table + at * pos_stride, c, s.cols, w);
+#pragma unroll
+    for (int j = 0; j < GROUPS_EACH; ++j) {
+        if (tok[j] < vocab) a[j] = load_raw<S, WHOLE>(table + tok[j] * table_stride, c[j], s.cols);
+        if (at[j] < n_pos) b[j] = load_raw<S, WHOLE>(pos_table + at[j] * pos_stride, c[j], s.cols);
+    }
+    const u64 draw = DROP ? draw_of(m) : 0;
+#pragma unroll
+    for (int j = 0; j < GROUPS_EACH; ++j) {
+        const u32 i = i0 + j * 256;
+        if (i >= s.n) continue;
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, w[8];
+        if (tok[j] < vocab) {
+            S::open(a[j], v);
+            for (int k = 0; k < 8; ++k) v[k] *= scale;
+        }
+        if (at[j] < n_pos) {
+            S::open(b[j], w);
             for (int k = 0; k < 8; ++k) v[k] += w[k];
         }
+        if (DROP) gate8(m, draw, s.row0 * s.per_row.d + i, v);
+        store_group<T>(out + row[j] * out_stride, c[j], s.cols, v);
     }
-    if (DROP) gate8(m, draw_of(m), s.row0 * s.per_row.d + i, v);
-    store_group<T>(out + row * out_stride, c, s.cols, v);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -193,42 +258,92 @@ __global__ __launch_bounds__(256) void fill_rows(Groups s, Result out, const uin
     if (i < s.n) fill_group(out, s, i, present);
 }
 
-// Few tokens: one launch.  A block stands for one token place and some columns; the block of a token's first place adds up the rows
-// of all its places, in order; the others end.  Every block looks through all tokens, so the work grows with their square.
-template <class T, bool DROP>
-__global__ __launch_bounds__(256) void grad_by_first(const int64_t* __restrict__ tokens, u32 n, u32 cols, u32 groups, Result out, Mask m,
-                                                     const typename T::elem* __restrict__ dy, u64 dy_stride) {
-    __shared__ u32 places[256];
-    __shared__ u32 in_wave[4];
-    const u32 t = blockIdx.x, tid = threadIdx.x, nt = blockDim.x;
+// Few tokens: one launch.  A wave stands for one token place and 64 groups of columns.  It compares its token with all of them; the wave of
+// a token's first place adds up the rows of all its places, in order, and the others end.  The launch's other blocks write the rows that have no
+// token, each block with a list of which of its rows have one.
+#define GRAD_SHORT 512
+#define FILL_EACH 4                              // groups that a thread of a filling block writes
+
+template <class T, bool DROP, bool WHOLE>
+__global__ __launch_bounds__(256) void grad_short(const int64_t* __restrict__ tokens, u32 n, u32 cols, u32 groups, u32 lead_blocks, Groups rows, Result out, Mask m,
+                                                  const typename T::elem* __restrict__ dy, u64 dy_stride) {
+    const u32 tid = threadIdx.x;
+    if (blockIdx.x >= lead_blocks) {
+        __shared__ u32 taken[256 * FILL_EACH + 1];
+        const u32 i0 = (blockIdx.x - lead_blocks) * (256 * FILL_EACH), i1 = rows.n - i0 < 256 * FILL_EACH ? rows.n : i0 + 256 * FILL_EACH;
+        const u32 r0 = rows.per_row.of(i0), r1 = rows.per_row.of(i1 - 1);
+        for (u32 r = tid; r <= r1 - r0; r += 256) taken[r] = 0;
+        __syncthreads();
+        for (u32 j = tid; j < n; j += 256) {
+            const u64 r = (u64)tokens[j] - rows.row0 - r0;
+            if (r <= r1 - r0) taken[r] = 1;
+        }
+        __syncthreads();
+        F32::raw v[FILL_EACH];
+#pragma unroll
+        for (int k = 0; k < FILL_EACH; ++k) {
+            const u32 i = i0 + k * 256 + tid, r = rows.per_row.of(i), c = (i - r * groups) * 8;
+            v[k] = F32::raw{};
+            if (i < i1 && out.base) v[k] = load_raw<F32, WHOLE>(out.base + (rows.row0 + r) * out.base_stride, c, cols);
+        }
+#pragma unroll
+        for (int k = 0; k < FILL_EACH; ++k) {
+            const u32 i = i0 + k * 256 + tid, r = rows.per_row.of(i), c = (i - r * groups) * 8;
+            if (i >= i1 || taken[r - r0]) continue;
+            float y[8];
+            F32::open(v[k], y);
+            store_group<F32>(out.grad + (rows.row0 + r) * out.grad_stride, c, cols, y);
+        }
+        return;
+    }
+    const u32 lane = tid & 63, unit = blockIdx.x * 4 + (tid >> 6), chunk = unit / n, t = unit - chunk * n;
+    const u32 c = (chunk * 64 + lane) * 8;
+    if (chunk * 64 >= groups) return;
     const u64 tok = (u64)tokens[t];
     if (tok >= out.vocab) return;
-    int earlier = 0;
-    for (u32 j = tid; j < t; j += nt) earlier |= (u64)tokens[j] == tok;
-    if (__syncthreads_or(earlier)) return;
-    const u32 c = (blockIdx.y * nt + tid) * 8;
-    const u64 draw = DROP ? draw_of(m) : 0;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (u32 from = t; from < n; from += nt) {
-        const bool hit = from + tid < n && (u64)tokens[from + tid] == tok;
-        const u64 hits = __ballot(hit);
-        if ((tid & 63) == 0) in_wave[tid >> 6] = (u32)__popcll(hits);
-        __syncthreads();
-        u32 before = 0, all = 0;
-        for (u32 w = 0; w < nt / 64; ++w) { if (w < tid >> 6) before += in_wave[w]; all += in_wave[w]; }
-        if (hit) places[before + (u32)__popcll(hits & ((1ull << (tid & 63)) - 1))] = from + tid;
-        __syncthreads();
-        if (c < cols)
-            for (u32 k = 0; k < all; ++k) {
-                const u64 row = places[k];
-                float v[8];
-                load_group<T>(dy + row * dy_stride, c, cols, v);
-                if (DROP) gate8(m, draw, row * groups + c / 8, v);
-                for (int e = 0; e < 8; ++e) sum[e] += v[e];
-            }
-        __syncthreads();
+    u64 hits[GRAD_SHORT / 64];
+#pragma unroll
+    for (u32 k = 0; k < GRAD_SHORT / 64; ++k) {
+        const u32 j = k * 64 + lane;
+        hits[k] = __ballot(j < n && (u64)tokens[j < n ? j : 0] == tok);
     }
-    if (c < cols) put_row(out.base, out.base_stride, out.grad, out.grad_stride, tok, c, cols, out.scale, sum);
+    u64 earlier = 0;
+#pragma unroll
+    for (u32 k = 0; k < GRAD_SHORT / 64; ++k) earlier |= k < t / 64 ? hits[k] : k == t / 64 ? hits[k] & ((1ull << (t & 63)) - 1) : 0;
+    if (earlier) return;
+    const bool here = c < cols;
+    const u64 draw = DROP ? draw_of(m) : 0;
+    F32::raw base = {};
+    if (here && out.base) base = load_raw<F32, WHOLE>(out.base + tok * out.base_stride, c, cols);
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (u32 k = 0; k < GRAD_SHORT / 64; ++k)
+        for (u64 left = hits[k]; left;) {
+            u64 row[8];
+            bool there[8];
+            typename T::raw v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                there[q] = left != 0;
+                row[q] = k * 64 + (left ? (u32)__ffsll((long long)left) - 1 : 0);
+                left &= left - 1;
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) if (there[q] && here) v[q] = load_raw<T, WHOLE>(dy + row[q] * dy_stride, c, cols);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if (!there[q] || !here) continue;
+                float x[8];
+                T::open(v[q], x);
+                if (DROP) gate8(m, draw, row[q] * groups + c / 8, x);
+                for (int e = 0; e < 8; ++e) sum[e] += x[e];
+            }
+        }
+    if (!here) return;
+    float y[8];
+    F32::open(base, y);
+    for (int e = 0; e < 8; ++e) y[e] += out.scale * sum[e];
+    store_group<F32>(out.grad + tok * out.grad_stride, c, cols, y);
 }
 
 // ---- the sort: least significant digit first, at most nine bits a pass ----
@@ -272,6 +387,15 @@ __device__ __forceinline__ u32 scan_block(u32 v, u32* part) {
 }
 
 struct SortShape { u32 n, passes, bits; u64 vocab; };        // bits: of a digit
+#define KEY_PAD 64                               // entries without a token before the sorted list and behind it
+
+__device__ __forceinline__ void pad_lists(u32* keys, u32* places, u32 n, u64 vocab) {
+    if (threadIdx.x < KEY_PAD) {
+        keys[(int)threadIdx.x - KEY_PAD] = NO_TOKEN(vocab);
+        keys[n + threadIdx.x] = NO_TOKEN(vocab);
+        places[n + threadIdx.x] = 0;
+    }
+}
 
 // All places of a short batch by one block, keys and places in LDS between the passes; the launch's other blocks write the result's rows
 // meanwhile (all of them: rows with a token are written again, they are few next to the table).
@@ -290,6 +414,7 @@ __global__ __launch_bounds__(1024) void sort_one_block(SortShape q, const int64_
     const u32 lane = tid & 63, w = tid >> 6;
     const u32 rows = (q.n + 1023) / 1024;                // of 64 places, of each wave
     if (tid == 0) *n_chains = 0;
+    pad_lists(keys_out, places_out, q.n, q.vocab);
     u32 key[SORT_BLOCK_ROWS], place[SORT_BLOCK_ROWS], rank[SORT_BLOCK_ROWS];
 #pragma unroll
     for (u32 r = 0; r < SORT_BLOCK_ROWS; ++r) {
@@ -369,6 +494,7 @@ __global__ __launch_bounds__(256) void sort_move(SortShape q, SortFrom from, u32
         for (u32 i = (blockIdx.x - tiles) * 256 + tid; i < s.n; i += (gridDim.x - tiles) * 256) fill_group(out, s, i, present);
         return;
     }
+    if (blockIdx.x == 0) pad_lists(keys_to, places_to, q.n, q.vocab);
     u32 total[2] = {0, 0}, mine[2] = {0, 0};
 #pragma unroll 8
     for (u32 t = 0; t < tiles; ++t) {
@@ -413,54 +539,65 @@ __global__ __launch_bounds__(256) void sort_move(SortShape q, SortFrom from, u32
 // ---- the sums over the sorted places ----
 // A thread takes eight columns of a piece of LEN sorted places.  A run (the places of one token) is summed by the piece it begins in, also where it ends in the next one.
 // A run that covers the whole next piece is long: its pieces' sums go to `chain` (two rows a piece: [0] of a run that comes from before, [1] of one that goes on)
-// and are added up by the next launch.  The pieces know which it is from the keys at their borders.
-template <class T, bool DROP, int LEN>
-__global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys, const u32* __restrict__ places, u32 n, Groups s, Result out, Mask m, const typename T::elem* __restrict__ dy, u64 dy_stride,
+// and are added up by the next launch.  The pieces know which it is from the keys at their borders; the list of keys has KEY_PAD entries "none" before it and behind it, so
+// that nothing asks where it ends.  Eight places at a time: their rows, and the rows of the base, are all in flight before the first is added; the next eight keys with them.
+template <class T, bool DROP, int LEN, bool WHOLE>
+__global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys, const u32* __restrict__ places, Groups s, Result out, Mask m, const typename T::elem* __restrict__ dy, u64 dy_stride,
                                                    float* __restrict__ chain, u32* __restrict__ chains, u32* __restrict__ n_chains) {
     const u32 i = blockIdx.x * 256 + threadIdx.x;
     if (i >= s.n) return;
     const u32 groups = s.per_row.d, local = s.per_row.of(i), g = i - local * groups, c = g * 8;
-    const u32 piece = (u32)s.row0 + local, p0 = piece * LEN, p1 = n - p0 < LEN ? n : p0 + LEN;
-    const u32 none = NO_TOKEN(out.vocab), k0 = keys[p0];
-    if (k0 == none) return;
+    const u32 piece = (u32)s.row0 + local, none = NO_TOKEN(out.vocab);
+    const u32* const key = keys + (u64)piece * LEN;
+    const u32* const place = places + (u64)piece * LEN;
     float* const slot = chain + ((u64)piece * 2 * groups + g) * 8;
-    u32 from = p0, to = p1;
-    bool first_to_chain = false, last_to_chain = false;
-    if (p0 && keys[p0 - 1] == k0) {
-        first_to_chain = (p0 > LEN && keys[p0 - LEN - 1] == k0) || (p1 - p0 == LEN && keys[p1 - 1] == k0);
-        if (!first_to_chain) {
+    u4v own[LEN / 4], after[LEN / 4], at_k[2], at_p[2];
 #pragma unroll
-            for (u32 j = 0; j < LEN; ++j) from += p0 + j < p1 && keys[p0 + j] == k0;
-        }
-    }
-    const u32 k1 = keys[p1 - 1];
-    if (p1 < n && k1 != none && keys[p1] == k1 && !(first_to_chain && k1 == k0)) {
-        last_to_chain = n - p1 >= LEN && keys[p1 + LEN - 1] == k1;
-        // a run that came from before and ends in this piece's last place is not this piece's to go on with: `from` is p1 then
-        if (!last_to_chain && from < p1) {
+    for (int j = 0; j < LEN / 4; ++j) { own[j] = ((const u4v*)key)[j]; after[j] = ((const u4v*)(key + LEN))[j]; }
+    at_p[0] = ((const u4v*)place)[0];
+    at_p[1] = ((const u4v*)place)[1];
+    const u32 before = *(key - 1), far = *(key - LEN - 1), k0 = own[0].x, k1 = own[LEN / 4 - 1].w;
+    if (k0 == none) return;
+    u32 same0 = 0, same1 = 0;
 #pragma unroll
-            for (u32 j = 0; j < LEN; ++j) to += p1 + j < n && keys[p1 + j] == k1;
-        }
-    }
+    for (int j = 0; j < LEN; ++j) { same0 += own[j / 4][j % 4] == k0; same1 += after[j / 4][j % 4] == k1; }
+    const bool came = before == k0, first_to_chain = came && (far == k0 || k1 == k0);
+    const u32 from = came && !first_to_chain ? same0 : 0;
+    const bool goes = k1 != none && same1 && !(first_to_chain && k1 == k0), last_to_chain = goes && same1 == LEN;
+    const u32 to = goes && !last_to_chain ? LEN + same1 : LEN;
     const u64 draw = DROP ? draw_of(m) : 0;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (u32 at = from; at < to; at += 4) {
-        u32 k[5], row[4];
-        float v[4][8];
+    at_k[0] = own[0];
+    at_k[1] = own[1];
+    for (u32 at = 0; at < to; at += 8) {
+        u32 k[9], p[8];
+        typename T::raw v[8];
+        F32::raw base[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            k[j] = at + j < to ? keys[at + j] : none;
-            row[j] = at + j < to ? places[at + j] : 0;
+        for (int j = 0; j < 8; ++j) {
+            const bool mine = at + j >= from && at + j < to;
+            k[j] = mine ? at_k[j / 4][j % 4] : none;
+            p[j] = at_p[j / 4][j % 4];
         }
-        k[4] = at + 4 < to ? keys[at + 4] : none;
+        // (past the last batch these are read too: the lists go on for KEY_PAD entries)
+        at_k[0] = *(const u4v*)(key + at + 8);
+        at_k[1] = *(const u4v*)(key + at + 12);
+        at_p[0] = *(const u4v*)(place + at + 8);
+        at_p[1] = *(const u4v*)(place + at + 12);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (k[j] != none) load_group<T>(dy + (u64)row[j] * dy_stride, c, s.cols, v[j]);
+        for (int j = 0; j < 8; ++j)
+            if (k[j] != none) {
+                v[j] = load_raw<T, WHOLE>(dy + (u64)p[j] * dy_stride, c, s.cols);
+                if (out.base) base[j] = load_raw<F32, WHOLE>(out.base + (u64)k[j] * out.base_stride, c, s.cols);
+            }
+        k[8] = at + 8 < to ? at_k[0].x : none;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 8; ++j) {
             if (k[j] == none) continue;
-            if (DROP) gate8(m, draw, (u64)row[j] * groups + g, v[j]);
-            for (int e = 0; e < 8; ++e) sum[e] += v[j][e];
+            float x[8];
+            T::open(v[j], x);
+            if (DROP) gate8(m, draw, (u64)p[j] * groups + g, x);
+            for (int e = 0; e < 8; ++e) sum[e] += x[e];
             if (k[j + 1] == k[j]) continue;
             if (first_to_chain && k[j] == k0) {
                 F32::put8(slot, sum);
@@ -468,7 +605,10 @@ __global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys,
                 F32::put8(slot + (u64)groups * 8, sum);
                 if (g == 0) chains[atomicAdd(n_chains, 1u)] = piece;           // in any order: the chains have nothing to do with each other
             } else {
-                put_row(out.base, out.base_stride, out.grad, out.grad_stride, k[j], c, s.cols, out.scale, sum);
+                float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (out.base) F32::open(base[j], y);
+                for (int e = 0; e < 8; ++e) y[e] += out.scale * sum[e];
+                store_group<F32>(out.grad + (u64)k[j] * out.grad_stride, c, s.cols, y);
             }
             for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
         }
@@ -485,10 +625,10 @@ __global__ __launch_bounds__(256) void grad_chains(const u32* __restrict__ keys,
         const u32 k = keys[(piece + 1) * len];             // the run covers the next piece
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (g < groups) {
-            if (strand == 0) F32::get8(chain + (((u64)piece * 2 + 1) * groups + g) * 8, sum);
-            for (u32 p = piece + 1 + strand; (u64)p * len < n && keys[p * len] == k; p += 16) {
+            if (strand == 0) F32::open(F32::load(chain + (((u64)piece * 2 + 1) * groups + g) * 8), sum);
+            for (u64 p = (u64)piece + 1 + strand; p * len < n && keys[p * len] == k; p += 16) {
                 float v[8];
-                F32::get8(chain + ((u64)p * 2 * groups + g) * 8, v);
+                F32::open(F32::load(chain + (p * 2 * groups + g) * 8), v);
                 for (int e = 0; e < 8; ++e) sum[e] += v[e];
             }
         }
@@ -547,7 +687,7 @@ __device__ __forceinline__ Soft soft_row(const typename T::elem* row, u32 n) {
     Soft a = {-INFINITY, 0.0f};
     for (u32 c = threadIdx.x * 8; c < n; c += NT * 8) {
         float v[8];
-        if (c + 8 <= n) T::get8(row + c, v);
+        if (c + 8 <= n) T::open(T::load(row + c), v);
         else for (u32 i = 0; i < 8; ++i) v[i] = c + i < n ? T::get(row + c + i) : -INFINITY;
         soft_add8(a, v);
     }
@@ -722,7 +862,9 @@ static void each_launch(u64 rows, u32 cols, F f) {
         f(Groups{row0, (u32)(n * per_row), cols, Divider::by(per_row)});
     }
 }
-static dim3 blocks_of(const Groups& s) { return dim3((s.n + 255) / 256); }
+static dim3 blocks_of(const Groups& s, u32 each = 1) { return dim3((s.n + 256 * each - 1) / (256 * each)); }
+
+template <int N> struct Int { static constexpr int value = N; };
 
 template <class F>
 static void by_type(int type, F f) {
@@ -753,8 +895,9 @@ extern "C" int dblp_embed(int device, void* stream, const int64_t* d_tokens, uin
             typedef decltype(st) S;
             typedef decltype(tt) T;
             each_launch(n_tokens, dim, [&](Groups s) {
-                const auto kernel = m.limit ? embed_groups<S, T, true> : embed_groups<S, T, false>;
-                hipLaunchKernelGGL(kernel, blocks_of(s), dim3(256), 0, (hipStream_t)stream, s, m, d_tokens, (const typename S::elem*)d_table, (u64)table_stride, (u64)vocab, scale,
+                const bool whole = dim % 8 == 0;
+                const auto kernel = m.limit ? (whole ? embed_groups<S, T, true, true> : embed_groups<S, T, true, false>) : (whole ? embed_groups<S, T, false, true> : embed_groups<S, T, false, false>);
+                hipLaunchKernelGGL(kernel, blocks_of(s, GROUPS_EACH), dim3(256), 0, (hipStream_t)stream, s, m, d_tokens, (const typename S::elem*)d_table, (u64)table_stride, (u64)vocab, scale,
                                    d_positions, (const typename S::elem*)d_pos_table, (u64)pos_stride, (u64)n_positions, (typename T::elem*)d_out, (u64)out_stride);
             });
         });
@@ -768,7 +911,6 @@ struct GradPlan {
     u32 len, pieces, passes, bits, tile, tiles;
     u64 keys[2], places[2], hist, present, chains, n_chains, chain, bytes;
 };
-#define GRAD_SHORT 512
 
 static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
     GradPlan p = {};
@@ -786,7 +928,7 @@ static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
     p.tiles = (u32)((n + p.tile - 1) / p.tile);
     u64 at = 0;
     const auto take = [&](u64 bytes) { const u64 here = at; at += round_up(bytes, 256); return here; };
-    for (int i = 0; i < 2; ++i) { p.keys[i] = take(4 * n); p.places[i] = take(4 * n); }
+    for (int i = 0; i < 2; ++i) { p.keys[i] = take(4 * (n + 2 * KEY_PAD)) + 4 * KEY_PAD; p.places[i] = take(4 * (n + KEY_PAD)); }
     p.hist = take(4ull * SORT_TILES * BINS);
     p.present = take(vocab);
     p.chains = take(4ull * p.pieces);
@@ -860,15 +1002,20 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
     const GradPlan p = grad_plan(n_tokens, vocab, dim);
     const u32 n = (u32)n_tokens, groups = (u32)((dim + 7ull) / 8);
     if (p.short_batch) {
-        if (d_base != d_grad)
-            each_launch(vocab, dim, [&](Groups s) { hipLaunchKernelGGL(fill_rows, blocks_of(s), dim3(256), 0, st, s, out, (const uint8_t*)nullptr); });
-        if (n)
-            by_type(dy_type, [&](auto tt) {
-                typedef decltype(tt) T;
-                const u32 nt = groups >= 256 ? 256 : (groups + 63) / 64 * 64;
-                const auto kernel = m.limit ? grad_by_first<T, true> : grad_by_first<T, false>;
-                hipLaunchKernelGGL(kernel, dim3(n, (groups + nt - 1) / nt), dim3(nt), 0, st, d_tokens, n, dim, groups, out, m, (const typename T::elem*)d_dy, (u64)dy_stride);
-            });
+        by_type(dy_type, [&](auto tt) {
+            typedef decltype(tt) T;
+            const bool whole = dim % 8 == 0;
+            const auto kernel = m.limit ? (whole ? grad_short<T, true, true> : grad_short<T, true, false>) : (whole ? grad_short<T, false, true> : grad_short<T, false, false>);
+            u32 lead = (u32)((n * ((groups + 63ull) / 64) + 3) / 4);
+            const auto go = [&](Groups s) {
+                const u32 fill = (u32)((s.n + 256ull * FILL_EACH - 1) / (256 * FILL_EACH));
+                if (lead + fill)
+                    hipLaunchKernelGGL(kernel, dim3(lead + fill), dim3(256), 0, st, d_tokens, n, dim, groups, lead, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride);
+                lead = 0;
+            };
+            if (d_base == d_grad) go(Groups{0, 0, dim, Divider::by(groups)});
+            else each_launch(vocab, dim, go);
+        });
         return launched(call);
     }
     uint8_t* const ws = (uint8_t*)d_workspace;
@@ -878,8 +1025,9 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
     by_type(dy_type, [&](auto tt) {
         typedef decltype(tt) T;
         each_launch(p.pieces, dim, [&](Groups s) {
-            const auto kernel = p.len == 8 ? (m.limit ? grad_pieces<T, true, 8> : grad_pieces<T, false, 8>) : (m.limit ? grad_pieces<T, true, 16> : grad_pieces<T, false, 16>);
-            hipLaunchKernelGGL(kernel, blocks_of(s), dim3(256), 0, st, (const u32*)keys, (const u32*)places, n, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride, chain, chains, n_chains);
+            const auto pick = [&](auto len, auto whole) { return m.limit ? grad_pieces<T, true, decltype(len)::value, decltype(whole)::value> : grad_pieces<T, false, decltype(len)::value, decltype(whole)::value>; };
+            const auto kernel = p.len == 8 ? (dim % 8 ? pick(Int<8>(), Int<0>()) : pick(Int<8>(), Int<1>())) : (dim % 8 ? pick(Int<16>(), Int<0>()) : pick(Int<16>(), Int<1>()));
+            hipLaunchKernelGGL(kernel, blocks_of(s), dim3(256), 0, st, (const u32*)keys, (const u32*)places, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride, chain, chains, n_chains);
         });
     });
     hipLaunchKernelGGL(grad_chains, dim3(p.pieces < 256 ? p.pieces : 256, (groups + 15) / 16), dim3(256), 0, st, (const u32*)keys, n, p.len, dim, groups, out, (const float*)chain, (const u32*)chains, (const u32*)n_chains);
@@ -905,8 +1053,9 @@ extern "C" int dblp_dropout(int device, void* stream, uint64_t rows, uint32_t co
         typedef decltype(tt) T;
         typedef const typename T::elem* in;
         each_launch(rows, cols, [&](Groups s) {
-            const auto kernel = d_residual ? dropout_groups<T, true> : dropout_groups<T, false>;
-            hipLaunchKernelGGL(kernel, blocks_of(s), dim3(256), 0, (hipStream_t)stream, s, m, (in)d_x, (u64)x_stride, (in)d_residual, (u64)residual_stride, (typename T::elem*)d_y, (u64)y_stride);
+            const bool whole = cols % 8 == 0;
+            const auto kernel = d_residual ? (whole ? dropout_groups<T, true, true> : dropout_groups<T, true, false>) : (whole ? dropout_groups<T, false, true> : dropout_groups<T, false, false>);
+            hipLaunchKernelGGL(kernel, blocks_of(s, GROUPS_EACH), dim3(256), 0, (hipStream_t)stream, s, m, (in)d_x, (u64)x_stride, (in)d_residual, (u64)residual_stride, (typename T::elem*)d_y, (u64)y_stride);
         });
     });
     return launched(call);
