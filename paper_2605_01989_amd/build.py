@@ -1,12 +1,12 @@
 """Builds libdblp_agg.so (HIP kernels + C-ABI) for gfx950, in-tree: the receiver (dblp_agg.hip) and the worker's
-operators (dblp_worker.hip)."""
+operators (worker_rows.hip, worker_logits.hip)."""
 from __future__ import annotations
 
 import os
 import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(_HERE, "csrc", f) for f in ("dblp_agg.hip", "dblp_worker.hip")]
+SRCS = [os.path.join(_HERE, "csrc", f) for f in ("dblp_agg.hip", "worker_rows.hip", "worker_logits.hip")]
 LIB = os.path.join(_HERE, "libdblp_agg.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

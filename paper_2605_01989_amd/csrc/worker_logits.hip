@@ -1,0 +1,420 @@
+// Logits of a worker's training step on gfx950 (MI355X): log probabilities of given tokens, and the clipped policy loss with its gradient.
+// Kernels and the C-ABI declared in include/dblp_worker.h.
+//
+// A row is read once: its largest value and the sum of its exponentials are found together, and where a gradient is wanted the row
+// stays in registers between the sum and the gradient (50257 16-bit values: 28 KB of a CU's 512 KB for each quarter of a block's threads).
+#include "worker_common.h"
+
+// ------------------------------------------------------------------------------------------
+// a row's largest value m and s = sum of exp(x - m).  Nothing met: (-inf, 0)
+// ------------------------------------------------------------------------------------------
+#define LOG2E 1.4426950408889634f
+
+struct Soft { float m, s; };
+__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.0f : m; }     // exp(-inf - -inf) would be NaN
+// x - shift is exact where it matters (x near the largest); the product with log2 e is off by |x - shift| 2^-24, the function by one step.
+__device__ __forceinline__ float exp_of(float x, float shift) { return __builtin_amdgcn_exp2f((x - shift) * LOG2E); }
+__device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
+    const float m = fmaxf(a.m, b.m), at = shift_of(m);
+    return {m, a.s * exp_of(a.m, at) + b.s * exp_of(b.m, at)};
+}
+__device__ __forceinline__ Soft soft_wave(Soft a) {
+    for (int d = 1; d < WAVE; d <<= 1) a = soft_join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d)});
+    return a;
+}
+// The whole block's, to all of its threads.  `part`: one entry for each wave.
+template <int NT>
+__device__ __forceinline__ Soft soft_block(Soft a, Soft* part) {
+    a = soft_wave(a);
+    if (NT == WAVE) return a;
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = part[0];
+#pragma unroll
+    for (int w = 1; w < NT / WAVE; ++w) a = soft_join(a, part[w]);
+    return a;
+}
+// N vectors of W values at once: one largest value, one change of scale.
+template <class V, int W, int N>
+__device__ __forceinline__ void soft_add(Soft& a, const typename V::raw (&r)[N]) {
+    float v[N][W], m = a.m;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        V::open(r[j], v[j]);
+#pragma unroll
+        for (int i = 0; i < W; i += 2) m = fmaxf(fmaxf(v[j][i], v[j][i + 1]), m);
+    }
+    const float at = shift_of(m);
+    float s = a.s * exp_of(a.m, at);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) t += exp_of(v[j][i], at);
+        s += t;
+    }
+    a = {m, s};
+}
+
+template <class T> struct Wide { static constexpr int W = sizeof(typename T::elem) == 4 ? 4 : 8; };      // 16 bytes
+
+// Columns [c, c + W) of a row, c < n; -inf past its end.
+template <class V, int W, bool FAR>
+__device__ __forceinline__ typename V::raw load_logits(const typename V::elem* row, u32 c, u32 n) {
+    if (c + W <= n) return FAR ? V::load_far(row + c) : V::load(row + c);
+    float v[W];
+    V::open(V::some(row + c, n - c), v);
+#pragma unroll
+    for (u32 i = 0; i < W; ++i) if (i >= n - c) v[i] = -INFINITY;
+    return V::pack(v);
+}
+template <class V, int W>
+__device__ __forceinline__ typename V::raw no_logits() {
+    float v[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = -INFINITY;
+    return V::pack(v);
+}
+
+// A thread's share of a row that is only read: STREAM vectors in flight.
+#define STREAM 4
+#define LOGPROB_NT 512
+template <class T, int NT, bool FAR>
+__device__ __forceinline__ Soft soft_row(const typename T::elem* row, u32 n) {
+    constexpr int W = Wide<T>::W;
+    typedef Vec<T, W> V;
+    Soft a = {-INFINITY, 0.0f};
+    const u32 whole = n / (NT * W * STREAM) * (NT * W * STREAM);
+    for (u32 c0 = 0; c0 < whole; c0 += NT * W * STREAM) {
+        typename V::raw r[STREAM];
+#pragma unroll
+        for (int j = 0; j < STREAM; ++j) r[j] = FAR ? V::load_far(row + c0 + (j * NT + threadIdx.x) * W) : V::load(row + c0 + (j * NT + threadIdx.x) * W);
+        soft_add<V, W, STREAM>(a, r);
+    }
+    if (whole < n) {
+        typename V::raw r[STREAM];
+#pragma unroll
+        for (int j = 0; j < STREAM; ++j) {
+            const u32 c = whole + (j * NT + threadIdx.x) * W;
+            r[j] = c < n ? load_logits<V, W, FAR>(row, c, n) : no_logits<V, W>();
+        }
+        soft_add<V, W, STREAM>(a, r);
+    }
+    return a;
+}
+
+// Log probability of a logit x.  A score is a difference of numbers of ten or twenty, and policies' ratios are differences of scores: the last sums are fp64, and
+// the logarithm is taken of a number in 1/2 .. 1, the exponent of s apart, so that it is off by 2^-24 and not by 2^-20.  The largest value and the logarithm are not added
+// up first: in a row of the type's lowest value the logarithm would be lost.
+__device__ __forceinline__ double log_of(float s) {
+    return ((double)__builtin_amdgcn_frexp_expf(s) + (double)__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(s))) * 0.6931471805599453;
+}
+__device__ __forceinline__ double logp_of(float x, Soft a) { return ((double)x - (double)a.m) - log_of(a.s); }
+
+template <class T, int NT, bool FAR>
+__global__ __launch_bounds__(NT) void logprob_rows(const typename T::elem* __restrict__ logits, u64 stride, u32 vocab, const int64_t* __restrict__ targets,
+                                                   float* __restrict__ logp, float* __restrict__ lse) {
+    __shared__ Soft part[NT / WAVE];
+    const u32 t = blockIdx.x;
+    const u64 at = (u64)targets[t];
+    if (at >= vocab) {
+        if (threadIdx.x == 0) { logp[t] = 0.0f; if (lse) lse[t] = 0.0f; }
+        return;
+    }
+    const typename T::elem* row = logits + (u64)t * stride;
+    const float x = threadIdx.x == 0 ? (float)row[at] : 0.0f;
+    const Soft a = soft_block<NT>(soft_row<T, NT, FAR>(row, vocab), part);
+    if (threadIdx.x == 0) {
+        if (lse) lse[t] = (float)((double)a.m + log_of(a.s));
+        logp[t] = a.m == -INFINITY ? -INFINITY : (float)logp_of(x, a);
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// policy loss
+// ------------------------------------------------------------------------------------------
+struct Policy { const int64_t* targets; const float *advantages, *weights, *old_logp, *ref_logp; float low, high, kl, grad_scale; };
+struct __align__(16) TokenPart { float policy, kl; u32 counted, clipped; };          // a token's part of the five sums, weighted
+
+// exp(d) - 1 - d, by its series where the difference would cancel (next term below 2^-30 of the sum).
+__device__ __forceinline__ float exp_past(float d) {
+    if (fabsf(d) < 0.5f) {
+        float t = 1.0f;
+#pragma unroll
+        for (int i = 10; i > 2; --i) t = 1.0f + d * (1.0f / i) * t;
+        return 0.5f * d * d * t;
+    }
+    return exp_of(d, 0.0f) - 1.0f - d;
+}
+// Of a counted token with log probability lp: what it adds to the sums, and d loss / d lp.  (In fp32, from differences taken in fp64; more would cost the registers that
+// hold the row.)
+__device__ __forceinline__ TokenPart token_part(const Policy& p, u32 t, double lp, float* slope) {
+    const float w = p.weights[t], a = p.advantages[t];
+    const float r = p.old_logp ? exp_of((float)(lp - (double)p.old_logp[t]), 0.0f) : 1.0f;
+    const float lo = 1.0f - p.low, hi = 1.0f + p.high;
+    const float free_term = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
+    const bool clipped = held < free_term;
+    float g = clipped ? 0.0f : -free_term, kl = 0.0f;
+    if (p.ref_logp) {
+        const float d = (float)((double)p.ref_logp[t] - lp);
+        kl = exp_past(d);
+        g -= p.kl * (kl + d);
+    }
+    *slope = w * g;
+    return {w * -(clipped ? held : free_term), w * kl, 1u, clipped ? 1u : 0u};
+}
+
+__device__ __forceinline__ void put_stats(float* stats, const double (&s)[4], float kl_coef) {
+    stats[0] = (float)(s[0] + (double)kl_coef * s[1]);
+    stats[1] = (float)s[0]; stats[2] = (float)s[1]; stats[3] = (float)s[2]; stats[4] = (float)s[3];
+}
+
+// What one thread finds out about a row: its token's part of the sums, and the slope for the row's gradient.  `stats`: of a batch of one token.
+__device__ __forceinline__ float close_row(const Policy& p, u32 t, float x, Soft a, float* logp, TokenPart* parts, float* stats) {
+    const double lp = logp_of(x, a);
+    float slope;
+    const TokenPart part = token_part(p, t, lp, &slope);
+    parts[t] = part;
+    if (logp) logp[t] = (float)lp;
+    if (stats) { const double s[4] = {part.policy, part.kl, (double)part.clipped, (double)part.counted}; put_stats(stats, s, p.kl); }
+    return slope * p.grad_scale;
+}
+// A row that is not counted: `empty`, all its logits are -inf.
+template <class T, int NT>
+__device__ __forceinline__ void skip_row(typename T::elem* drow, u32 vocab, u32 t, bool empty, float* logp, TokenPart* parts, float* stats) {
+    constexpr int W = Wide<T>::W;
+    if (threadIdx.x == 0) {
+        parts[t] = {0.0f, 0.0f, 0u, 0u};
+        if (logp) logp[t] = empty ? -INFINITY : 0.0f;
+        if (stats) for (int i = 0; i < 5; ++i) stats[i] = 0.0f;
+    }
+    const float z[W] = {};
+    if (drow) for (u32 c = threadIdx.x * W; c < vocab; c += NT * W) store_cols<Vec<T, W>, W>(drow, c, vocab, z);
+}
+
+#define HELD_WAVES __attribute__((amdgpu_waves_per_eu(4)))        // registers for two rows of 512 threads a CU
+// A block takes a row and holds it: NV vectors a thread, all on their way at once.  The gradient of the target is written over by the thread that wrote its vector.
+template <class T, int NT, int NV, bool FAR>
+__global__ __launch_bounds__(NT) HELD_WAVES void policy_held(Policy p, const typename T::elem* logits, u64 stride, u32 vocab, typename T::elem* dlogits, u64 dstride,
+                                                  float* __restrict__ logp, TokenPart* __restrict__ parts, float* stats) {
+    constexpr int W = Wide<T>::W, STEP = NV % 4 == 0 ? 4 : 2;
+    typedef Vec<T, W> V;
+    __shared__ Soft part[NT / WAVE];
+    __shared__ float slope_sh;
+    const u32 t = blockIdx.x, tid = threadIdx.x;
+    const u64 at = (u64)p.targets[t];
+    const typename T::elem* row = logits + (u64)t * stride;
+    typename T::elem* drow = dlogits + (u64)t * dstride;
+    if (at >= vocab || p.weights[t] == 0.0f) { skip_row<T, NT>(drow, vocab, t, false, logp, parts, stats); return; }
+    // The row's last vector, where it is not whole, is read from the row's last W values; those that the vector before it has are taken out.
+    typename V::raw v[NV / STEP][STEP];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const u32 c = (j * NT + tid) * W;
+        v[j / STEP][j % STEP] = no_logits<V, W>();
+        if (c < vocab) v[j / STEP][j % STEP] = FAR ? V::load_far(row + (c + W <= vocab ? c : vocab - W)) : V::load(row + (c + W <= vocab ? c : vocab - W));
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const u32 c = (j * NT + tid) * W;
+        if (c >= vocab || c + W <= vocab) continue;
+        float y[W];
+        V::open(v[j / STEP][j % STEP], y);
+#pragma unroll
+        for (u32 i = 0; i < W; ++i) if (i < c + W - vocab) y[i] = -INFINITY;
+        v[j / STEP][j % STEP] = V::pack(y);
+    }
+    const float x = (float)row[at];
+    Soft a = {-INFINITY, 0.0f};
+#pragma unroll
+    for (int j = 0; j < NV / STEP; ++j) soft_add<V, W, STEP>(a, v[j]);
+    a = soft_block<NT>(a, part);
+    if (a.m == -INFINITY) { skip_row<T, NT>(drow, vocab, t, true, logp, parts, stats); return; }
+    if (tid == 0) slope_sh = close_row(p, t, x, a, logp, parts, stats);
+    __syncthreads();
+    const float g = slope_sh, k = -g / a.s;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const u32 c = (j * NT + tid) * W;
+        if (c >= vocab) continue;
+        float y[W];
+        V::open(v[j / STEP][j % STEP], y);
+#pragma unroll
+        for (int i = 0; i < W; ++i) y[i] = k * exp_of(y[i], a.m);
+        if (c + W <= vocab) {
+            store_cols<V, W, FAR>(drow, c, vocab, y);
+        } else {
+#pragma unroll
+            for (u32 i = 0; i < W; ++i) if (i >= c + W - vocab) drow[vocab - W + i] = (typename T::elem)y[i];
+        }
+        if (at - c < W) {                                  // the target's again, by the thread that wrote it
+            const float e = exp_of(x, a.m);
+            drow[at] = (typename T::elem)(g + k * e);
+        }
+    }
+}
+
+// Rows that registers do not hold, and calls without a gradient: one pass for the sum, a second one for the gradient, which finds most of the row in the caches.
+template <class T, int NT>
+__global__ __launch_bounds__(NT) void policy_twice(Policy p, const typename T::elem* logits, u64 stride, u32 vocab, typename T::elem* dlogits, u64 dstride,
+                                                   float* __restrict__ logp, TokenPart* __restrict__ parts, float* stats) {
+    constexpr int W = Wide<T>::W;
+    typedef Vec<T, W> V;
+    __shared__ Soft part[NT / WAVE];
+    __shared__ float slope_sh;
+    const u32 t = blockIdx.x, tid = threadIdx.x;
+    const u64 at = (u64)p.targets[t];
+    const typename T::elem* row = logits + (u64)t * stride;
+    typename T::elem* drow = dlogits ? dlogits + (u64)t * dstride : nullptr;
+    if (at >= vocab || p.weights[t] == 0.0f) { skip_row<T, NT>(drow, vocab, t, false, logp, parts, stats); return; }
+    const float x = tid == 0 ? (float)row[at] : 0.0f;
+    const Soft a = soft_block<NT>(soft_row<T, NT, false>(row, vocab), part);
+    if (a.m == -INFINITY) { skip_row<T, NT>(drow, vocab, t, true, logp, parts, stats); return; }
+    if (tid == 0) slope_sh = close_row(p, t, x, a, logp, parts, stats);
+    __syncthreads();
+    if (!drow) return;
+    const float g = slope_sh, k = -g / a.s;
+    for (u32 c = tid * W; c < vocab; c += NT * W) {
+        float y[W];
+        V::open(load_logits<V, W, false>(row, c, vocab), y);
+#pragma unroll
+        for (int i = 0; i < W; ++i) y[i] = k * exp_of(y[i], a.m) + (c + i == at ? g : 0.0f);
+        store_cols<V, W>(drow, c, vocab, y);
+    }
+}
+
+// The sums over all tokens in fp64 and a fixed order: each block those of its share, one block the blocks'.
+#define SUM_SHARE 16384
+template <int NT>
+__device__ __forceinline__ bool sum_block(double (&s)[4], double (&sh)[4][NT / WAVE]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        for (int d = 1; d < WAVE; d <<= 1) s[i] += __shfl_xor(s[i], d);
+        if ((threadIdx.x & 63) == 0) sh[i][threadIdx.x >> 6] = s[i];
+    }
+    __syncthreads();
+    if (threadIdx.x) return false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { s[i] = 0; for (int w = 0; w < NT / WAVE; ++w) s[i] += sh[i][w]; }
+    return true;
+}
+__global__ __launch_bounds__(1024) void policy_sums(const TokenPart* __restrict__ parts, u32 n, float kl_coef, double* __restrict__ shares, float* __restrict__ stats) {
+    __shared__ double sh[4][16];
+    double s[4] = {0, 0, 0, 0};
+    const u32 lo = blockIdx.x * SUM_SHARE, hi = n - lo < SUM_SHARE ? n : lo + SUM_SHARE;
+#pragma unroll 8
+    for (u32 t = lo + threadIdx.x; t < hi; t += 1024) {
+        const TokenPart p = parts[t];
+        s[0] += (double)p.policy; s[1] += (double)p.kl; s[2] += (double)p.clipped; s[3] += (double)p.counted;
+    }
+    if (!sum_block<1024>(s, sh)) return;
+    if (gridDim.x == 1) put_stats(stats, s, kl_coef);
+    else for (int i = 0; i < 4; ++i) shares[4 * blockIdx.x + i] = s[i];
+}
+__global__ __launch_bounds__(256) void policy_join(const double* __restrict__ shares, u32 n, float kl_coef, float* __restrict__ stats) {
+    __shared__ double sh[4][4];
+    double s[4] = {0, 0, 0, 0};
+    for (u32 b = threadIdx.x; b < n; b += 256)
+        for (int i = 0; i < 4; ++i) s[i] += shares[4 * (u64)b + i];
+    if (sum_block<256>(s, sh)) put_stats(stats, s, kl_coef);
+}
+
+// ------------------------------------------------------------------------------------------
+// C-ABI
+// ------------------------------------------------------------------------------------------
+#define FAR_BYTES (256ull << 20)                 // logits that the memory-side cache does not hold are read and written past it
+
+struct LogitsPlan { u64 shares, bytes; };        // the tokens' parts come first
+static LogitsPlan logits_plan(u64 n) {
+    const u64 parts = round_up(n * sizeof(TokenPart), 256);
+    return {parts, parts + round_up((n + SUM_SHARE - 1) / SUM_SHARE * 32, 256) + 256};
+}
+
+extern "C" uint64_t dblp_logits_workspace(uint64_t n_tokens, uint32_t vocab) {
+    if (n_tokens >= COUNT_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT) return 0;
+    return logits_plan(n_tokens).bytes;
+}
+
+extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, uint32_t vocab, const void* d_logits,
+                                   uint64_t logits_stride, int type, const int64_t* d_targets, float* d_logp, float* d_lse,
+                                   void* d_workspace, uint64_t workspace_bytes) {
+    const char* call = "token_logprobs";
+    REFUSE_IF(bad_type(type), "unknown type");
+    REFUSE_IF(vocab == 0 || vocab >= COUNT_LIMIT || n_tokens >= COUNT_LIMIT, "size out of range");
+    REFUSE_IF(n_tokens && (!d_logits || !d_targets || !d_logp), "null pointer");
+    REFUSE_IF(off(d_logits, type_bytes(type)) || off(d_targets, 8) || off(d_logp, 4) || off(d_lse, 4), "misaligned pointer");
+    REFUSE_IF(!d_workspace || off(d_workspace, 256) || workspace_bytes < dblp_logits_workspace(n_tokens, vocab), "workspace missing, misaligned or too small");
+    if (n_tokens == 0) return DBLP_OK;
+    OnDevice on(device);
+    if (on.err != hipSuccess) return no_device(call, on.err);
+    const bool far = n_tokens * vocab * type_bytes(type) > FAR_BYTES;
+    by_type(type, [&](auto tt) {
+        typedef decltype(tt) T;
+        const auto go = [&](auto nt) {
+            constexpr int NT = decltype(nt)::value;
+            hipLaunchKernelGGL(far ? (logprob_rows<T, NT, true>) : (logprob_rows<T, NT, false>), dim3((u32)n_tokens), dim3(NT), 0, (hipStream_t)stream, (const typename T::elem*)d_logits, (u64)logits_stride, vocab, d_targets, d_logp, d_lse);
+        };
+        // a wave for a row that it reads in one step; many threads where there are few rows
+        if (vocab <= 64 * Wide<T>::W * STREAM) go(Int<64>());
+        else if (n_tokens <= 512 && vocab > 512 * Wide<T>::W * STREAM) go(Int<1024>());
+        else go(Int<LOGPROB_NT>());
+    });
+    return launched(call);
+}
+
+extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uint32_t vocab, const void* d_logits,
+                                uint64_t logits_stride, int type, const int64_t* d_targets, const float* d_advantages,
+                                const float* d_weights, const float* d_old_logp, const float* d_ref_logp, float clip_low,
+                                float clip_high, float kl_coef, float grad_scale, void* d_dlogits, uint64_t dlogits_stride,
+                                float* d_logp, float* d_stats, void* d_workspace, uint64_t workspace_bytes) {
+    const char* call = "policy_loss";
+    REFUSE_IF(bad_type(type), "unknown type");
+    REFUSE_IF(vocab == 0 || vocab >= COUNT_LIMIT || n_tokens >= COUNT_LIMIT, "size out of range");
+    REFUSE_IF(!d_stats || (n_tokens && (!d_logits || !d_targets || !d_advantages || !d_weights)), "null pointer");
+    REFUSE_IF(off(d_logits, type_bytes(type)) || off(d_dlogits, type_bytes(type)) || off(d_targets, 8) || off(d_advantages, 4) || off(d_weights, 4) || off(d_old_logp, 4) ||
+              off(d_ref_logp, 4) || off(d_logp, 4) || off(d_stats, 4), "misaligned pointer");
+    REFUSE_IF(!(clip_low >= 0.0f && clip_low <= 1.0f && clip_high >= 0.0f && isfinite(clip_high)), "clip_low must be in 0..1 and clip_high at least 0");
+    REFUSE_IF(!isfinite(kl_coef) || !isfinite(grad_scale), "kl_coef and grad_scale must be finite");
+    REFUSE_IF(d_dlogits && n_tokens > 1 && dlogits_stride < vocab, "the gradient's rows overlap");
+    REFUSE_IF(d_dlogits == d_logits && n_tokens > 1 && dlogits_stride != logits_stride, "in place, the strides must be equal");
+    REFUSE_IF(!d_workspace || off(d_workspace, 256) || workspace_bytes < dblp_logits_workspace(n_tokens, vocab), "workspace missing, misaligned or too small");
+    OnDevice on(device);
+    if (on.err != hipSuccess) return no_device(call, on.err);
+    const Policy p = {d_targets, d_advantages, d_weights, d_old_logp, d_ref_logp, clip_low, clip_high, kl_coef, grad_scale};
+    TokenPart* const parts = (TokenPart*)d_workspace;
+    double* const shares = (double*)((uint8_t*)d_workspace + logits_plan(n_tokens).shares);
+    const hipStream_t st = (hipStream_t)stream;
+    const u32 n = (u32)n_tokens;
+    float* const own_stats = n == 1 ? d_stats : nullptr;         // one token's sums are its own
+    const bool far = n_tokens * vocab * type_bytes(type) > FAR_BYTES / 2;
+    if (n)
+        by_type(type, [&](auto tt) {
+            typedef decltype(tt) T;
+            typedef typename T::elem E;
+            constexpr u32 W = Wide<T>::W;
+            const auto twice = [&](auto nt) {
+                constexpr int NT = decltype(nt)::value;
+                hipLaunchKernelGGL((policy_twice<T, NT>), dim3(n), dim3(NT), 0, st, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, d_logp, parts, own_stats);
+            };
+            const auto held = [&](auto nt, auto nv) {
+                constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+                hipLaunchKernelGGL(far ? (policy_held<T, NT, NV, true>) : (policy_held<T, NT, NV, false>), dim3(n), dim3(NT), 0, st, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, d_logp, parts, own_stats);
+            };
+            if (!d_dlogits || vocab < W) vocab <= 64 * W * STREAM ? twice(Int<64>()) : twice(Int<512>());
+            else if (vocab <= 64 * 2 * W) held(Int<64>(), Int<2>());
+            else if (vocab <= 64 * 8 * W) held(Int<64>(), Int<8>());
+            else if (vocab <= 256 * 4 * W) held(Int<256>(), Int<4>());
+            else if (vocab <= 256 * 8 * W) held(Int<256>(), Int<8>());
+            else if (vocab <= 512 * 8 * W) held(Int<512>(), Int<8>());
+            else if (vocab <= 512 * 14 * W) held(Int<512>(), Int<14>());
+            else if (vocab <= 1024 * 14 * W) held(Int<1024>(), Int<14>());
+            else if (vocab <= 1024 * 20 * W) held(Int<1024>(), Int<20>());
+            else twice(Int<1024>());
+        });
+    if (n != 1) {
+        const u32 blocks = n ? (n + SUM_SHARE - 1) / SUM_SHARE : 1;
+        hipLaunchKernelGGL(policy_sums, dim3(blocks), dim3(1024), 0, st, (const TokenPart*)parts, n, kl_coef, shares, d_stats);
+        if (blocks > 1) hipLaunchKernelGGL(policy_join, dim3(1), dim3(256), 0, st, (const double*)shares, blocks, kl_coef, d_stats);
+    }
+    return launched(call);
+}
