@@ -58,16 +58,18 @@ __device__ __forceinline__ void soft_add(Soft& a, const typename V::raw (&r)[N])
 
 template <class T> struct Wide { static constexpr int W = sizeof(typename T::elem) == 4 ? 4 : 8; };      // 16 bytes
 
-// Columns [c, c + W) of a row, c < n; -inf past its end.
-template <class V, int W, bool FAR>
-__device__ __forceinline__ typename V::raw load_logits(const typename V::elem* row, u32 c, u32 n) {
-    if (c + W <= n) return FAR ? V::load_far(row + c) : V::load(row + c);
-    float v[W];
-    V::open(V::some(row + c, n - c), v);
-#pragma unroll
-    for (u32 i = 0; i < W; ++i) if (i >= n - c) v[i] = -INFINITY;
-    return V::pack(v);
+// A row as vectors of W values from the first place whose address is a multiple of four (16-byte accesses at odd multiples of two run at two thirds of the rate: 8192
+// rows of 50257 16-bit values take 163 us to read, of 50258 127), and single values: a head of at most one, a tail of fewer than W.
+struct Cut { u32 head, vecs, singles; };
+template <class T>
+__device__ __forceinline__ Cut cut_row(const typename T::elem* row, u32 n) {
+    constexpr u32 W = Wide<T>::W;
+    const u32 head = ((uintptr_t)row & 2) ? 1 : 0, vecs = (n - head) / W;
+    return {head, vecs, n - vecs * W};
 }
+template <int W>
+__device__ __forceinline__ u32 place_of_single(const Cut& c, u32 i) { return i < c.head ? i : i + c.vecs * W; }
+
 template <class V, int W>
 __device__ __forceinline__ typename V::raw no_logits() {
     float v[W];
@@ -75,31 +77,39 @@ __device__ __forceinline__ typename V::raw no_logits() {
     for (int i = 0; i < W; ++i) v[i] = -INFINITY;
     return V::pack(v);
 }
+__device__ __forceinline__ void soft_add_one(Soft& a, float x) { a = soft_join(a, {x, x == -INFINITY ? 0.0f : 1.0f}); }
 
-// A thread's share of a row that is only read: STREAM vectors in flight.
+// A thread's share of vectors [lo, hi) of a row that is only read: STREAM vectors in flight.
 #define STREAM 4
-#define LOGPROB_NT 512
 template <class T, int NT, bool FAR>
-__device__ __forceinline__ Soft soft_row(const typename T::elem* row, u32 n) {
+__device__ __forceinline__ void soft_vecs(Soft& a, const typename T::elem* body, u32 lo, u32 hi) {
     constexpr int W = Wide<T>::W;
     typedef Vec<T, W> V;
-    Soft a = {-INFINITY, 0.0f};
-    const u32 whole = n / (NT * W * STREAM) * (NT * W * STREAM);
-    for (u32 c0 = 0; c0 < whole; c0 += NT * W * STREAM) {
-        typename V::raw r[STREAM];
+    const u32 whole = lo + (hi - lo) / (NT * STREAM) * (NT * STREAM);
+    typename V::raw r[STREAM];
+    for (u32 i = lo; i < whole; i += NT * STREAM) {
 #pragma unroll
-        for (int j = 0; j < STREAM; ++j) r[j] = FAR ? V::load_far(row + c0 + (j * NT + threadIdx.x) * W) : V::load(row + c0 + (j * NT + threadIdx.x) * W);
+        for (int j = 0; j < STREAM; ++j) r[j] = FAR ? V::load_far(body + (u64)(i + j * NT + threadIdx.x) * W) : V::load(body + (u64)(i + j * NT + threadIdx.x) * W);
         soft_add<V, W, STREAM>(a, r);
     }
-    if (whole < n) {
-        typename V::raw r[STREAM];
+    if (whole < hi) {
 #pragma unroll
         for (int j = 0; j < STREAM; ++j) {
-            const u32 c = whole + (j * NT + threadIdx.x) * W;
-            r[j] = c < n ? load_logits<V, W, FAR>(row, c, n) : no_logits<V, W>();
+            const u32 i = whole + j * NT + threadIdx.x;
+            r[j] = no_logits<V, W>();
+            if (i < hi) r[j] = FAR ? V::load_far(body + (u64)i * W) : V::load(body + (u64)i * W);
         }
         soft_add<V, W, STREAM>(a, r);
     }
+}
+template <class T, int NT, bool FAR>
+__device__ __forceinline__ Soft soft_row(const typename T::elem* row, u32 n) {
+    constexpr int W = Wide<T>::W;
+    const Cut c = cut_row<T>(row, n);
+    Soft a = {-INFINITY, 0.0f};
+    const float single = threadIdx.x < c.singles ? (float)row[place_of_single<W>(c, threadIdx.x)] : -INFINITY;
+    soft_vecs<T, NT, FAR>(a, row + c.head, 0, c.vecs);
+    soft_add_one(a, single);
     return a;
 }
 
@@ -188,70 +198,102 @@ __device__ __forceinline__ void skip_row(typename T::elem* drow, u32 vocab, u32 
         if (logp) logp[t] = empty ? -INFINITY : 0.0f;
         if (stats) for (int i = 0; i < 5; ++i) stats[i] = 0.0f;
     }
-    const float z[W] = {};
-    if (drow) for (u32 c = threadIdx.x * W; c < vocab; c += NT * W) store_cols<Vec<T, W>, W>(drow, c, vocab, z);
+    if (!drow) return;
+    // whole lines: from the first place that is a multiple of 16 bytes
+    const u32 ahead = (u32)(-(uintptr_t)drow & 15) / sizeof(typename T::elem), head = ahead < vocab ? ahead : vocab, vecs = (vocab - head) / W, singles = vocab - vecs * W;
+    for (u32 i = threadIdx.x; i < vecs; i += NT) *(u4v*)(drow + head + (u64)i * W) = u4v{0, 0, 0, 0};
+    if (threadIdx.x < singles) drow[threadIdx.x < head ? threadIdx.x : threadIdx.x + vecs * W] = (typename T::elem)0.0f;
 }
 
 #define HELD_WAVES __attribute__((amdgpu_waves_per_eu(4)))        // registers for two rows of 512 threads a CU
-// A block takes a row and holds it: NV vectors a thread, all on their way at once.  The gradient of the target is written over by the thread that wrote its vector.
+// A block takes a row and holds it: NV vectors a thread, all on their way at once.  A wave's vectors follow each other.  Where the gradient's row begins at another
+// multiple of two than the logits', a vector is stored one place on, with the first value of the next one (of the next lane, or of the wave's next vector's first lane); the
+// first value of a wave and the last vector of a wave or of the row are stored value by value.
 template <class T, int NT, int NV, bool FAR>
 __global__ __launch_bounds__(NT) HELD_WAVES void policy_held(Policy p, const typename T::elem* logits, u64 stride, u32 vocab, typename T::elem* dlogits, u64 dstride,
                                                   float* __restrict__ logp, TokenPart* __restrict__ parts, float* stats) {
     constexpr int W = Wide<T>::W, STEP = NV % 4 == 0 ? 4 : 2;
     typedef Vec<T, W> V;
+    typedef typename T::elem E;
     __shared__ Soft part[NT / WAVE];
     __shared__ float slope_sh;
     const u32 t = blockIdx.x, tid = threadIdx.x;
     const u64 at = (u64)p.targets[t];
-    const typename T::elem* row = logits + (u64)t * stride;
-    typename T::elem* drow = dlogits + (u64)t * dstride;
+    const E* row = logits + (u64)t * stride;
+    E* drow = dlogits + (u64)t * dstride;
     if (at >= vocab || p.weights[t] == 0.0f) { skip_row<T, NT>(drow, vocab, t, false, logp, parts, stats); return; }
-    // The row's last vector, where it is not whole, is read from the row's last W values; those that the vector before it has are taken out.
+    const Cut cut = cut_row<T>(row, vocab);
+    const u32 first = (tid >> 6) * (NV * WAVE), lane = tid & 63;            // of the wave's vectors
+    const E* body = row + cut.head + (u64)first * W;
     typename V::raw v[NV / STEP][STEP];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const u32 c = (j * NT + tid) * W;
         v[j / STEP][j % STEP] = no_logits<V, W>();
-        if (c < vocab) v[j / STEP][j % STEP] = FAR ? V::load_far(row + (c + W <= vocab ? c : vocab - W)) : V::load(row + (c + W <= vocab ? c : vocab - W));
+        if (first + j * WAVE + lane < cut.vecs) v[j / STEP][j % STEP] = FAR ? V::load_far(body + (j * WAVE + lane) * W) : V::load(body + (j * WAVE + lane) * W);
     }
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const u32 c = (j * NT + tid) * W;
-        if (c >= vocab || c + W <= vocab) continue;
-        float y[W];
-        V::open(v[j / STEP][j % STEP], y);
-#pragma unroll
-        for (u32 i = 0; i < W; ++i) if (i < c + W - vocab) y[i] = -INFINITY;
-        v[j / STEP][j % STEP] = V::pack(y);
-    }
-    const float x = (float)row[at];
+    const float single = tid < cut.singles ? (float)row[place_of_single<W>(cut, tid)] : -INFINITY, x = (float)row[at];
     Soft a = {-INFINITY, 0.0f};
 #pragma unroll
-    for (int j = 0; j < NV / STEP; ++j) soft_add<V, W, STEP>(a, v[j]);
+    for (int j = 0; j < NV / STEP; ++j) {
+        soft_add<V, W, STEP>(a, v[j]);
+        __builtin_amdgcn_sched_barrier(0);                 // a step's converted values are not kept beside the next one's
+    }
+    soft_add_one(a, single);
     a = soft_block<NT>(a, part);
     if (a.m == -INFINITY) { skip_row<T, NT>(drow, vocab, t, true, logp, parts, stats); return; }
     if (tid == 0) slope_sh = close_row(p, t, x, a, logp, parts, stats);
     __syncthreads();
     const float g = slope_sh, k = -g / a.s;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const u32 c = (j * NT + tid) * W;
-        if (c >= vocab) continue;
+    for (int j = 0; j < NV; ++j) asm("" : "+v"(v[j / STEP][j % STEP]));     // the row as it lies in memory, not its values converted before the sum
+    const auto gradient = [&](int j) {
         float y[W];
         V::open(v[j / STEP][j % STEP], y);
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] = k * exp_of(y[i], a.m);
-        if (c + W <= vocab) {
-            store_cols<V, W, FAR>(drow, c, vocab, y);
-        } else {
+        return V::pack(y);
+    };
+    E* dbody = drow + cut.head + (u64)first * W;
+    bool shifted = false;
+    if constexpr (W == 8) shifted = (((uintptr_t)row ^ (uintptr_t)drow) & 2) != 0;
+    if (!shifted) {
 #pragma unroll
-            for (u32 i = 0; i < W; ++i) if (i >= c + W - vocab) drow[vocab - W + i] = (typename T::elem)y[i];
-        }
-        if (at - c < W) {                                  // the target's again, by the thread that wrote it
-            const float e = exp_of(x, a.m);
-            drow[at] = (typename T::elem)(g + k * e);
+        for (int j = 0; j < NV; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (first + j * WAVE + lane >= cut.vecs) continue;
+            const typename V::raw y = gradient(j);
+            if (FAR) V::store_far(dbody + (j * WAVE + lane) * W, y);
+            else V::store(dbody + (j * WAVE + lane) * W, y);
         }
     }
+    if constexpr (W == 8) {
+        if (shifted) {
+            typename V::raw now = gradient(0), next = now;
+            if (lane == 0 && first < cut.vecs) *(u16*)dbody = (u16)now.x;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (j + 1 < NV) next = gradient(j + 1);
+                const u32 follow = (u32)__shfl_down((int)now.x, 1), wrap = (u32)__builtin_amdgcn_readfirstlane((int)next.x);
+                const u32 i = first + j * WAVE + lane, behind = lane == 63 ? wrap : follow;
+                E* to = dbody + (j * WAVE + lane) * W + 1;
+                if (i + 1 < cut.vecs && !(j + 1 == NV && lane == 63)) {
+                    V::store(to, (typename V::raw){now.x >> 16 | now.y << 16, now.y >> 16 | now.z << 16, now.z >> 16 | now.w << 16, now.w >> 16 | behind << 16});
+                } else if (i < cut.vecs) {
+                    u16* one = (u16*)to;
+                    one[0] = (u16)(now.x >> 16);
+                    one[1] = (u16)now.y; one[2] = (u16)(now.y >> 16);
+                    one[3] = (u16)now.z; one[4] = (u16)(now.z >> 16);
+                    one[5] = (u16)now.w; one[6] = (u16)(now.w >> 16);
+                }
+                now = next;
+            }
+        }
+    }
+    if (tid < cut.singles) drow[place_of_single<W>(cut, tid)] = (E)(k * exp_of(single, a.m));
+    // the target's once more, when its first value is written: whichever thread that was, the barrier is behind it
+    __syncthreads();
+    if (tid == 0) drow[at] = (E)(g + k * exp_of(x, a.m));
 }
 
 // Rows that registers do not hold, and calls without a gradient: one pass for the sum, a second one for the gradient, which finds most of the row in the caches.
@@ -274,12 +316,18 @@ __global__ __launch_bounds__(NT) void policy_twice(Policy p, const typename T::e
     __syncthreads();
     if (!drow) return;
     const float g = slope_sh, k = -g / a.s;
-    for (u32 c = tid * W; c < vocab; c += NT * W) {
+    const Cut cut = cut_row<T>(row, vocab);
+    for (u32 i = tid; i < cut.vecs; i += NT) {
+        const u64 c = cut.head + (u64)i * W;
         float y[W];
-        V::open(load_logits<V, W, false>(row, c, vocab), y);
+        V::open(V::load(row + c), y);
 #pragma unroll
-        for (int i = 0; i < W; ++i) y[i] = k * exp_of(y[i], a.m) + (c + i == at ? g : 0.0f);
-        store_cols<V, W>(drow, c, vocab, y);
+        for (int e = 0; e < W; ++e) y[e] = k * exp_of(y[e], a.m) + (c + e == at ? g : 0.0f);
+        V::store(drow + c, V::pack(y));
+    }
+    if (tid < cut.singles) {
+        const u32 c = place_of_single<W>(cut, tid);
+        drow[c] = (typename T::elem)(k * exp_of((float)row[c], a.m) + (c == at ? g : 0.0f));
     }
 }
 
@@ -357,7 +405,7 @@ extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, 
         // a wave for a row that it reads in one step; many threads where there are few rows
         if (vocab <= 64 * Wide<T>::W * STREAM) go(Int<64>());
         else if (n_tokens <= 512 && vocab > 512 * Wide<T>::W * STREAM) go(Int<1024>());
-        else go(Int<LOGPROB_NT>());
+        else go(Int<512>());
     });
     return launched(call);
 }
@@ -386,7 +434,8 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
     const hipStream_t st = (hipStream_t)stream;
     const u32 n = (u32)n_tokens;
     float* const own_stats = n == 1 ? d_stats : nullptr;         // one token's sums are its own
-    const bool far = n_tokens * vocab * type_bytes(type) > FAR_BYTES / 2;
+    // (past the cache only where every row begins at a multiple of 16 bytes: other stores with the hint cost parts of lines)
+    const bool far = n_tokens * vocab * type_bytes(type) > FAR_BYTES / 2 && !off(d_logits, 16) && !off(d_dlogits, 16) && logits_stride * type_bytes(type) % 16 == 0 && dlogits_stride * type_bytes(type) % 16 == 0;
     if (n)
         by_type(type, [&](auto tt) {
             typedef decltype(tt) T;
@@ -400,7 +449,7 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
                 constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
                 hipLaunchKernelGGL(far ? (policy_held<T, NT, NV, true>) : (policy_held<T, NT, NV, false>), dim3(n), dim3(NT), 0, st, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, d_logp, parts, own_stats);
             };
-            if (!d_dlogits || vocab < W) vocab <= 64 * W * STREAM ? twice(Int<64>()) : twice(Int<512>());
+            if (!d_dlogits) vocab <= 64 * W * STREAM ? twice(Int<64>()) : twice(Int<512>());
             else if (vocab <= 64 * 2 * W) held(Int<64>(), Int<2>());
             else if (vocab <= 64 * 8 * W) held(Int<64>(), Int<8>());
             else if (vocab <= 256 * 4 * W) held(Int<256>(), Int<4>());
@@ -408,7 +457,7 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
             else if (vocab <= 512 * 8 * W) held(Int<512>(), Int<8>());
             else if (vocab <= 512 * 14 * W) held(Int<512>(), Int<14>());
             else if (vocab <= 1024 * 14 * W) held(Int<1024>(), Int<14>());
-            else if (vocab <= 1024 * 20 * W) held(Int<1024>(), Int<20>());
+            else if (vocab <= 1024 * 18 * W) held(Int<1024>(), Int<18>());
             else twice(Int<1024>());
         });
     if (n != 1) {
