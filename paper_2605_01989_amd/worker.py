@@ -28,11 +28,12 @@ class Drop(ctypes.Structure):
 
 _lib = None
 _torch = None
+_raw_stream = None               # torch's current stream of a device as an address, without an object for it (2 us less a call)
 _types = {}
 
 
 def _load():
-    global _lib, _torch
+    global _lib, _torch, _raw_stream
     import torch
     L = lib()
     vp, u64, u32, i32, f32 = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int, ctypes.c_float
@@ -49,6 +50,7 @@ def _load():
     L.dblp_worker_error.restype = ctypes.c_char_p
     _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
     _torch = torch
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _lib = L
     return L
 
@@ -64,22 +66,24 @@ def _check(rc):
 
 def _matrix(name, t, dev, rows, cols, dtype=None):
     """(address, row stride) of a matrix; rows or cols None: any."""
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        _bad(f"{name}: shape {tuple(t.shape)} where ({rows}, {cols}) is expected")
-    if t.stride(1) != 1 and t.shape[1] > 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        _bad(f"{name}: shape {tuple(shape)} where ({rows}, {cols}) is expected")
+    if stride[1] != 1 and shape[1] > 1:
         _bad(f"{name}: columns must be adjacent")
     if t.device != dev:
         _bad(f"{name}: on {t.device}, not {dev}")
     if t.dtype not in _types or (dtype is not None and t.dtype != dtype):
         _bad(f"{name}: type {t.dtype}")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
 
 
 def _vector(name, t, dev, n, dtype):
     if t is None:
         return None
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or t.device != dev or (n > 1 and t.stride(0) != 1):
-        _bad(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device} where {n} adjacent {dtype} on {dev} are expected")
+    shape = t.shape
+    if len(shape) != 1 or shape[0] != n or t.dtype != dtype or t.device != dev or (n > 1 and not t.is_contiguous()):
+        _bad(f"{name}: {tuple(shape)} {t.dtype} on {t.device} where {n} adjacent {dtype} on {dev} are expected")
     return t.data_ptr()
 
 
@@ -90,10 +94,11 @@ def _space(t, dev):
 
 
 def _place(dev, stream):
+    """(device ordinal, stream) of a call."""
     if dev.type != "cuda":
         _bad(f"tensors must be on the GPU, not on {dev}")
     if stream is None:
-        stream = _torch.cuda.current_stream(dev).cuda_stream
+        stream = _raw_stream(dev.index) if _raw_stream else _torch.cuda.current_stream(dev).cuda_stream
     return dev.index, stream
 
 
