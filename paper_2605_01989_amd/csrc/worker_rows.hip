@@ -8,17 +8,21 @@
 // ------------------------------------------------------------------------------------------
 // dropout and embedding
 // ------------------------------------------------------------------------------------------
-#define UNITS_EACH 2            // units that a thread has in flight
+// Units that a thread has in flight.  Dropout: one is fastest (8192 x 768 with a residual 7.4 us, 9.1 with two); four columns take two, whose gates
+// lanes share.  Embedding: two, the row's address being a load itself (32768 x 4096 77 us, 84 with one, 95 with four).
+template <int W> struct InFlight { static constexpr int N = W == 4 ? 2 : 1; };
+#define EMBED_EACH 2
 #define FAR_BYTES (256ull << 20)  // matrices that the memory-side cache does not hold are read and written past it
 
-// The gates of a thread's units i and i + 256, as words for load's `shut`.
-template <int W>
-__device__ __forceinline__ void gates_of_units(const Mask& m, u64 draw, u64 unit0, u32 (&gate)[UNITS_EACH][W / 2]) {
+// The gates of a thread's units i, i + 256, ..., as words for `shut`.
+template <int W, int N>
+__device__ __forceinline__ void gates_of_units(const Mask& m, u64 draw, u64 unit0, u32 (&gate)[N][W / 2]) {
     if constexpr (W == 4) {
-        gates_of_two(m, draw, unit0 / 2, (unit0 + 256) / 2, gate[0], gate[1]);
+#pragma unroll
+        for (int j = 0; j < N; j += 2) gates_of_two(m, draw, (unit0 + j * 256) / 2, (unit0 + j * 256 + 256) / 2, gate[j], gate[j + 1]);
     } else {
 #pragma unroll
-        for (int j = 0; j < UNITS_EACH; ++j) {
+        for (int j = 0; j < N; ++j) {
             const Gates g = gates_of(m, draw, unit0 + j * 256);
 #pragma unroll
             for (int k = 0; k < 4; ++k) gate[j][k] = g.w[k];
@@ -30,13 +34,14 @@ template <class T, int W, bool RES, bool WHOLE, bool FAR>
 __global__ __launch_bounds__(256) void dropout_units(Units s, Mask m, const typename T::elem* x, u64 x_stride,
                                                      const typename T::elem* res, u64 res_stride, typename T::elem* y, u64 y_stride) {
     typedef Vec<T, W> V;
-    const u32 i0 = blockIdx.x * (256 * UNITS_EACH) + threadIdx.x;
-    typename V::raw a[UNITS_EACH], b[UNITS_EACH];
-    u32 c[UNITS_EACH], gate[UNITS_EACH][W / 2];
-    u64 row[UNITS_EACH];
-    bool mine[UNITS_EACH];
+    constexpr int N = InFlight<W>::N;
+    const u32 i0 = blockIdx.x * (256 * N) + threadIdx.x;
+    typename V::raw a[N], b[N];
+    u32 c[N], gate[N][W / 2];
+    u64 row[N];
+    bool mine[N];
 #pragma unroll
-    for (int j = 0; j < UNITS_EACH; ++j) {
+    for (int j = 0; j < N; ++j) {
         const u32 i = i0 + j * 256, r = s.per_row.of(i);
         c[j] = (i - r * s.per_row.d) * W;
         row[j] = s.row0 + r;
@@ -45,9 +50,9 @@ __global__ __launch_bounds__(256) void dropout_units(Units s, Mask m, const type
         a[j] = load_cols<V, W, WHOLE, FAR>(x + row[j] * x_stride, c[j], s.cols);
         if (RES) b[j] = load_cols<V, W, WHOLE, FAR>(res + row[j] * res_stride, c[j], s.cols);
     }
-    gates_of_units<W>(m, draw_of(m), s.row0 * s.per_row.d + i0, gate);
+    gates_of_units<W, N>(m, draw_of(m), s.row0 * s.per_row.d + i0, gate);
 #pragma unroll
-    for (int j = 0; j < UNITS_EACH; ++j) {
+    for (int j = 0; j < N; ++j) {
         if (!mine[j]) continue;
         float v[W], w[W];
         V::shut(a[j], gate[j]);
@@ -67,13 +72,14 @@ __global__ __launch_bounds__(256) void embed_units(Units s, Mask m, const int64_
                                                    typename T::elem* __restrict__ out, u64 out_stride) {
     typedef Vec<S, W> VS;
     typedef Vec<T, W> VT;
-    const u32 i0 = blockIdx.x * (256 * UNITS_EACH) + threadIdx.x;
-    typename VS::raw a[UNITS_EACH], b[UNITS_EACH];
-    u32 c[UNITS_EACH], gate[UNITS_EACH][W / 2];
-    u64 row[UNITS_EACH], tok[UNITS_EACH], at[UNITS_EACH];
-    bool mine[UNITS_EACH];
+    constexpr int N = EMBED_EACH;
+    const u32 i0 = blockIdx.x * (256 * N) + threadIdx.x;
+    typename VS::raw a[N], b[N];
+    u32 c[N], gate[N][W / 2];
+    u64 row[N], tok[N], at[N];
+    bool mine[N];
 #pragma unroll
-    for (int j = 0; j < UNITS_EACH; ++j) {
+    for (int j = 0; j < N; ++j) {
         const u32 i = i0 + j * 256, r = s.per_row.of(i);
         c[j] = (i - r * s.per_row.d) * W;
         row[j] = s.row0 + r;
@@ -82,13 +88,13 @@ __global__ __launch_bounds__(256) void embed_units(Units s, Mask m, const int64_
         at[j] = mine[j] && positions ? (u64)positions[row[j]] : n_pos;
     }
 #pragma unroll
-    for (int j = 0; j < UNITS_EACH; ++j) {
+    for (int j = 0; j < N; ++j) {
         if (tok[j] < vocab) a[j] = load_cols<VS, W, WHOLE>(table + tok[j] * table_stride, c[j], s.cols);
         if (at[j] < n_pos) b[j] = load_cols<VS, W, WHOLE>(pos_table + at[j] * pos_stride, c[j], s.cols);
     }
-    if (DROP) gates_of_units<W>(m, draw_of(m), s.row0 * s.per_row.d + i0, gate);
+    if (DROP) gates_of_units<W, N>(m, draw_of(m), s.row0 * s.per_row.d + i0, gate);
 #pragma unroll
-    for (int j = 0; j < UNITS_EACH; ++j) {
+    for (int j = 0; j < N; ++j) {
         if (!mine[j]) continue;
         float v[W] = {}, w[W];
         if (tok[j] < vocab) {                        // (a select, not a product with zero: scale may be infinite)
@@ -114,7 +120,8 @@ __global__ __launch_bounds__(256) void embed_units(Units s, Mask m, const int64_
 // gradient of the embedding: a table row's gradient is the sum over the places of its token, so the places are sorted by token
 // (stably: a row is summed in the order of its places) and the sorted list is cut into pieces of equal length
 // ------------------------------------------------------------------------------------------
-struct Result { const float* base; u64 base_stride; float* grad; u64 grad_stride; u64 vocab; float scale; };
+// far: base and gradient are more than the memory-side cache should hold, and lie on multiples of 16 bytes
+struct Result { const float* base; u64 base_stride; float* grad; u64 grad_stride; u64 vocab; float scale; bool far; };
 typedef Vec<F32, 4> G4;                          // of the gradient and its base
 
 // Rows of the result as they are without a token: FILL_EACH units a thread, NT threads a block.  `present`: a byte a row, whether it has a token and
@@ -143,13 +150,19 @@ __device__ __forceinline__ void fill_block(const Result& out, const Units& s, u3
     }
     if (out.base) {
 #pragma unroll
-        for (int k = 0; k < FILL_EACH; ++k) if (mine[k]) v[k] = load_cols<G4, 4, false>(out.base + (s.row0 + r[k]) * out.base_stride, c[k], s.cols);
+        for (int k = 0; k < FILL_EACH; ++k) {
+            if (!mine[k]) continue;
+            const float* row = out.base + (s.row0 + r[k]) * out.base_stride;
+            v[k] = out.far ? load_cols<G4, 4, true, true>(row, c[k], s.cols) : load_cols<G4, 4, false>(row, c[k], s.cols);
+        }
     }
 #pragma unroll
     for (int k = 0; k < FILL_EACH; ++k) {
         if (!mine[k]) continue;
         const float y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-        store_cols<G4, 4>(out.grad + (s.row0 + r[k]) * out.grad_stride, c[k], s.cols, y);
+        float* row = out.grad + (s.row0 + r[k]) * out.grad_stride;
+        if (out.far) store_cols<G4, 4, true>(row, c[k], s.cols, y);
+        else store_cols<G4, 4>(row, c[k], s.cols, y);
     }
 }
 static u32 fill_blocks(const Units& s, u32 nt = 256) { return blocks_of(s.n, nt * FILL_EACH); }
@@ -303,14 +316,14 @@ __device__ __forceinline__ void pad_lists(u32* keys, u32* places, u32 n, u64 voc
     }
 }
 
-// All places of a short batch by one block, keys and places in LDS between the passes; the launch's other blocks write the result's rows
-// meanwhile (those that have a token are written again later, they are few next to the table).
+// All places of a short batch by one block, keys and places in LDS between the passes; the launch's other blocks write rows of the result
+// meanwhile (those that have a token are written again later, they are few next to the table).  `present`: marks of the rows that have a token, or null.
 #define SORT_BLOCK_ROWS 16
 #define SORT_BLOCK_MOST (1024 * SORT_BLOCK_ROWS)
 struct SortLds { u32 keys[SORT_BLOCK_MOST]; u16 places[SORT_BLOCK_MOST]; u32 counts[16][BINS]; u32 part[16]; };
 
 __global__ __launch_bounds__(1024) void sort_one_block(SortShape q, const int64_t* __restrict__ tokens, u32* __restrict__ keys_out, u32* __restrict__ places_out, u32* __restrict__ n_chains,
-                                                       Units s, Result out) {
+                                                       uint8_t* __restrict__ present, Units s, Result out) {
     __shared__ SortLds L;
     const u32 tid = threadIdx.x;
     if (blockIdx.x) {
@@ -321,6 +334,7 @@ __global__ __launch_bounds__(1024) void sort_one_block(SortShape q, const int64_
     const u32 rows = (q.n + 1023) / 1024;                // of 64 places, of each wave
     if (tid == 0) *n_chains = 0;
     pad_lists(keys_out, places_out, q.n, q.vocab);
+    if (present) for (u32 i = tid; i < (u32)(q.vocab + 3) / 4; i += 1024) ((u32*)present)[i] = 0;      // (the passes' barriers come before the marks)
     u32 key[SORT_BLOCK_ROWS], place[SORT_BLOCK_ROWS], rank[SORT_BLOCK_ROWS];
 #pragma unroll
     for (u32 r = 0; r < SORT_BLOCK_ROWS; ++r) {
@@ -356,7 +370,11 @@ __global__ __launch_bounds__(1024) void sort_one_block(SortShape q, const int64_
         for (u32 r = 0; r < SORT_BLOCK_ROWS; ++r)
             if (r < rows && (w * rows + r) * 64 + lane < q.n) {
                 const u32 to = L.counts[w][(key[r] >> shift) & mask] + rank[r];
-                if (last) { keys_out[to] = key[r]; places_out[to] = place[r]; }
+                if (last) {
+                    keys_out[to] = key[r];
+                    places_out[to] = place[r];
+                    if (present && key[r] != NO_TOKEN(q.vocab)) present[key[r]] = 1;
+                }
                 else { L.keys[to] = key[r]; L.places[to] = (u16)place[r]; }
             }
         if (last) break;
@@ -370,7 +388,7 @@ __global__ __launch_bounds__(1024) void sort_one_block(SortShape q, const int64_
 }
 
 // Longer batches: at most SORT_TILES tiles, two launches a pass (count, move).  The first launch clears the marks of the rows that have a token, the
-// second sets them, the later ones write some of the rows that have none beside their own work.
+// second sets them; their other blocks write rows of the result, the later ones only such that have no token.
 #define SORT_TILES 64
 #define SORT_STEP 1024                           // items that a block of 256 threads moves at once
 struct SortFrom { const int64_t* tokens; const u32 *keys, *places; };            // tokens in the first pass, keys and places later
@@ -502,7 +520,7 @@ __global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys,
 #pragma unroll
         for (int j = 0; j < B; ++j)
             if (k[j] != none && here) {
-                v[j] = load_cols<V, 4, WHOLE>(dy + (u64)p[j] * dy_stride, c, s.cols);
+                v[j] = load_cols<V, 4, WHOLE, true>(dy + (u64)p[j] * dy_stride, c, s.cols);
                 if (BASE) base[j] = load_cols<G4, 4, WHOLE>(out.base + (u64)k[j] * out.base_stride, c, s.cols);
             }
         k[B] = at + B < to ? at_k[0].x : none;
@@ -617,7 +635,7 @@ extern "C" int dblp_embed(int device, void* stream, const int64_t* d_tokens, uin
             each_launch<W>(n_tokens, dim, [&](Units s) {
                 const auto pick = [&](auto whole, auto far_out) { return m.on ? embed_units<S, T, W, true, decltype(whole)::value, decltype(far_out)::value> : embed_units<S, T, W, false, decltype(whole)::value, decltype(far_out)::value>; };
                 const auto kernel = dim % 8 ? pick(Int<0>(), Int<0>()) : far ? pick(Int<1>(), Int<1>()) : pick(Int<1>(), Int<0>());
-                hipLaunchKernelGGL(kernel, dim3(blocks_of(s.n, 256 * UNITS_EACH)), dim3(256), 0, (hipStream_t)stream, s, m, d_tokens, (const typename S::elem*)d_table, (u64)table_stride, (u64)vocab, scale,
+                hipLaunchKernelGGL(kernel, dim3(blocks_of(s.n, 256 * EMBED_EACH)), dim3(256), 0, (hipStream_t)stream, s, m, d_tokens, (const typename S::elem*)d_table, (u64)table_stride, (u64)vocab, scale,
                                    d_positions, (const typename S::elem*)d_pos_table, (u64)pos_stride, (u64)n_positions, (typename T::elem*)d_out, (u64)out_stride);
             });
         });
@@ -663,10 +681,12 @@ extern "C" uint64_t dblp_embed_grad_workspace(uint64_t n_tokens, uint64_t vocab,
     return grad_plan(n_tokens, vocab, dim).bytes;
 }
 
-// Which rows without a token are written beside which launch.  Sorting and chains leave the memory idle for about as long as it takes to move these
-// bytes, what is left goes beside the pieces.  (A short batch's sort is one block's, and the whole table is written beside it.)
-#define FILL_SORT (24ull << 20)                  // beside each launch of a tiled sort that knows the marks
+// Which rows without a token are written beside which launch.  Sorting, short batches' pieces and chains leave the memory idle for about as long as it takes to
+// move these bytes; what is left goes beside the one-block sort, or the pieces of a long batch.  Rows written before the marks are known may be written again.
+#define FILL_SORT (24ull << 20)                  // beside each launch of a tiled sort
+#define FILL_PIECES (32ull << 20)
 #define FILL_CHAINS (12ull << 20)
+#define MARK_MOST (1u << 20)                     // rows whose marks one block clears beside its sort
 
 struct Fill {
     u32 dim, per_row;
@@ -699,7 +719,9 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
     const hipStream_t st = (hipStream_t)stream;
-    const Result out = {d_base, base_stride, d_grad, grad_stride, vocab, scale};
+    // (the hint takes a copy of 154 MB from 55 to 48 us, one of 38 MB from 11 to 14)
+    const bool far = vocab * dim * (d_base ? 8 : 4) > FAR_BYTES / 2 && dim % 4 == 0 && !off(d_base, 16) && !off(d_grad, 16) && base_stride % 4 == 0 && grad_stride % 4 == 0;
+    const Result out = {d_base, base_stride, d_grad, grad_stride, vocab, scale, far};
     const GradPlan p = grad_plan(n_tokens, vocab, dim);
     const u32 n = (u32)n_tokens, units = units_per_row<4>(dim);
     if (p.short_batch) {
@@ -730,20 +752,20 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
     if (!in_place && !beside)
         each_launch<4>(vocab, dim, [&](Units s) { hipLaunchKernelGGL(fill_rows, dim3(fill_blocks(s)), dim3(256), 0, st, s, out); });
     Fill fill = {dim, units, 0, beside ? vocab : 0, (u64)dim * (d_base ? 8 : 4)};
-    uint8_t* const present = beside && !one_block ? ws + p.present : nullptr;
+    uint8_t* const present = beside && (!one_block || vocab <= MARK_MOST) ? ws + p.present : nullptr;
     int at = 0;
     if (one_block) {
-        const Units s = fill.take(fill.left());
-        hipLaunchKernelGGL(sort_one_block, dim3(1 + fill_blocks(s, 1024)), dim3(1024), 0, st, q, d_tokens, (u32*)(ws + p.keys[0]), (u32*)(ws + p.places[0]), n_chains, s, out);
+        const Units s = fill.all_but(present ? FILL_PIECES + FILL_CHAINS : 0);
+        hipLaunchKernelGGL(sort_one_block, dim3(1 + fill_blocks(s, 1024)), dim3(1024), 0, st, q, d_tokens, (u32*)(ws + p.keys[0]), (u32*)(ws + p.places[0]), n_chains, present, s, out);
     } else {
         for (u32 pass = 0; pass < p.passes; ++pass, at ^= 1) {
             const SortFrom from = {pass ? nullptr : d_tokens, pass ? (u32*)(ws + p.keys[at ^ 1]) : nullptr, pass ? (u32*)(ws + p.places[at ^ 1]) : nullptr};
             const u32 clear = pass == 0 && present ? (u32)(round_up(vocab, 256) / 4) : 0;
-            const Units a = fill.take(pass ? FILL_SORT : 0), b = fill.take(pass ? FILL_SORT : 0);
+            const Units a = fill.take(FILL_SORT), b = fill.take(FILL_SORT);
             const u32 others = fill_blocks(a) + (u32)((clear + 1023) / 1024);
-            hipLaunchKernelGGL(sort_count, dim3(p.tiles + others), dim3(256), 0, st, q, from, pass * p.bits, p.tile, p.tiles, (u32*)(ws + p.hist), n_chains, (u32*)present, clear, a, out, (const uint8_t*)present);
+            hipLaunchKernelGGL(sort_count, dim3(p.tiles + others), dim3(256), 0, st, q, from, pass * p.bits, p.tile, p.tiles, (u32*)(ws + p.hist), n_chains, (u32*)present, clear, a, out, (const uint8_t*)(pass ? present : nullptr));
             hipLaunchKernelGGL(sort_move, dim3(p.tiles + fill_blocks(b)), dim3(256), 0, st, q, from, pass * p.bits, p.tile, p.tiles, (const u32*)(ws + p.hist), (u32*)(ws + p.keys[at]), (u32*)(ws + p.places[at]),
-                               pass == 0 ? present : (uint8_t*)nullptr, b, out, (const uint8_t*)present);
+                               pass == 0 ? present : (uint8_t*)nullptr, b, out, (const uint8_t*)(pass ? present : nullptr));
         }
         at ^= 1;
     }
@@ -785,7 +807,7 @@ extern "C" int dblp_dropout(int device, void* stream, uint64_t rows, uint32_t co
     if (rows == 0) return DBLP_OK;
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
-    const bool far = rows * cols * type_bytes(type) * (d_residual ? 3 : 2) > FAR_BYTES;
+    const bool far = rows * cols * type_bytes(type) * (d_residual ? 3 : 2) >= FAR_BYTES;
     by_type(type, [&](auto tt) {
         typedef decltype(tt) T;
         typedef const typename T::elem* in;
@@ -793,7 +815,7 @@ extern "C" int dblp_dropout(int device, void* stream, uint64_t rows, uint32_t co
         each_launch<W>(rows, cols, [&](Units s) {
             const auto pick = [&](auto whole, auto past) { return d_residual ? dropout_units<T, W, true, decltype(whole)::value, decltype(past)::value> : dropout_units<T, W, false, decltype(whole)::value, decltype(past)::value>; };
             const auto kernel = cols % 8 ? pick(Int<0>(), Int<0>()) : far ? pick(Int<1>(), Int<1>()) : pick(Int<1>(), Int<0>());
-            hipLaunchKernelGGL(kernel, dim3(blocks_of(s.n, 256 * UNITS_EACH)), dim3(256), 0, (hipStream_t)stream, s, m, (in)d_x, (u64)x_stride, (in)d_residual, (u64)residual_stride, (typename T::elem*)d_y, (u64)y_stride);
+            hipLaunchKernelGGL(kernel, dim3(blocks_of(s.n, 256 * InFlight<W>::N)), dim3(256), 0, (hipStream_t)stream, s, m, (in)d_x, (u64)x_stride, (in)d_residual, (u64)residual_stride, (typename T::elem*)d_y, (u64)y_stride);
         });
     });
     return launched(call);
