@@ -140,6 +140,57 @@ __global__ __launch_bounds__(NT) void logprob_rows(const typename T::elem* __res
     }
 }
 
+// Few long rows: blocks share a row.  This launch finds (m, s) of each share and keeps the target's logit (the next launch may write the gradient over it), the next
+// one joins them.
+#define SHARES_MOST 32
+#define SHARE_NT 256
+struct Shares { u32 n, vecs; };                  // shares of a row, vectors of each
+template <class T>
+__device__ __forceinline__ void share_of(const Cut& c, const Shares& q, u32 s, u32* lo, u32* hi) {
+    *lo = s * q.vecs < c.vecs ? s * q.vecs : c.vecs;
+    *hi = c.vecs - *lo < q.vecs ? c.vecs : *lo + q.vecs;
+}
+// (`weights`: a row of weight zero is not read; null: all rows with a target are)
+template <class T>
+__global__ __launch_bounds__(SHARE_NT) void soft_shares(Shares q, const typename T::elem* __restrict__ logits, u64 stride, u32 vocab, const int64_t* __restrict__ targets, const float* __restrict__ weights,
+                                                        Soft* __restrict__ softs, float* __restrict__ chosen) {
+    constexpr int W = Wide<T>::W;
+    __shared__ Soft part[SHARE_NT / WAVE];
+    const u32 s = blockIdx.x, t = blockIdx.y;
+    if ((u64)targets[t] >= vocab || (weights && weights[t] == 0.0f)) return;
+    const typename T::elem* row = logits + (u64)t * stride;
+    const Cut c = cut_row<T>(row, vocab);
+    u32 lo, hi;
+    share_of<T>(c, q, s, &lo, &hi);
+    Soft a = {-INFINITY, 0.0f};
+    const float single = s == 0 && threadIdx.x < c.singles ? (float)row[place_of_single<W>(c, threadIdx.x)] : -INFINITY;
+    soft_vecs<T, SHARE_NT, false>(a, row + c.head, lo, hi);
+    soft_add_one(a, single);
+    a = soft_block<SHARE_NT>(a, part);
+    if (threadIdx.x == 0) {
+        softs[t * q.n + s] = a;
+        if (s == 0) chosen[t] = (float)row[targets[t]];
+    }
+}
+// A row's (m, s), to every lane of a wave.
+__device__ __forceinline__ Soft soft_of_row(const Soft* softs, u32 t, u32 n) {
+    const u32 lane = threadIdx.x & 63;
+    return soft_wave(lane < n ? softs[t * n + lane] : Soft{-INFINITY, 0.0f});
+}
+__global__ __launch_bounds__(64) void logprob_join(Shares q, u32 vocab, const int64_t* __restrict__ targets, const Soft* __restrict__ softs, const float* __restrict__ chosen,
+                                                   float* __restrict__ logp, float* __restrict__ lse) {
+    const u32 t = blockIdx.x;
+    const u64 at = (u64)targets[t];
+    if (at >= vocab) {
+        if (threadIdx.x == 0) { logp[t] = 0.0f; if (lse) lse[t] = 0.0f; }
+        return;
+    }
+    const Soft a = soft_of_row(softs, t, q.n);
+    if (threadIdx.x) return;
+    if (lse) lse[t] = (float)((double)a.m + log_of(a.s));
+    logp[t] = a.m == -INFINITY ? -INFINITY : (float)logp_of(chosen[t], a);
+}
+
 // ------------------------------------------------------------------------------------------
 // policy loss
 // ------------------------------------------------------------------------------------------
@@ -346,6 +397,71 @@ __device__ __forceinline__ bool sum_block(double (&s)[4], double (&sh)[4][NT / W
     for (int i = 0; i < 4; ++i) { s[i] = 0; for (int w = 0; w < NT / WAVE; ++w) s[i] += sh[i][w]; }
     return true;
 }
+// Few long rows, the second launch: every block of a row joins its shares and finds the slope for itself; one block more does so for all tokens (at most SHARE_NT) and adds
+// them up.
+template <class T>
+__global__ __launch_bounds__(SHARE_NT) void policy_shares(Shares q, Policy p, const typename T::elem* logits, u64 stride, u32 vocab, typename T::elem* dlogits, u64 dstride, u32 n,
+                                                          const Soft* __restrict__ softs, const float* __restrict__ chosen, float* __restrict__ logp, float* __restrict__ stats) {
+    constexpr int W = Wide<T>::W;
+    typedef Vec<T, W> V;
+    typedef typename T::elem E;
+    const u32 s = blockIdx.x, tid = threadIdx.x;
+    if (s == q.n) {                                        // the sums
+        __shared__ double sh[4][SHARE_NT / WAVE];
+        if (blockIdx.y) return;
+        double sum[4] = {0, 0, 0, 0};
+        if (tid < n) {
+            const u64 at = (u64)p.targets[tid];
+            const bool read = at < vocab && p.weights[tid] != 0.0f;
+            Soft a = {-INFINITY, 0.0f};
+            if (read) for (u32 i = 0; i < q.n; ++i) a = soft_join(a, softs[tid * q.n + i]);
+            double lp = read ? -INFINITY : 0.0;
+            if (a.m != -INFINITY) {
+                float slope;
+                lp = logp_of(chosen[tid], a);
+                const TokenPart part = token_part(p, tid, lp, &slope);
+                sum[0] = part.policy; sum[1] = part.kl; sum[2] = part.clipped; sum[3] = part.counted;
+            }
+            if (logp) logp[tid] = (float)lp;
+        }
+        if (sum_block<SHARE_NT>(sum, sh)) put_stats(stats, sum, p.kl);
+        return;
+    }
+    const u32 t = blockIdx.y;
+    const u64 at = (u64)p.targets[t];
+    const E* row = logits + (u64)t * stride;
+    E* drow = dlogits + (u64)t * dstride;
+    const Cut c = cut_row<T>(row, vocab);
+    u32 lo, hi;
+    share_of<T>(c, q, s, &lo, &hi);
+    Soft a = {-INFINITY, 0.0f};
+    if (at < vocab && p.weights[t] != 0.0f) a = soft_of_row(softs, t, q.n);
+    const bool counted = a.m != -INFINITY;
+    float g = 0.0f;
+    if (counted) token_part(p, t, logp_of(chosen[t], a), &g);
+    g *= p.grad_scale;
+    const float k = counted ? -g / a.s : 0.0f;
+    const u32 single = s == 0 && tid < c.singles ? place_of_single<W>(c, tid) : 0;
+    for (u32 i = lo + tid; i < hi; i += SHARE_NT * STREAM) {
+        typename V::raw r[STREAM] = {};
+        if (counted) {
+#pragma unroll
+            for (int j = 0; j < STREAM; ++j) if (i + j * SHARE_NT < hi) r[j] = V::load(row + c.head + (u64)(i + j * SHARE_NT) * W);
+        }
+#pragma unroll
+        for (int j = 0; j < STREAM; ++j) {
+            if (i + j * SHARE_NT >= hi) continue;
+            const u64 to = c.head + (u64)(i + j * SHARE_NT) * W;
+            float y[W];
+            V::open(r[j], y);
+#pragma unroll
+            for (int e = 0; e < W; ++e) y[e] = counted ? k * exp_of(y[e], a.m) + (to + e == at ? g : 0.0f) : 0.0f;
+            V::store(drow + to, V::pack(y));
+        }
+    }
+    if (s == 0 && tid < c.singles) drow[single] = (E)(counted ? k * exp_of((float)row[single], a.m) + (single == at ? g : 0.0f) : 0.0f);
+}
+
 __global__ __launch_bounds__(1024) void policy_sums(const TokenPart* __restrict__ parts, u32 n, float kl_coef, double* __restrict__ shares, float* __restrict__ stats) {
     __shared__ double sh[4][16];
     double s[4] = {0, 0, 0, 0};
@@ -372,10 +488,23 @@ __global__ __launch_bounds__(256) void policy_join(const double* __restrict__ sh
 // ------------------------------------------------------------------------------------------
 #define FAR_BYTES (256ull << 20)                 // logits that the memory-side cache does not hold are read and written past it
 
-struct LogitsPlan { u64 shares, bytes; };        // the tokens' parts come first
+// Where the workspace holds the shares of sums and of rows; the tokens' parts come first.
+struct LogitsPlan { u64 sums, softs, chosen, bytes; };
+// Fewer rows than FEW_ROWS leave half of the CUs without one: blocks share a row of at least MANY_VECS vectors.  Policy loss, with the sums, of rows of 50257 floats: 64 rows
+// 17 us by a block each, 14.5 shared; 100 18, 16; 140 19, 20; 190 21, 25; two rows of 150000 25, 10.
+#define FEW_ROWS 128
+#define MANY_VECS 2048
 static LogitsPlan logits_plan(u64 n) {
-    const u64 parts = round_up(n * sizeof(TokenPart), 256);
-    return {parts, parts + round_up((n + SUM_SHARE - 1) / SUM_SHARE * 32, 256) + 256};
+    const u64 sums = round_up(n * sizeof(TokenPart), 256), softs = sums + round_up((n + SUM_SHARE - 1) / SUM_SHARE * 32, 256);
+    const u64 few = n < FEW_ROWS ? n : 0, chosen = softs + round_up(few * SHARES_MOST * sizeof(Soft), 256);
+    return {sums, softs, chosen, chosen + round_up(few * 4, 256) + 256};
+}
+// About three blocks a CU, of at least two vectors a thread.
+static Shares shares_of(u64 n, u32 vecs) {
+    u32 k = (u32)(768 / n);
+    if (k > vecs / (2 * SHARE_NT)) k = vecs / (2 * SHARE_NT);
+    if (k > SHARES_MOST) k = SHARES_MOST;
+    return {k, (vecs + k - 1) / k};
 }
 
 extern "C" uint64_t dblp_logits_workspace(uint64_t n_tokens, uint32_t vocab) {
@@ -402,6 +531,16 @@ extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, 
             constexpr int NT = decltype(nt)::value;
             hipLaunchKernelGGL(far ? (logprob_rows<T, NT, true>) : (logprob_rows<T, NT, false>), dim3((u32)n_tokens), dim3(NT), 0, (hipStream_t)stream, (const typename T::elem*)d_logits, (u64)logits_stride, vocab, d_targets, d_logp, d_lse);
         };
+        const u32 vecs = vocab / Wide<T>::W;
+        // rows that one CU reads for longer than a launch more takes, on the host too: one row of 200000 floats 12 us by a block, 5 shared; of 50257 16-bit values 6, 5
+        if (n_tokens < FEW_ROWS / 2 && vecs >= 16 * MANY_VECS) {
+            const Shares q = shares_of(n_tokens, vecs);
+            Soft* const softs = (Soft*)((uint8_t*)d_workspace + logits_plan(n_tokens).softs);
+            float* const chosen = (float*)((uint8_t*)d_workspace + logits_plan(n_tokens).chosen);
+            hipLaunchKernelGGL(soft_shares<T>, dim3(q.n, (u32)n_tokens), dim3(SHARE_NT), 0, (hipStream_t)stream, q, (const typename T::elem*)d_logits, (u64)logits_stride, vocab, d_targets, (const float*)nullptr, softs, chosen);
+            hipLaunchKernelGGL(logprob_join, dim3((u32)n_tokens), dim3(64), 0, (hipStream_t)stream, q, vocab, d_targets, (const Soft*)softs, (const float*)chosen, d_logp, d_lse);
+            return;
+        }
         // a wave for a row that it reads in one step; many threads where there are few rows
         if (vocab <= 64 * Wide<T>::W * STREAM) go(Int<64>());
         else if (n_tokens <= 512 && vocab > 512 * Wide<T>::W * STREAM) go(Int<1024>());
@@ -430,7 +569,10 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
     if (on.err != hipSuccess) return no_device(call, on.err);
     const Policy p = {d_targets, d_advantages, d_weights, d_old_logp, d_ref_logp, clip_low, clip_high, kl_coef, grad_scale};
     TokenPart* const parts = (TokenPart*)d_workspace;
-    double* const shares = (double*)((uint8_t*)d_workspace + logits_plan(n_tokens).shares);
+    double* const shares = (double*)((uint8_t*)d_workspace + logits_plan(n_tokens).sums);
+    Soft* const softs = (Soft*)((uint8_t*)d_workspace + logits_plan(n_tokens).softs);
+    float* const chosen = (float*)((uint8_t*)d_workspace + logits_plan(n_tokens).chosen);
+    bool summed = false;
     const hipStream_t st = (hipStream_t)stream;
     const u32 n = (u32)n_tokens;
     float* const own_stats = n == 1 ? d_stats : nullptr;         // one token's sums are its own
@@ -449,7 +591,15 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
                 constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
                 hipLaunchKernelGGL(far ? (policy_held<T, NT, NV, true>) : (policy_held<T, NT, NV, false>), dim3(n), dim3(NT), 0, st, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, d_logp, parts, own_stats);
             };
-            if (!d_dlogits) vocab <= 64 * W * STREAM ? twice(Int<64>()) : twice(Int<512>());
+            const u32 vecs = vocab / W;
+            // (one token's row, if registers hold it, needs one launch where sharing needs two)
+            if (d_dlogits && n < FEW_ROWS && vecs >= MANY_VECS && !(n == 1 && vocab <= 1024 * 18 * W)) {
+                const Shares q = shares_of(n, vecs);
+                hipLaunchKernelGGL(soft_shares<T>, dim3(q.n, n), dim3(SHARE_NT), 0, st, q, (const E*)d_logits, (u64)logits_stride, vocab, d_targets, d_weights, softs, chosen);
+                hipLaunchKernelGGL(policy_shares<T>, dim3(q.n + 1, n), dim3(SHARE_NT), 0, st, q, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, n, (const Soft*)softs, (const float*)chosen, d_logp, d_stats);
+                summed = true;
+            }
+            else if (!d_dlogits) vocab <= 64 * W * STREAM ? twice(Int<64>()) : twice(Int<512>());
             else if (vocab <= 64 * 2 * W) held(Int<64>(), Int<2>());
             else if (vocab <= 64 * 8 * W) held(Int<64>(), Int<8>());
             else if (vocab <= 256 * 4 * W) held(Int<256>(), Int<4>());
@@ -460,7 +610,7 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
             else if (vocab <= 1024 * 18 * W) held(Int<1024>(), Int<18>());
             else twice(Int<1024>());
         });
-    if (n != 1) {
+    if (n != 1 && !summed) {
         const u32 blocks = n ? (n + SUM_SHARE - 1) / SUM_SHARE : 1;
         hipLaunchKernelGGL(policy_sums, dim3(blocks), dim3(1024), 0, st, (const TokenPart*)parts, n, kl_coef, shares, d_stats);
         if (blocks > 1) hipLaunchKernelGGL(policy_join, dim3(1), dim3(256), 0, st, (const double*)shares, blocks, kl_coef, d_stats);

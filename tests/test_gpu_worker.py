@@ -242,7 +242,7 @@ def test_embed_grad_is_the_gradient_and_leaves_other_rows_alone():
 
 # (rows, vocabulary, padding, shift): one value, odd widths, rows that a block takes in one, several and many pieces
 LOGITS = [(0, 5, 0, 0), (1, 1, 0, 0), (2, 7, 0, 1), (5, 100, 0, 0), (3, 1021, 3, 1), (40, 4096, 0, 0), (1, 50257, 0, 0), (7, 50257, 47, 0), (300, 5003, 0, 1), (2, 140001, 0, 1),
-          (1, 300000, 0, 0), (700, 515, 1, 0)]
+          (1, 300000, 0, 0), (700, 515, 1, 0), (90, 16387, 0, 1), (130, 16390, 1, 0), (3, 262145, 1, 1)]
 
 
 def make_logits(g, n, vocab, pad, shift, t):
