@@ -90,7 +90,8 @@ int dblp_dropout(int device, void* stream, uint64_t rows, uint32_t cols, const v
                  void* d_y, uint64_t y_stride, int type);
 
 /* logp[t] = logits[t][targets[t]] - lse[t], lse[t] = log sum_j exp(logits[t][j]).  d_lse may be NULL.  A row
- * without a target is not read, its logp and lse are 0.  A row whose logits are all -inf has lse = logp = -inf. */
+ * without a target is not read, its logp and lse are 0.  A row whose logits are all -inf has lse = logp = -inf,
+ * one that holds NaN or +inf has NaN. */
 int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, uint32_t vocab, const void* d_logits,
                         uint64_t logits_stride, int type, const int64_t* d_targets, float* d_logp, float* d_lse,
                         void* d_workspace, uint64_t workspace_bytes);
@@ -99,7 +100,7 @@ int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, uint32_t vo
  *   r  = exp(lp - old_logp[t])                          (d_old_logp NULL: the policy is its own old one, r = 1)
  *   pl = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),      A = advantages[t]
  *   kl = exp(ref_logp[t] - lp) - (ref_logp[t] - lp) - 1          (d_ref_logp NULL: 0)
- *   loss = sum of weights[t] (pl + kl_coef kl)
+ *   loss = sum of weights[t] (pl + kl_coef kl)          (kl_coef 0: no KL term in loss and gradient, its sum is watched)
  *   d loss / d lp = weights[t] ([clipped term larger or equal] -r A + kl_coef (1 - exp(ref_logp[t] - lp)))
  *   dlogits[t][j] = grad_scale (d loss / d lp) ([j = targets[t]] - softmax(logits[t])[j])
  * The weights hold the normalisation (one over the number of tokens, or of a sequence's tokens, ...).  With A = 1 and no old

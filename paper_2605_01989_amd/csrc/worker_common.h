@@ -1,5 +1,6 @@
 // What the worker's operators share: element types and their vectors, dropout masks, and the host's checks and launches.
 #pragma once
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

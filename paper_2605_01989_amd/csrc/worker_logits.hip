@@ -6,7 +6,7 @@
 #include "worker_common.h"
 
 // ------------------------------------------------------------------------------------------
-// a row's largest value m and s = sum of exp(x - m).  Nothing met: (-inf, 0)
+// a row's largest value m and s = sum of exp(x - m).  Nothing met: (-inf, 0), and nothing else has s = 0: a NaN makes s NaN, whatever m is
 // ------------------------------------------------------------------------------------------
 #define LOG2E 1.4426950408889634f
 
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(NT) void logprob_rows(const typename T::elem* __res
     const Soft a = soft_block<NT>(soft_row<T, NT, FAR>(row, vocab), part);
     if (threadIdx.x == 0) {
         if (lse) lse[t] = (float)((double)a.m + log_of(a.s));
-        logp[t] = a.m == -INFINITY ? -INFINITY : (float)logp_of(x, a);
+        logp[t] = a.s == 0.0f ? -INFINITY : (float)logp_of(x, a);
     }
 }
 
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64) void logprob_join(Shares q, u32 vocab, const in
     const Soft a = soft_of_row(softs, t, q.n);
     if (threadIdx.x) return;
     if (lse) lse[t] = (float)((double)a.m + log_of(a.s));
-    logp[t] = a.m == -INFINITY ? -INFINITY : (float)logp_of(chosen[t], a);
+    logp[t] = a.s == 0.0f ? -INFINITY : (float)logp_of(chosen[t], a);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -211,7 +211,8 @@ __device__ __forceinline__ float exp_past(float d) {
 // hold the row.)
 __device__ __forceinline__ TokenPart token_part(const Policy& p, u32 t, double lp, float* slope) {
     const float w = p.weights[t], a = p.advantages[t];
-    const float r = p.old_logp ? exp_of((float)(lp - (double)p.old_logp[t]), 0.0f) : 1.0f;
+    float r = p.old_logp ? exp_of((float)(lp - (double)p.old_logp[t]), 0.0f) : 1.0f;
+    if (r == INFINITY) r = FLT_MAX;                        // a ratio past fp32 times an advantage of zero is zero
     const float lo = 1.0f - p.low, hi = 1.0f + p.high;
     const float free_term = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
     const bool clipped = held < free_term;
@@ -219,14 +220,14 @@ __device__ __forceinline__ TokenPart token_part(const Policy& p, u32 t, double l
     if (p.ref_logp) {
         const float d = (float)((double)p.ref_logp[t] - lp);
         kl = exp_past(d);
-        g -= p.kl * (kl + d);
+        if (p.kl != 0.0f) g -= p.kl * (kl + d);            // (watched only: an infinite term is not multiplied by zero)
     }
     *slope = w * g;
     return {w * -(clipped ? held : free_term), w * kl, 1u, clipped ? 1u : 0u};
 }
 
 __device__ __forceinline__ void put_stats(float* stats, const double (&s)[4], float kl_coef) {
-    stats[0] = (float)(s[0] + (double)kl_coef * s[1]);
+    stats[0] = (float)(kl_coef != 0.0f ? s[0] + (double)kl_coef * s[1] : s[0]);
     stats[1] = (float)s[0]; stats[2] = (float)s[1]; stats[3] = (float)s[2]; stats[4] = (float)s[3];
 }
 
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(NT) HELD_WAVES void policy_held(Policy p, const typ
     }
     soft_add_one(a, single);
     a = soft_block<NT>(a, part);
-    if (a.m == -INFINITY) { skip_row<T, NT>(drow, vocab, t, true, logp, parts, stats); return; }
+    if (a.s == 0.0f) { skip_row<T, NT>(drow, vocab, t, true, logp, parts, stats); return; }
     if (tid == 0) slope_sh = close_row(p, t, x, a, logp, parts, stats);
     __syncthreads();
     const float g = slope_sh, k = -g / a.s;
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(NT) void policy_twice(Policy p, const typename T::e
     if (at >= vocab || p.weights[t] == 0.0f) { skip_row<T, NT>(drow, vocab, t, false, logp, parts, stats); return; }
     const float x = tid == 0 ? (float)row[at] : 0.0f;
     const Soft a = soft_block<NT>(soft_row<T, NT, false>(row, vocab), part);
-    if (a.m == -INFINITY) { skip_row<T, NT>(drow, vocab, t, true, logp, parts, stats); return; }
+    if (a.s == 0.0f) { skip_row<T, NT>(drow, vocab, t, true, logp, parts, stats); return; }
     if (tid == 0) slope_sh = close_row(p, t, x, a, logp, parts, stats);
     __syncthreads();
     if (!drow) return;
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(SHARE_NT) void policy_shares(Shares q, Policy p, co
             Soft a = {-INFINITY, 0.0f};
             if (read) for (u32 i = 0; i < q.n; ++i) a = soft_join(a, softs[tid * q.n + i]);
             double lp = read ? -INFINITY : 0.0;
-            if (a.m != -INFINITY) {
+            if (a.s != 0.0f) {
                 float slope;
                 lp = logp_of(chosen[tid], a);
                 const TokenPart part = token_part(p, tid, lp, &slope);
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(SHARE_NT) void policy_shares(Shares q, Policy p, co
     share_of<T>(c, q, s, &lo, &hi);
     Soft a = {-INFINITY, 0.0f};
     if (at < vocab && p.weights[t] != 0.0f) a = soft_of_row(softs, t, q.n);
-    const bool counted = a.m != -INFINITY;
+    const bool counted = a.s != 0.0f;
     float g = 0.0f;
     if (counted) token_part(p, t, logp_of(chosen[t], a), &g);
     g *= p.grad_scale;

@@ -531,3 +531,56 @@ def test_refusals_of_the_binding_on_the_gpu():
             f()
     dblp.dropout(x, y, drop)                                    # and the library goes on working
     torch.cuda.synchronize()
+
+
+# (rows, vocabulary): a wave a row; rows held by a block; rows in two passes; few long rows shared by blocks
+PATHS = [(9, 100), (140, 9001), (3, 300001), (2, 600011)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n, vocab", PATHS)
+def test_rows_of_nan_are_not_taken_for_empty(n, vocab, t):
+    """A row of NaN, or of NaN among -inf, has no largest value either, but it is no masked row."""
+    import paper_2605_01989_amd as dblp
+    g, t = gen(21), TYPES[t]
+    x = torch.randn(n, vocab, generator=g, device="cuda").to(t)
+    x[0] = float("nan")
+    x[1] = -float("inf")
+    x[1, vocab // 3] = float("nan")
+    target, w = torch.full((n,), 2, device="cuda"), torch.ones(n, device="cuda")
+    ws = torch.empty(dblp.logits_workspace(n, vocab), dtype=torch.uint8, device="cuda")
+    logp, lse = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    dblp.token_logprobs(x, target, logp, ws, lse=lse)
+    assert bool(torch.isnan(lse[:2]).all()) and bool(torch.isnan(logp[:2]).all()) and bool(torch.isfinite(lse[2:]).all())
+    stats, d = torch.zeros(5, device="cuda"), torch.zeros_like(x)
+    for grad in (d, None):
+        logp.zero_()
+        dblp.policy_loss(x, target, w, w, stats, ws, old_logp=torch.zeros_like(w), dlogits=grad, logp=logp)
+        assert bool(torch.isnan(logp[:2]).all()) and bool(torch.isnan(stats[0])) and float(stats[4]) == n
+    assert bool(torch.isnan(d[:2]).all()) and bool(torch.isfinite(d[2:]).all())
+
+
+@pytest.mark.parametrize("n, vocab", PATHS)
+def test_ratios_and_references_that_overflow(n, vocab):
+    """exp(lp - old) and exp(ref - lp) past the largest fp32 number: an advantage of zero still gives zero, a coefficient of zero takes the KL
+    term out of loss and gradient (the sum of the KL itself is infinite)."""
+    import paper_2605_01989_amd as dblp
+    g = gen(22)
+    x = torch.randn(n, vocab, generator=g, device="cuda")
+    target, w = torch.randint(0, vocab, (n,), generator=g, device="cuda"), torch.ones(n, device="cuda")
+    ws = torch.empty(dblp.logits_workspace(n, vocab), dtype=torch.uint8, device="cuda")
+    lp, stats, d, want = torch.empty(n, device="cuda"), torch.empty(5, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    dblp.token_logprobs(x, target, lp, ws)
+    for grad in (d, None):
+        dblp.policy_loss(x, target, torch.zeros(n, device="cuda"), w, stats, ws, old_logp=lp - 200, dlogits=grad)
+        assert stats[:4].tolist() == [0, 0, 0, 0]
+    assert bool((d == 0).all())
+    dblp.policy_loss(x, target, w, w, stats, ws, dlogits=want)
+    loss = float(stats[0])
+    for grad in (d, None):
+        dblp.policy_loss(x, target, w, w, stats, ws, ref_logp=lp + 200, kl_coef=0.0, dlogits=grad)
+        assert float(stats[0]) == float(stats[1]) == loss and float(stats[2]) == float("inf")
+    assert torch.equal(d, want)
+    # above the border a positive advantage is clipped, however large the ratio
+    dblp.policy_loss(x, target, w, w, stats, ws, old_logp=lp - 200, dlogits=d, clip=(0.2, 0.5))
+    assert abs(float(stats[0]) + 1.5 * n) <= 4 * U * 1.5 * n and float(stats[3]) == n and bool((d == 0).all())
