@@ -10,7 +10,7 @@
  *
  * The protocol sends a lost packet again byte for byte, so a worker that computes its step again must
  * find the same gradient: every result here is a function of the arguments alone.  There are no
- * floating-point atomics, a gradient row is summed in the order of its tokens, and a dropout mask is
+ * floating-point atomics, a gradient row's sum is grouped by the tokens alone, and a dropout mask is
  * computed from (seed, draw, place) wherever it is needed and never stored.
  *
  * Conventions (those of dblp_agg.h, without a context)
@@ -29,7 +29,8 @@
  *   - A token, position or target outside its table (negative, or not below the number of rows) is "none":
  *     its row of the table is taken as zero, it has no gradient, it is not counted in a loss.  This is
  *     how padding and prompts are marked; nothing is read out of bounds.
- *   - Zero tokens or rows are allowed.  Limits: tokens, rows and vocabulary below 2^31, columns below 2^31.
+ *   - Zero tokens or rows are allowed.  Limits: tokens, rows, vocabulary and columns below 2^31, columns of
+ *     dblp_embed_grad below 2^22.
  *   - A workspace is DEVICE memory of the size that dblp_*_workspace gives, 256-byte aligned, of any
  *     contents; it is free again when the stream has passed the call.
  */
@@ -70,8 +71,8 @@ int dblp_embed(int device, void* stream, const int64_t* d_tokens, uint64_t n_tok
                const int64_t* d_positions, const void* d_pos_table, uint64_t pos_stride, uint64_t n_positions,
                const dblp_drop* h_drop, void* d_out, uint64_t out_stride, int out_type);
 
-/* grad[v] = base[v] + scale * sum of drop(dy[t]) over all t with tokens[t] = v, ascending in t, for every v
- * below vocab.  grad is fp32, what a packet carries.  d_base NULL: zeros; d_base == d_grad (and equal strides):
+/* grad[v] = base[v] + scale * sum of drop(dy[t]) over all t with tokens[t] = v, for every v below vocab; the
+ * terms are added in ascending t within groups that n_tokens and the tokens fix.  grad is fp32, what a packet carries.  d_base NULL: zeros; d_base == d_grad (and equal strides):
  * in place, only rows that have a token are touched (a tied table's other gradient, or an earlier micro-batch);
  * another fp32 matrix: every row is written.  The position table's gradient is the same call on the positions.
  * h_drop: the mask of the forward pass. */

@@ -508,6 +508,19 @@ static Shares shares_of(u64 n, u32 vecs) {
     return {k, (vecs + k - 1) / k};
 }
 
+// Calls f(first row, rows) for launches of a block of NT threads a row: a grid has fewer than 2^32 threads.
+template <int NT, class F>
+static void each_rows(u64 rows, F f) {
+    constexpr u64 most = COUNT_LIMIT / NT;
+    for (u64 row0 = 0; row0 < rows; row0 += most) f(row0, (u32)(rows - row0 < most ? rows - row0 : most));
+}
+static Policy rows_from(Policy p, u64 row0) {
+    p.targets += row0; p.advantages += row0; p.weights += row0;
+    if (p.old_logp) p.old_logp += row0;
+    if (p.ref_logp) p.ref_logp += row0;
+    return p;
+}
+
 extern "C" uint64_t dblp_logits_workspace(uint64_t n_tokens, uint32_t vocab) {
     if (n_tokens >= COUNT_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT) return 0;
     return logits_plan(n_tokens).bytes;
@@ -530,7 +543,10 @@ extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, 
         typedef decltype(tt) T;
         const auto go = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
-            hipLaunchKernelGGL(far ? (logprob_rows<T, NT, true>) : (logprob_rows<T, NT, false>), dim3((u32)n_tokens), dim3(NT), 0, (hipStream_t)stream, (const typename T::elem*)d_logits, (u64)logits_stride, vocab, d_targets, d_logp, d_lse);
+            each_rows<NT>(n_tokens, [&](u64 row0, u32 rows) {
+                hipLaunchKernelGGL(far ? (logprob_rows<T, NT, true>) : (logprob_rows<T, NT, false>), dim3(rows), dim3(NT), 0, (hipStream_t)stream, (const typename T::elem*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
+                                   d_targets + row0, d_logp + row0, d_lse ? d_lse + row0 : nullptr);
+            });
         };
         const u32 vecs = vocab / Wide<T>::W;
         // rows that one CU reads for longer than a launch more takes, on the host too: one row of 200000 floats 12 us by a block, 5 shared; of 50257 16-bit values 6, 5
@@ -586,11 +602,17 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
             constexpr u32 W = Wide<T>::W;
             const auto twice = [&](auto nt) {
                 constexpr int NT = decltype(nt)::value;
-                hipLaunchKernelGGL((policy_twice<T, NT>), dim3(n), dim3(NT), 0, st, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, d_logp, parts, own_stats);
+                each_rows<NT>(n, [&](u64 row0, u32 rows) {
+                    hipLaunchKernelGGL((policy_twice<T, NT>), dim3(rows), dim3(NT), 0, st, rows_from(p, row0), (const E*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
+                                       d_dlogits ? (E*)d_dlogits + row0 * dlogits_stride : nullptr, (u64)dlogits_stride, d_logp ? d_logp + row0 : nullptr, parts + row0, own_stats);
+                });
             };
             const auto held = [&](auto nt, auto nv) {
                 constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-                hipLaunchKernelGGL(far ? (policy_held<T, NT, NV, true>) : (policy_held<T, NT, NV, false>), dim3(n), dim3(NT), 0, st, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, d_logp, parts, own_stats);
+                each_rows<NT>(n, [&](u64 row0, u32 rows) {
+                    hipLaunchKernelGGL(far ? (policy_held<T, NT, NV, true>) : (policy_held<T, NT, NV, false>), dim3(rows), dim3(NT), 0, st, rows_from(p, row0), (const E*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
+                                       (E*)d_dlogits + row0 * dlogits_stride, (u64)dlogits_stride, d_logp ? d_logp + row0 : nullptr, parts + row0, own_stats);
+                });
             };
             const u32 vecs = vocab / W;
             // (one token's row, if registers hold it, needs one launch where sharing needs two)

@@ -173,6 +173,7 @@ __global__ __launch_bounds__(256) void fill_rows(Units s, Result out) { fill_blo
 // a token's first place adds up the rows of all its places, a quarter of the places a wave, and the others end.  The launch's other blocks write the rows that have no
 // token, each block with a list of which of its rows have one.  (Sorting takes three launches, 17 us for 500 tokens of 768 columns; this one 8.)
 #define GRAD_SHORT 512
+#define GRAD_DIM_LIMIT (1u << 22)                // so that a block for each place and 256 columns is a grid of fewer than 2^32 threads
 #define SHORT_FILL 4                             // units that a thread of a filling block writes
 
 template <class T, bool DROP, bool WHOLE>
@@ -684,7 +685,7 @@ static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
 }
 
 extern "C" uint64_t dblp_embed_grad_workspace(uint64_t n_tokens, uint64_t vocab, uint32_t dim) {
-    if (n_tokens >= COUNT_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT || dim == 0 || dim >= COUNT_LIMIT) return 0;
+    if (n_tokens >= COUNT_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT || dim == 0 || dim >= GRAD_DIM_LIMIT) return 0;
     return grad_plan(n_tokens, vocab, dim).bytes;
 }
 
@@ -715,7 +716,7 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
                                void* d_workspace, uint64_t workspace_bytes) {
     const char* call = "embed_grad";
     REFUSE_IF(bad_type(dy_type), "unknown type");
-    REFUSE_IF(dim == 0 || dim >= COUNT_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT || n_tokens >= COUNT_LIMIT, "size out of range");
+    REFUSE_IF(dim == 0 || dim >= GRAD_DIM_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT || n_tokens >= COUNT_LIMIT, "size out of range");
     REFUSE_IF(!d_grad || (n_tokens && (!d_tokens || !d_dy)), "null pointer");
     REFUSE_IF(off(d_tokens, 8) || off(d_dy, type_bytes(dy_type)) || off(d_base, 4) || off(d_grad, 4), "misaligned pointer");
     REFUSE_IF(vocab > 1 && grad_stride < dim, "the gradient's rows overlap");

@@ -22,8 +22,10 @@ class Drop(ctypes.Structure):
     _fields_ = [("seed", ctypes.c_uint64), ("draw", ctypes.c_uint64), ("d_draw", ctypes.c_void_p), ("p", ctypes.c_double)]
 
     def __init__(self, seed, draw, p, d_draw=None):
+        if d_draw is not None and not (d_draw.is_cuda and d_draw.numel() == 1 and d_draw.element_size() == 8 and not d_draw.is_floating_point()):
+            _bad("d_draw: must be one 64-bit integer on the GPU")
         super().__init__(seed, draw, None if d_draw is None else d_draw.data_ptr(), p)
-        self._keep = d_draw
+        self._draw = d_draw                      # kept alive with the mask
 
 
 _lib = None
@@ -87,6 +89,19 @@ def _vector(name, t, dev, n, dtype):
     return t.data_ptr()
 
 
+def _mask(drop, dev):
+    if drop is not None and (type(drop) is not Drop or (drop._draw is not None and drop._draw.device != dev)):
+        _bad(f"drop: must be a Drop, its d_draw on {dev}")
+    return drop
+
+
+def _shape(name, t):
+    """(rows, columns), device."""
+    if t.ndim != 2:
+        _bad(f"{name}: shape {tuple(t.shape)}, not that of a matrix")
+    return t.shape, t.device
+
+
 def _space(t, dev):
     if t.device != dev or not t.is_contiguous():
         _bad(f"workspace: must be contiguous and on {dev}")
@@ -105,7 +120,7 @@ def _place(dev, stream):
 def embed(tokens, table, out, scale=1.0, positions=None, pos_table=None, drop=None, stream=None):
     """out[t] = drop(scale * table[tokens[t]] + pos_table[positions[t]])."""
     L = _lib or _load()
-    n, dim, dev = tokens.numel(), table.shape[-1], tokens.device
+    n, ((_, dim), dev) = tokens.numel(), _shape("table", table)
     index, stream = _place(dev, stream)
     p, p_stride = _matrix("table", table, dev, None, dim)
     o, o_stride = _matrix("out", out, dev, n, dim)
@@ -114,7 +129,7 @@ def embed(tokens, table, out, scale=1.0, positions=None, pos_table=None, drop=No
         q, q_stride = _matrix("pos_table", pos_table, dev, None, dim, table.dtype)
         n_pos = pos_table.shape[0]
     _check(L.dblp_embed(index, stream, _vector("tokens", tokens, dev, n, _torch.int64), n, dim, p, p_stride, table.shape[0], _types[table.dtype],
-                        scale, _vector("positions", positions, dev, n, _torch.int64), q, q_stride, n_pos, drop, o, o_stride, _types[out.dtype]))
+                        scale, _vector("positions", positions, dev, n, _torch.int64), q, q_stride, n_pos, _mask(drop, dev), o, o_stride, _types[out.dtype]))
 
 
 def embed_grad_workspace(n_tokens, vocab, dim) -> int:
@@ -125,24 +140,24 @@ def embed_grad_workspace(n_tokens, vocab, dim) -> int:
 def embed_grad(tokens, dy, grad, workspace, scale=1.0, drop=None, base=None, stream=None):
     """grad[v] = base[v] + scale * sum of drop(dy[t]) over the tokens that are v; base None: zeros, base grad: in place."""
     L = _lib or _load()
-    n, (vocab, dim), dev = tokens.numel(), grad.shape, grad.device
+    n, ((vocab, dim), dev) = tokens.numel(), _shape("grad", grad)
     index, stream = _place(dev, stream)
     g, g_stride = _matrix("grad", grad, dev, None, dim, _torch.float32)
     d, d_stride = _matrix("dy", dy, dev, n, dim)
     b, b_stride = (None, 0) if base is None else _matrix("base", base, dev, vocab, dim, _torch.float32)
-    _check(L.dblp_embed_grad(index, stream, _vector("tokens", tokens, dev, n, _torch.int64), n, dim, vocab, scale, drop, d, d_stride, _types[dy.dtype],
+    _check(L.dblp_embed_grad(index, stream, _vector("tokens", tokens, dev, n, _torch.int64), n, dim, vocab, scale, _mask(drop, dev), d, d_stride, _types[dy.dtype],
                              b, b_stride, g, g_stride, *_space(workspace, dev)))
 
 
 def dropout(x, y, drop, residual=None, stream=None):
     """y = drop(x) + residual; on y's gradient, without a residual, it is the gradient of x."""
     L = _lib or _load()
-    (rows, cols), dev = x.shape, x.device
+    (rows, cols), dev = _shape("x", x)
     index, stream = _place(dev, stream)
     a, a_stride = _matrix("x", x, dev, rows, cols)
     o, o_stride = _matrix("y", y, dev, rows, cols, x.dtype)
     r, r_stride = (None, 0) if residual is None else _matrix("residual", residual, dev, rows, cols, x.dtype)
-    _check(L.dblp_dropout(index, stream, rows, cols, a, a_stride, r, r_stride, drop, o, o_stride, _types[x.dtype]))
+    _check(L.dblp_dropout(index, stream, rows, cols, a, a_stride, r, r_stride, _mask(drop, dev), o, o_stride, _types[x.dtype]))
 
 
 def logits_workspace(n_tokens, vocab) -> int:
@@ -153,7 +168,7 @@ def logits_workspace(n_tokens, vocab) -> int:
 def token_logprobs(logits, targets, logp, workspace, lse=None, stream=None):
     """logp[t] = logits[t, targets[t]] - lse[t]; 0 where the target is none."""
     L = _lib or _load()
-    (n, vocab), dev, f32 = logits.shape, logits.device, _torch.float32
+    ((n, vocab), dev), f32 = _shape("logits", logits), _torch.float32
     index, stream = _place(dev, stream)
     x, x_stride = _matrix("logits", logits, dev, n, vocab)
     _check(L.dblp_token_logprobs(index, stream, n, vocab, x, x_stride, _types[logits.dtype], _vector("targets", targets, dev, n, _torch.int64),
@@ -164,7 +179,7 @@ def policy_loss(logits, targets, advantages, weights, stats, workspace, old_logp
                 clip=(0.2, 0.2), kl_coef=0.0, grad_scale=1.0, stream=None):
     """stats = loss, its policy and KL sums, tokens clipped and counted; dlogits = grad_scale * d loss / d logits (in place: dlogits=logits)."""
     L = _lib or _load()
-    (n, vocab), dev, f32 = logits.shape, logits.device, _torch.float32
+    ((n, vocab), dev), f32 = _shape("logits", logits), _torch.float32
     index, stream = _place(dev, stream)
     x, x_stride = _matrix("logits", logits, dev, n, vocab)
     d, d_stride = (None, 0) if dlogits is None else _matrix("dlogits", dlogits, dev, n, vocab, logits.dtype)

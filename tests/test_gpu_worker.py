@@ -584,3 +584,30 @@ def test_ratios_and_references_that_overflow(n, vocab):
     # above the border a positive advantage is clipped, however large the ratio
     dblp.policy_loss(x, target, w, w, stats, ws, old_logp=lp - 200, dlogits=d, clip=(0.2, 0.5))
     assert abs(float(stats[0]) + 1.5 * n) <= 4 * U * 1.5 * n and float(stats[3]) == n and bool((d == 0).all())
+
+
+def test_more_rows_than_one_launch_takes():
+    """2^26 + 77 rows, a wave each, are more threads than a grid has: the last rows' results are those of a call on them alone."""
+    import paper_2605_01989_amd as dblp
+    g, n, vocab, tail = gen(23), 2**26 + 77, 5, 2**13
+    x = torch.empty(n, vocab, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    target = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    adv, w = torch.empty(n, device="cuda").normal_(generator=g), torch.ones(n, device="cuda")
+    ws = torch.empty(dblp.logits_workspace(n, vocab), dtype=torch.uint8, device="cuda")
+    for first in (0, 2**25 - 5, n - tail):
+        part = slice(first, first + tail)
+        lp, lse = torch.empty(tail, device="cuda"), torch.empty(tail, device="cuda")
+        dblp.token_logprobs(x[part], target[part], lp, ws, lse=lse)
+        d, stats = torch.empty(tail, vocab, dtype=torch.bfloat16, device="cuda"), torch.empty(5, device="cuda")
+        dblp.policy_loss(x[part], target[part], adv[part], w[part], stats, ws, old_logp=lse, dlogits=d)
+        if first == 0:
+            logp, lses = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+            dblp.token_logprobs(x, target, logp, ws, lse=lses)
+            grad, total = torch.empty_like(x), torch.empty(5, device="cuda")
+            dblp.policy_loss(x, target, adv, w, total, ws, old_logp=lses, dlogits=grad)
+            assert float(total[4]) == float(torch.tensor(float(n)))          # (one fp32 number)
+            only = torch.empty(5, device="cuda")
+            dblp.policy_loss(x, target, adv, w, only, ws, old_logp=lses)
+        assert torch.equal(logp[part], lp) and torch.equal(lses[part], lse) and torch.equal(grad[part], d)
+    # without the gradient the sums are those of the same tokens: each within lse's error of the other, times its ratio
+    assert float(only[4]) == float(total[4]) and abs(float(only[0] - total[0])) <= 1e-5 * n

@@ -131,3 +131,34 @@ def test_binding_refuses_what_the_library_cannot_see():
         with pytest.raises(dblp.DblpError):
             worker._vector("v", bad, meta.device, 4, torch.float32)
     assert ctypes.sizeof(worker.Drop) == 32
+
+
+def test_the_gradient_of_very_wide_rows_is_refused():
+    worker._load()
+    assert dblp.embed_grad_workspace(1, 1, 1 << 22) == 0 and dblp.embed_grad_workspace(1, 1, (1 << 22) - 1) > 0
+    assert _grad(dim=1 << 22, gstride=1 << 22) == binding.EINVAL
+
+
+def test_binding_refuses_draw_counters_and_masks_that_the_gpu_cannot_read():
+    for bad in (torch.zeros(1, dtype=torch.int64), torch.zeros(1, dtype=torch.int64, device="meta"), torch.zeros(1)):
+        with pytest.raises(dblp.DblpError) as e:
+            dblp.Drop(1, 2, 0.5, bad)
+        assert e.value.code == binding.EINVAL
+    meta = torch.device("meta")
+    for bad in (0.5, (1, 2, 0.5)):
+        with pytest.raises(dblp.DblpError):
+            worker._mask(bad, meta)
+    drop = dblp.Drop(1, 2, 0.5)
+    assert worker._mask(None, meta) is None and worker._mask(drop, meta) is drop
+    drop._draw = torch.zeros(1, dtype=torch.int64)                           # on another device than the call's tensors
+    with pytest.raises(dblp.DblpError):
+        worker._mask(drop, meta)
+
+
+def test_binding_refuses_what_is_no_matrix():
+    v, t = torch.zeros(8), torch.zeros(8, dtype=torch.int64)
+    for f in (lambda: dblp.embed(t, v, v), lambda: dblp.embed_grad(t, v, v, v), lambda: dblp.dropout(v, v, dblp.Drop(1, 2, 0.5)),
+              lambda: dblp.token_logprobs(v, t, v, v), lambda: dblp.policy_loss(torch.tensor(0.0), t, v, v, v, v)):
+        with pytest.raises(dblp.DblpError) as e:
+            f()
+        assert e.value.code == binding.EINVAL
