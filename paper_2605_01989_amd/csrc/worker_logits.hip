@@ -257,7 +257,9 @@ __device__ __forceinline__ void skip_row(typename T::elem* drow, u32 vocab, u32 
     if (threadIdx.x < singles) drow[threadIdx.x < head ? threadIdx.x : threadIdx.x + vecs * W] = (typename T::elem)0.0f;
 }
 
-#define HELD_WAVES __attribute__((amdgpu_waves_per_eu(4)))        // registers for two rows of 512 threads a CU
+// Registers for two rows of 512 threads a CU, or one of 1024: 22 vectors a thread fit without spilling (152 k and 178 k 16-bit values at 92 % of a large copy's rate, which two
+// passes reach 68 % of).  Three rows a CU, with a few registers spilled, are slower: 8192 rows of 50257 16-bit values 292 us, 277 with two.
+#define HELD_WAVES __attribute__((amdgpu_waves_per_eu(4)))
 // A block takes a row and holds it: NV vectors a thread, all on their way at once.  A wave's vectors follow each other.  Where the gradient's row begins at another
 // multiple of two than the logits', a vector is stored one place on, with the first value of the next one (of the next lane, or of the wave's next vector's first lane); the
 // first value of a wave and the last vector of a wave or of the row are stored value by value.
@@ -558,9 +560,12 @@ extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, 
             hipLaunchKernelGGL(logprob_join, dim3((u32)n_tokens), dim3(64), 0, (hipStream_t)stream, q, vocab, d_targets, (const Soft*)softs, (const float*)chosen, d_logp, d_lse);
             return;
         }
-        // a wave for a row that it reads in one step; many threads where there are few rows
-        if (vocab <= 64 * Wide<T>::W * STREAM) go(Int<64>());
-        else if (n_tokens <= 512 && vocab > 512 * Wide<T>::W * STREAM) go(Int<1024>());
+        // Threads that end with their row: each has at most six vectors of it, in two steps.  A batch of 160 MB of 2500 16-bit values takes 32 us by 64 threads a row, 38 by 128,
+        // 124 by 512; of 7539 33, 31 and 50 (29 by 256); of 12000 32, 32, 33 (30 by 256); of 16000 35, 34, 28 (33 by 256).  Between one and three rows a CU, long rows
+        // are read by 256 threads too: 400 of 50257 10 us, 11 by 512; 520 of them 13, 15; 520 of 128256 28, 32; but 130 of 128256 15, 10.
+        if (vecs <= 64 * 6) go(Int<64>());
+        else if (vecs <= 128 * 6) go(Int<128>());
+        else if (vecs <= 256 * 6 || (n_tokens >= 256 && n_tokens < 768)) go(Int<256>());
         else go(Int<512>());
     });
     return launched(call);
@@ -631,6 +636,7 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
             else if (vocab <= 512 * 14 * W) held(Int<512>(), Int<14>());
             else if (vocab <= 1024 * 14 * W) held(Int<1024>(), Int<14>());
             else if (vocab <= 1024 * 18 * W) held(Int<1024>(), Int<18>());
+            else if (vocab <= 1024 * 22 * W) held(Int<1024>(), Int<22>());
             else twice(Int<1024>());
         });
     if (n != 1 && !summed) {

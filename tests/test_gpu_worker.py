@@ -611,3 +611,29 @@ def test_more_rows_than_one_launch_takes():
         assert torch.equal(logp[part], lp) and torch.equal(lses[part], lse) and torch.equal(grad[part], d)
     # without the gradient the sums are those of the same tokens: each within lse's error of the other, times its ratio
     assert float(only[4]) == float(total[4]) and abs(float(only[0] - total[0])) <= 1e-5 * n
+
+
+# vocabularies at the borders between the numbers of threads and of held vectors, by value size
+BORDERS = [64 * 6 * 4, 64 * 6 * 8 + 1, 128 * 6 * 4 + 9, 128 * 6 * 8, 256 * 6 * 4 + 1, 256 * 6 * 8 + 8, 1024 * 18 * 4 + 3, 1024 * 22 * 4, 1024 * 22 * 4 + 1, 1024 * 18 * 8 + 1, 151937, 1024 * 22 * 8, 1024 * 22 * 8 + 1]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("vocab", BORDERS)
+def test_logits_at_the_borders_between_variants(vocab, t):
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    for n in (130, 257) if vocab < 20000 else (130,):
+        g = gen(vocab + n)
+        _, x, target = make_logits(g, n, vocab, 1, 1, t)
+        target, adv, w, old, back = policy_inputs(g, x, target, 0.3)
+        ws = torch.full((dblp.logits_workspace(n, vocab),), 0xA5, dtype=torch.uint8, device="cuda")
+        logp, lse, stats = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(5, device="cuda")
+        dblp.token_logprobs(x, target, logp, ws, lse=lse)
+        lp, l = ref.logprobs(x, target)
+        off = ((target < 0) | (target >= vocab)).cpu()
+        close(lse, torch.where(off, 0.0, l), lse_error(x), torch.float32)
+        close(logp, torch.where(off, 0.0, lp), lse_error(x), torch.float32)
+        buf, d = matrix(g, n, vocab, t, vocab + 2, 0, fill=4.0)
+        dblp.policy_loss(x, target, adv, w, stats, ws, dlogits=d, logp=logp, old_logp=old, ref_logp=back, clip=(0.2, 0.3), kl_coef=0.1)
+        check_policy((stats, logp, d), ref.policy(x, target, adv, w, old, back, (0.2, 0.3), 0.1, 1.0), x, t, 1.0)
+        assert untouched(buf, d)
