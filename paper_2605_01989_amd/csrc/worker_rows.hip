@@ -542,6 +542,7 @@ __global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys,
                 if (k[j] == none) continue;
                 float x[4];
                 if (DROP) V::shut(v[j], gate[j - j0]);
+                else if constexpr (sizeof(typename T::elem) == 2) asm volatile("" : "+v"(v[j]));        // not converted before its turn: the eight rows' floats took 170 registers, and 65536 x 1024 without dropout 176 us
                 V::open(v[j], x);
                 for (int e = 0; e < 4; ++e) sum[e] += DROP ? x[e] * m.keep : x[e];
                 if (k[j + 1] == k[j]) continue;
