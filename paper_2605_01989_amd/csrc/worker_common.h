@@ -125,15 +125,20 @@ struct Vec<T, 4> {
     static __device__ __forceinline__ raw pack(const float (&v)[4]) { return __builtin_bit_cast(raw, __builtin_convertvector(((f4v){v[0], v[1], v[2], v[3]}), half4)); }
 };
 
-// Columns [c, c + W) of a row of `cols`, c < cols; those past the end read as zero.  WHOLE: there are none.  Otherwise a row's last
-// columns are read from its last W elements and shifted down in registers: one load for every thread, without a branch that would have
-// to wait for it (rows of fewer than W elements apart).  FAR: with the hint that the data are not used again soon.
+// Columns [c, c + W) of a row of `cols`, c < cols; those past the end are zero.  WHOLE: there are none.  Otherwise a row's last
+// columns are read from its last W elements and shifted down in registers (rows of fewer than W elements apart): one load for every thread.
+// The shift is a call of its own, for when all loads have been asked for: made with the load it would wait for each of them (embed_grad of
+// 17000 tokens of 333 columns).  FAR: with the hint that the data are not used again soon.
 template <class V, int W, bool WHOLE, bool FAR = false>
 __device__ __forceinline__ typename V::raw load_cols(const typename V::elem* row, u32 c, u32 cols) {
     if (WHOLE) return FAR ? V::load_far(row + c) : V::load(row + c);
     if (cols < W) return V::some(row, cols);
     const u32 at = c + W <= cols ? c : cols - W;
-    return V::down(FAR ? V::load_far(row + at) : V::load(row + at), c - at);
+    return FAR ? V::load_far(row + at) : V::load(row + at);
+}
+template <class V, int W, bool WHOLE>
+__device__ __forceinline__ typename V::raw settle_cols(typename V::raw r, u32 c, u32 cols) {
+    return WHOLE || cols < W ? r : V::down(r, c + W <= cols ? 0 : c + W - cols);
 }
 // ... and those past the end are not written.
 template <class V, int W, bool FAR = false>

@@ -55,11 +55,12 @@ __global__ __launch_bounds__(256) void dropout_units(Units s, Mask m, const type
     for (int j = 0; j < N; ++j) {
         if (!mine[j]) continue;
         float v[W], w[W];
+        a[j] = settle_cols<V, W, WHOLE>(a[j], c[j], s.cols);
         V::shut(a[j], gate[j]);
         V::open(a[j], v);
         for (int k = 0; k < W; ++k) v[k] *= m.keep;
         if (RES) {
-            V::open(b[j], w);
+            V::open(settle_cols<V, W, WHOLE>(b[j], c[j], s.cols), w);
             for (int k = 0; k < W; ++k) v[k] += w[k];
         }
         store_cols<V, W, FAR>(y + row[j] * y_stride, c[j], s.cols, v);
@@ -98,11 +99,11 @@ __global__ __launch_bounds__(256) void embed_units(Units s, Mask m, const int64_
         if (!mine[j]) continue;
         float v[W] = {}, w[W];
         if (tok[j] < vocab) {                        // (a select, not a product with zero: scale may be infinite)
-            VS::open(a[j], v);
+            VS::open(settle_cols<VS, W, WHOLE>(a[j], c[j], s.cols), v);
             for (int k = 0; k < W; ++k) v[k] *= scale;
         }
         if (at[j] < n_pos) {
-            VS::open(b[j], w);
+            VS::open(settle_cols<VS, W, WHOLE>(b[j], c[j], s.cols), w);
             for (int k = 0; k < W; ++k) v[k] += w[k];
         }
         if (DROP) {
@@ -155,6 +156,10 @@ __device__ __forceinline__ void fill_block(const Result& out, const Units& s, u3
             const float* row = out.base + (s.row0 + r[k]) * out.base_stride;
             v[k] = out.far ? load_cols<G4, 4, true, true>(row, c[k], s.cols) : load_cols<G4, 4, false>(row, c[k], s.cols);
         }
+        if (!out.far) {
+#pragma unroll
+            for (int k = 0; k < FILL_EACH; ++k) if (mine[k]) v[k] = settle_cols<G4, 4, false>(v[k], c[k], s.cols);
+        }
     }
 #pragma unroll
     for (int k = 0; k < FILL_EACH; ++k) {
@@ -203,6 +208,7 @@ __global__ __launch_bounds__(256) void grad_short(const int64_t* __restrict__ to
         for (int k = 0; k < SHORT_FILL; ++k) {
             const u32 i = i0 + k * 256 + tid, r = rows.per_row.of(i), c = (i - r * units) * 4;
             if (i >= i1 || c >= cols || taken[r - r0]) continue;
+            if (out.base) v[k] = settle_cols<G4, 4, WHOLE>(v[k], c, cols);
             const float y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
             store_cols<G4, 4>(out.grad + (rows.row0 + r) * out.grad_stride, c, cols, y);
         }
@@ -254,6 +260,7 @@ __global__ __launch_bounds__(256) void grad_short(const int64_t* __restrict__ to
                 for (int h = q; h < q + 2; ++h) {
                     float x[4];
                     if (!there[h]) continue;
+                    if (here) v[h] = settle_cols<V, 4, WHOLE>(v[h], c, cols);
                     if (DROP) V::shut(v[h], gate[h]);
                     V::open(v[h], x);
                     for (int e = 0; e < 4; ++e) sum[e] += DROP ? x[e] * m.keep : x[e];
@@ -265,6 +272,7 @@ __global__ __launch_bounds__(256) void grad_short(const int64_t* __restrict__ to
     __syncthreads();
     if (w || !here) return;
     const f4v all = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    if (out.base) base = settle_cols<G4, 4, WHOLE>(base, c, cols);
     float y[4];
     for (int e = 0; e < 4; ++e) y[e] = base[e] + out.scale * all[e];
     store_cols<G4, 4>(out.grad + tok * out.grad_stride, c, cols, y);
@@ -324,9 +332,9 @@ __device__ __forceinline__ void pad_lists(u32* keys, u32* places, u32 n, u64 voc
     }
 }
 
-// All places of a short batch by one block, keys and places in LDS between the passes; the launch's other blocks write rows of the result
-// meanwhile (those that have a token are written again later, they are few next to the table).  `present`: marks of the rows that have a token, or null.
-#define SORT_BLOCK_ROWS 16
+// All places of a short batch by one block, keys and places in LDS between the passes (8192 places 22 us, as long as four launches of tiles take; 16000 39);
+// the launch's other blocks write rows of the result meanwhile (those that have a token are written again later, they are few next to the table).  `present`: marks of the rows that have a token, or null.
+#define SORT_BLOCK_ROWS 8
 #define SORT_BLOCK_MOST (1024 * SORT_BLOCK_ROWS)
 struct SortLds { u32 keys[SORT_BLOCK_MOST]; u16 places[SORT_BLOCK_MOST]; u32 counts[16][BINS]; u32 part[16]; };
 
@@ -434,11 +442,15 @@ __global__ __launch_bounds__(256) void sort_move(SortShape q, SortFrom from, u32
     if (blockIdx.x == 0) pad_lists(keys_to, places_to, q.n, q.vocab);
     const u32 mask = (1u << q.bits) - 1, lo = blockIdx.x * tile, hi = q.n - lo < tile ? q.n : lo + tile;
     u32 total[2] = {0, 0}, mine[2] = {0, 0};
-#pragma unroll 32
-    for (u32 t = 0; t < tiles; ++t) {
-        const uint2 c = *(const uint2*)(hist + t * BINS + 2 * tid);
-        if (t < blockIdx.x) { mine[0] += c.x; mine[1] += c.y; }
-        total[0] += c.x; total[1] += c.y;
+    for (u32 t0 = 0; t0 < tiles; t0 += 16) {               // sixteen tiles' counts in flight, also where there are fewer
+        uint2 c[16];
+#pragma unroll
+        for (u32 j = 0; j < 16; ++j) c[j] = *(const uint2*)(hist + (t0 + j < tiles ? t0 + j : tiles - 1) * BINS + 2 * tid);
+#pragma unroll
+        for (u32 j = 0; j < 16; ++j) {
+            if (t0 + j < blockIdx.x) { mine[0] += c[j].x; mine[1] += c[j].y; }
+            if (t0 + j < tiles) { total[0] += c[j].x; total[1] += c[j].y; }
+        }
     }
     const u32 before = scan_block<256>(total[0] + total[1], part);
     next[2 * tid] = before + mine[0];
@@ -541,6 +553,7 @@ __global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys,
             for (int j = j0; j < j0 + 2; ++j) {
                 if (k[j] == none) continue;
                 float x[4];
+                if (here) v[j] = settle_cols<V, 4, WHOLE>(v[j], c, s.cols);
                 if (DROP) V::shut(v[j], gate[j - j0]);
                 else if constexpr (sizeof(typename T::elem) == 2) asm volatile("" : "+v"(v[j]));        // not converted before its turn: the eight rows' floats took 170 registers, and 65536 x 1024 without dropout 176 us
                 V::open(v[j], x);
@@ -553,6 +566,7 @@ __global__ __launch_bounds__(256) void grad_pieces(const u32* __restrict__ keys,
                     if (unit == 0) chains[atomicAdd(n_chains, 1u)] = make_uint2(piece, k1);        // in any order: the chains have nothing to do with each other
                 } else if (here) {
                     float y[4];
+                    if (BASE) base[j] = settle_cols<G4, 4, WHOLE>(base[j], c, s.cols);
                     for (int e = 0; e < 4; ++e) y[e] = (BASE ? base[j][e] : 0.0f) + out.scale * sum[e];
                     store_cols<G4, 4>(out.grad + (u64)k[j] * out.grad_stride, c, s.cols, y);
                 }
@@ -604,6 +618,7 @@ __global__ __launch_bounds__(256) void grad_chains(const u32* __restrict__ keys,
         }
         if (lead) {
             const f4v all = sh[0][ul];
+            if (out.base) base = settle_cols<G4, 4, false>(base, unit * 4, cols);
             float y[4];
             for (int e = 0; e < 4; ++e) y[e] = base[e] + out.scale * all[e];
             store_cols<G4, 4>(out.grad + (u64)k * out.grad_stride, unit * 4, cols, y);
@@ -669,7 +684,7 @@ static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
     while ((vocab >> bits) != 0) ++bits;                 // keys run to vocab itself
     p.passes = (bits + 8) / 9;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.len = n <= SORT_BLOCK_MOST ? 8 : 16;               // few places: enough threads; many: fewer chains (65536 x 1024: 12 us of chains, 18 with 8)
+    p.len = n <= 16384 ? 8 : 16;               // few places: enough threads; many: fewer chains (65536 x 1024: 12 us of chains, 18 with 8)
     p.pieces = (u32)((n + p.len - 1) / p.len);
     p.tile = (u32)round_up((n + SORT_TILES - 1) / SORT_TILES, SORT_STEP);
     p.tiles = (u32)((n + p.tile - 1) / p.tile);
@@ -692,7 +707,8 @@ extern "C" uint64_t dblp_embed_grad_workspace(uint64_t n_tokens, uint64_t vocab,
 
 // Which rows without a token are written beside which launch.  Sorting, short batches' pieces and chains leave the memory idle for about as long as it takes to
 // move these bytes; what is left goes beside the one-block sort, or the pieces of a long batch.  Rows written before the marks are known may be written again.
-#define FILL_SORT (24ull << 20)                  // beside each launch of a tiled sort
+#define FILL_COUNT (24ull << 20)                 // beside each count of a tiled sort, twice that where a base is read (65536 x 1024 on a base of 50257 rows 151 us, 159 with
+#define FILL_MOVE (64ull << 20)                  // 24 beside each launch; 9000 x 768 on a base 79, 88) and beside each move
 #define FILL_PIECES (32ull << 20)
 #define FILL_CHAINS (12ull << 20)
 #define MARK_MOST (1u << 20)                     // rows whose marks one block clears beside its sort
@@ -770,7 +786,7 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
         for (u32 pass = 0; pass < p.passes; ++pass, at ^= 1) {
             const SortFrom from = {pass ? nullptr : d_tokens, pass ? (u32*)(ws + p.keys[at ^ 1]) : nullptr, pass ? (u32*)(ws + p.places[at ^ 1]) : nullptr};
             const u32 clear = pass == 0 && present ? (u32)(round_up(vocab, 256) / 4) : 0;
-            const Units a = fill.take(FILL_SORT), b = fill.take(FILL_SORT);
+            const Units a = fill.take(d_base ? 2 * FILL_COUNT : FILL_COUNT), b = fill.take(FILL_MOVE);
             const u32 others = fill_blocks(a) + (u32)((clear + 1023) / 1024);
             hipLaunchKernelGGL(sort_count, dim3(p.tiles + others), dim3(256), 0, st, q, from, pass * p.bits, p.tile, p.tiles, (u32*)(ws + p.hist), n_chains, (u32*)present, clear, a, out, (const uint8_t*)(pass ? present : nullptr));
             hipLaunchKernelGGL(sort_move, dim3(p.tiles + fill_blocks(b)), dim3(256), 0, st, q, from, pass * p.bits, p.tile, p.tiles, (const u32*)(ws + p.hist), (u32*)(ws + p.keys[at]), (u32*)(ws + p.places[at]),

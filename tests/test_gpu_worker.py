@@ -637,3 +637,9 @@ def test_logits_at_the_borders_between_variants(vocab, t):
         dblp.policy_loss(x, target, adv, w, stats, ws, dlogits=d, logp=logp, old_logp=old, ref_logp=back, clip=(0.2, 0.3), kl_coef=0.1)
         check_policy((stats, logp, d), ref.policy(x, target, adv, w, old, back, (0.2, 0.3), 0.1, 1.0), x, t, 1.0)
         assert untouched(buf, d)
+
+
+# odd widths below and above a unit, batches on both sides of one block's sort and of one piece length, with and without a base
+@pytest.mark.parametrize("n, vocab, dim, kind", [(8192, 900, 3, "skewed"), (8193, 900, 2, "bad"), (8200, 40000, 333, "skewed"), (16384, 70, 5, "any"), (16385, 600, 1, "skewed"), (17000, 300, 130, "any")])
+def test_embed_grad_between_its_sorts(n, vocab, dim, kind):
+    test_embed_grad(n, vocab, dim, kind)
