@@ -32,7 +32,8 @@
  *   - Zero tokens or rows are allowed.  Limits: tokens, rows, vocabulary and columns below 2^31, columns of
  *     dblp_embed_grad below 2^22.
  *   - A workspace is DEVICE memory of the size that dblp_*_workspace gives, 256-byte aligned, of any
- *     contents; it is free again when the stream has passed the call.
+ *     contents; it is free again when the stream has passed the call.  One of a larger call (more tokens, a
+ *     larger vocabulary, more columns) is large enough for a smaller one.
  */
 #ifndef DBLP_WORKER_H
 #define DBLP_WORKER_H

@@ -493,7 +493,7 @@ __global__ __launch_bounds__(256) void policy_join(const double* __restrict__ sh
 // ------------------------------------------------------------------------------------------
 #define FAR_BYTES (256ull << 20)                 // logits that the memory-side cache does not hold are read and written past it
 
-// Where the workspace holds the shares of sums and of rows; the tokens' parts come first.
+// Where the workspace holds the shares of sums and of rows; the tokens' parts come first.  (A larger batch's is large enough for a smaller one.)
 struct LogitsPlan { u64 sums, softs, chosen, bytes; };
 // Fewer rows than FEW_ROWS leave half of the CUs without one: blocks share a row of at least MANY_VECS vectors.  Policy loss, with the sums, of rows of 50257 floats: 64 rows
 // 17 us by a block each, 14.5 shared; 100 18, 16; 140 19, 20; 190 21, 25; two rows of 150000 25, 10.
@@ -501,7 +501,7 @@ struct LogitsPlan { u64 sums, softs, chosen, bytes; };
 #define MANY_VECS 2048
 static LogitsPlan logits_plan(u64 n) {
     const u64 sums = round_up(n * sizeof(TokenPart), 256), softs = sums + round_up((n + SUM_SHARE - 1) / SUM_SHARE * 32, 256);
-    const u64 few = n < FEW_ROWS ? n : 0, chosen = softs + round_up(few * SHARES_MOST * sizeof(Soft), 256);
+    const u64 few = n < FEW_ROWS ? n : FEW_ROWS - 1, chosen = softs + round_up(few * SHARES_MOST * sizeof(Soft), 256);
     return {sums, softs, chosen, chosen + round_up(few * 4, 256) + 256};
 }
 // About three blocks a CU, of at least two vectors a thread.

@@ -678,6 +678,7 @@ struct GradPlan {
     u64 keys[2], places[2], hist, present, chains, n_chains, chain, bytes;
 };
 
+#define GRAD_FEW 16384                           // tokens whose pieces are short
 static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
     GradPlan p = {};
     p.short_batch = n <= GRAD_SHORT;
@@ -688,7 +689,7 @@ static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
     while ((vocab >> bits) != 0) ++bits;                 // keys run to vocab itself
     p.passes = (bits + 8) / 9;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.len = n <= 16384 ? 8 : 16;               // few places: enough threads; many: fewer chains (65536 x 1024: 12 us of chains, 18 with 8)
+    p.len = n <= GRAD_FEW ? 8 : 16;               // few places: enough threads; many: fewer chains (65536 x 1024: 12 us of chains, 18 with 8)
     p.pieces = (u32)((n + p.len - 1) / p.len);
     p.tile = (u32)round_up((n + SORT_TILES - 1) / SORT_TILES, SORT_STEP);
     p.tiles = (u32)((n + p.tile - 1) / p.tile);
@@ -706,7 +707,8 @@ static GradPlan grad_plan(u64 n, u64 vocab, u32 dim) {
 
 extern "C" uint64_t dblp_embed_grad_workspace(uint64_t n_tokens, uint64_t vocab, uint32_t dim) {
     if (n_tokens >= COUNT_LIMIT || vocab == 0 || vocab >= COUNT_LIMIT || dim == 0 || dim >= GRAD_DIM_LIMIT) return 0;
-    return grad_plan(n_tokens, vocab, dim).bytes;
+    const u64 bytes = grad_plan(n_tokens, vocab, dim).bytes, few = n_tokens > GRAD_FEW ? grad_plan(GRAD_FEW, vocab, dim).bytes : 0;
+    return bytes > few ? bytes : few;                // (a larger batch's is large enough for a smaller one)
 }
 
 // Which rows without a token are written beside which launch.  Sorting, short batches' pieces and chains leave the memory idle for about as long as it takes to

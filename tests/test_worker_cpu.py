@@ -162,3 +162,14 @@ def test_binding_refuses_what_is_no_matrix():
         with pytest.raises(dblp.DblpError) as e:
             f()
         assert e.value.code == binding.EINVAL
+
+
+def test_a_workspace_of_a_larger_call_is_large_enough():
+    counts = [0, 1, 2, 127, 128, 129, 512, 513, 8192, 8193, 16383, 16384, 16385, 16400, 30000, 65536, 10**6]
+    for vocab, dim in ((1, 1), (1000, 333), (50257, 1024), (200000, 7)):
+        grads, logits = ([f(n, *a) for n in counts] for f, a in ((dblp.embed_grad_workspace, (vocab, dim)), (dblp.logits_workspace, (vocab,))))
+        assert grads == sorted(grads) and logits == sorted(logits)
+    for n in (5, 600, 9000, 70000):
+        for sizes in ([dblp.embed_grad_workspace(n, v, 64) for v in (1, 2, 511, 512, 513, 2**18, 2**20 + 1, 2**30)],
+                      [dblp.embed_grad_workspace(n, 1000, d) for d in (1, 8, 9, 1000, 2**20)], [dblp.logits_workspace(n, v) for v in (1, 2048, 50257, 2**30)]):
+            assert sizes == sorted(sizes)
