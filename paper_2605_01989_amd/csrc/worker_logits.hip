@@ -3,8 +3,8 @@
 //
 // A row is read once: its largest value and the sum of its exponentials are found together, and where a gradient is wanted the row
 // stays in registers between the sum and the gradient (50257 16-bit values: 100 KB of a CU's 512 KB, two rows a CU).
-// Memory bounds all of it: log probabilities of 8192 x 50257 16-bit values, 30 % of the rows masked, take 92 us (6.2 TB/s, the rate of a large read), their policy loss
-// 277 us (583 MB read, 826 written: 5.1 TB/s, where a large copy reaches 5.2).  A row of 50257 alone is bound by its launch: 5 us of the GPU's time.
+// Memory bounds all of it: log probabilities of 8192 x 50257 16-bit values, 30 % of the rows masked, take 90 us (6.4 TB/s, the rate of a large read), their policy loss
+// 275 us (583 MB read, 826 written: 5.1 TB/s, where a large copy reaches 5.2).  A row of 50257 alone is bound by its launch: 5 us of the GPU's time.
 #include "worker_common.h"
 
 // ------------------------------------------------------------------------------------------
@@ -21,8 +21,13 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
     return {m, a.s * exp_of(a.m, at) + b.s * exp_of(b.m, at)};
 }
 __device__ __forceinline__ Soft soft_wave(Soft a) {
-    for (int d = 1; d < WAVE; d <<= 1) a = soft_join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d)});
-    return a;
+    float m = a.m;
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float s = a.s * exp_of(a.m, shift_of(m));              // scaled once
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) s += __shfl_xor(s, d);
+    return {m, s};
 }
 // The whole block's, to all of its threads.  `part`: one entry for each wave.
 template <int NT>
@@ -101,7 +106,13 @@ __device__ __forceinline__ void soft_vecs(Soft& a, const typename T::elem* body,
             r[j] = no_logits<V, W>();
             if (i < hi) r[j] = FAR ? V::load_far(body + (u64)i * W) : V::load(body + (u64)i * W);
         }
-        soft_add<V, W, STREAM>(a, r);
+        // as many as hold anything: rows shorter than a step are bound by these instructions (160 MB of rows of 256 16-bit values 107 us, 178 with all four)
+        if (hi - whole > 2 * NT) soft_add<V, W, STREAM>(a, r);
+        else {
+            const typename V::raw first[1] = {r[0]}, second[1] = {r[1]};
+            soft_add<V, W, 1>(a, first);
+            if (hi - whole > NT) soft_add<V, W, 1>(a, second);
+        }
     }
 }
 template <class T, int NT, bool FAR>
