@@ -270,7 +270,7 @@ __device__ __forceinline__ void skip_row(typename T::elem* drow, u32 vocab, u32 
     if (threadIdx.x < singles) drow[threadIdx.x < head ? threadIdx.x : threadIdx.x + vecs * W] = (typename T::elem)0.0f;
 }
 
-// Registers for two rows of 512 threads a CU, or one of 1024: 22 vectors a thread fit without spilling (152 k and 178 k 16-bit values at 92 % of a large copy's rate, which two
+// Registers for two rows of 512 threads a CU, or one of 1024: two are faster wherever 512 threads hold the row (3051 rows of 65536 16-bit values 155 us, 196 by 1024).  22 vectors a thread fit without spilling (152 k and 178 k 16-bit values at 92 % of a large copy's rate, which two
 // passes reach 68 % of).  Three rows a CU, with a few registers spilled, are slower: 8192 rows of 50257 16-bit values 292 us, 277 with two.
 #define HELD_WAVES __attribute__((amdgpu_waves_per_eu(4)))
 // A block takes a row and holds it: NV vectors a thread, all on their way at once.  A wave's vectors follow each other.  Where the gradient's row begins at another
@@ -647,6 +647,8 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
             else if (vocab <= 256 * 8 * W) held(Int<256>(), Int<8>());
             else if (vocab <= 512 * 8 * W) held(Int<512>(), Int<8>());
             else if (vocab <= 512 * 14 * W) held(Int<512>(), Int<14>());
+            else if (vocab <= 512 * 18 * W) held(Int<512>(), Int<18>());
+            else if (vocab <= 512 * 22 * W) held(Int<512>(), Int<22>());
             else if (vocab <= 1024 * 14 * W) held(Int<1024>(), Int<14>());
             else if (vocab <= 1024 * 18 * W) held(Int<1024>(), Int<18>());
             else if (vocab <= 1024 * 22 * W) held(Int<1024>(), Int<22>());

@@ -643,3 +643,9 @@ def test_logits_at_the_borders_between_variants(vocab, t):
 @pytest.mark.parametrize("n, vocab, dim, kind", [(8192, 900, 3, "skewed"), (8193, 900, 2, "bad"), (8200, 40000, 333, "skewed"), (16384, 70, 5, "any"), (16385, 600, 1, "skewed"), (17000, 300, 130, "any")])
 def test_embed_grad_between_its_sorts(n, vocab, dim, kind):
     test_embed_grad(n, vocab, dim, kind)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("vocab", [512 * 14 * 4 + 1, 512 * 18 * 4 + 2, 512 * 22 * 4 + 1, 512 * 14 * 8 + 1, 512 * 18 * 8, 512 * 18 * 8 + 3, 512 * 22 * 8, 512 * 22 * 8 + 1])
+def test_logits_at_the_borders_between_two_rows_a_unit_and_one(vocab, t):
+    test_logits_at_the_borders_between_variants(vocab, t)
