@@ -105,6 +105,8 @@ int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, uint32_t vo
  *   loss = sum of weights[t] (pl + kl_coef kl)          (kl_coef 0: no KL term in loss and gradient, its sum is watched)
  *   d loss / d lp = weights[t] ([clipped term larger or equal] -r A + kl_coef (1 - exp(ref_logp[t] - lp)))
  *   dlogits[t][j] = grad_scale (d loss / d lp) ([j = targets[t]] - softmax(logits[t])[j])
+ * A reference of -inf or far below the policy (a token that it masks) has an endless or large kl, and its gradient is that of a
+ * slope of kl_coef.  Where lp is -inf (a token of probability zero was taken) kl is exp(inf) - inf, NaN, and the row's gradient infinite or NaN.
  * The weights hold the normalisation (one over the number of tokens, or of a sequence's tokens, ...).  With A = 1 and no old
  * and reference policy the gradient is that of the cross-entropy, whose value is -sum weights logp.
  * Not counted: targets[t] is none, weights[t] = 0, or all of the row's logits are -inf.  Such a token's row of

@@ -210,15 +210,19 @@ __global__ __launch_bounds__(64) void logprob_join(Shares q, u32 vocab, const in
 struct Policy { const int64_t* targets; const float *advantages, *weights, *old_logp, *ref_logp; float low, high, kl, grad_scale; };
 struct __align__(16) TokenPart { float policy, kl; u32 counted, clipped; };          // a token's part of the five sums, weighted
 
-// exp(d) - 1 - d, by its series where the difference would cancel (next term below 2^-30 of the sum).
-__device__ __forceinline__ float exp_past(float d) {
+// e = exp(d) - 1 and k = e - d, by k's series where the differences would cancel (next term below 2^-30 of the sum).  e is not k + d: of a reference far below the
+// policy (d = -1e9, -inf) nothing would be left of it, and the gradient is made of it.
+struct Past { float e, k; };
+__device__ __forceinline__ Past past_of(float d) {
     if (fabsf(d) < 0.5f) {
         float t = 1.0f;
 #pragma unroll
         for (int i = 10; i > 2; --i) t = 1.0f + d * (1.0f / i) * t;
-        return 0.5f * d * d * t;
+        const float k = 0.5f * d * d * t;
+        return {d + k, k};
     }
-    return exp_of(d, 0.0f) - 1.0f - d;
+    const float e = exp_of(d, 0.0f) - 1.0f;
+    return {e, e - d};
 }
 // Of a counted token with log probability lp: what it adds to the sums, and d loss / d lp.  (In fp32, from differences taken in fp64; more would cost the registers that
 // hold the row.)
@@ -231,9 +235,9 @@ __device__ __forceinline__ TokenPart token_part(const Policy& p, u32 t, double l
     const bool clipped = held < free_term;
     float g = clipped ? 0.0f : -free_term, kl = 0.0f;
     if (p.ref_logp) {
-        const float d = (float)((double)p.ref_logp[t] - lp);
-        kl = exp_past(d);
-        if (p.kl != 0.0f) g -= p.kl * (kl + d);            // (watched only: an infinite term is not multiplied by zero)
+        const Past past = past_of((float)((double)p.ref_logp[t] - lp));
+        kl = past.k;
+        if (p.kl != 0.0f) g -= p.kl * past.e;              // (watched only: an infinite term is not multiplied by zero)
     }
     *slope = w * g;
     return {w * -(clipped ? held : free_term), w * kl, 1u, clipped ? 1u : 0u};
