@@ -24,8 +24,8 @@
  *     element.  An input's rows may overlap or be the same row (stride 0); an output's stride is at least
  *     its columns.  An output overlaps no other argument except where "in place" says so.  Rows whose
  *     address and stride are multiples of 16 bytes are fastest.
- *   - Types of matrices: DBLP_F32, DBLP_BF16, DBLP_F16.  Everything is computed in fp32 (sums of whole
- *     batches in fp64) and rounded once, to nearest even, when it is stored.
+ *   - Types of matrices: DBLP_F32, DBLP_BF16, DBLP_F16.  Everything is computed in fp32 (what is
+ *     made of a token's score, and sums of whole batches, in fp64) and rounded once, to nearest even, when it is stored.
  *   - A token, position or target outside its table (negative, or not below the number of rows) is "none":
  *     its row of the table is taken as zero, it has no gradient, it is not counted in a loss.  This is
  *     how padding and prompts are marked; nothing is read out of bounds.
@@ -102,6 +102,7 @@ int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, uint32_t vo
  *   r  = exp(lp - old_logp[t])                          (d_old_logp NULL: the policy is its own old one, r = 1)
  *   pl = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),      A = advantages[t]
  *   kl = exp(ref_logp[t] - lp) - (ref_logp[t] - lp) - 1          (d_ref_logp NULL: 0)
+ *      (a ratio past fp64 counts as the largest number, so that A = 0 has no part in the loss)
  *   loss = sum of weights[t] (pl + kl_coef kl)          (kl_coef 0: no KL term in loss and gradient, its sum is watched)
  *   d loss / d lp = weights[t] ([clipped term larger or equal] -r A + kl_coef (1 - exp(ref_logp[t] - lp)))
  *   dlogits[t][j] = grad_scale (d loss / d lp) ([j = targets[t]] - softmax(logits[t])[j])

@@ -210,37 +210,47 @@ __global__ __launch_bounds__(64) void logprob_join(Shares q, u32 vocab, const in
 struct Policy { const int64_t* targets; const float *advantages, *weights, *old_logp, *ref_logp; float low, high, kl, grad_scale; };
 struct __align__(16) TokenPart { float policy, kl; u32 counted, clipped; };          // a token's part of the five sums, weighted
 
-// e = exp(d) - 1 and k = e - d, by k's series where the differences would cancel (next term below 2^-30 of the sum).  e is not k + d: of a reference far below the
+// exp(x) as 2^n times the series of what is left, below 0.35: the first term left out is 2^-37 of it.
+__device__ __forceinline__ double exp_wide(double x) {
+    x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;       // past both ends of fp64; NaN stays
+    const double n = rint(x * 1.4426950408889634);
+    x = fma(n, -0.6931471805599453, x);
+    double t = 1.0 / 362880;
+    t = fma(t, x, 1.0 / 40320); t = fma(t, x, 1.0 / 5040); t = fma(t, x, 1.0 / 720); t = fma(t, x, 1.0 / 120); t = fma(t, x, 1.0 / 24);
+    t = fma(t, x, 1.0 / 6); t = fma(t, x, 0.5); t = fma(t, x, 1.0); t = fma(t, x, 1.0);
+    return ldexp(t, (int)n);
+}
+// e = exp(d) - 1 and k = e - d, by k's series where the differences would cancel (next term 2^-36 of the sum).  e is not k + d: of a reference far below the
 // policy (d = -1e9, -inf) nothing would be left of it, and the gradient is made of it.
-struct Past { float e, k; };
-__device__ __forceinline__ Past past_of(float d) {
-    if (fabsf(d) < 0.5f) {
-        float t = 1.0f;
-#pragma unroll
-        for (int i = 10; i > 2; --i) t = 1.0f + d * (1.0f / i) * t;
-        const float k = 0.5f * d * d * t;
+struct Past { double e, k; };
+__device__ __forceinline__ Past past_of(double d) {
+    if (fabs(d) < 0.25) {
+        double t = 1.0 / 362880;
+        t = fma(t, d, 1.0 / 40320); t = fma(t, d, 1.0 / 5040); t = fma(t, d, 1.0 / 720); t = fma(t, d, 1.0 / 120); t = fma(t, d, 1.0 / 24);
+        t = fma(t, d, 1.0 / 6); t = fma(t, d, 0.5);
+        const double k = d * d * t;
         return {d + k, k};
     }
-    const float e = exp_of(d, 0.0f) - 1.0f;
+    const double e = exp_wide(d) - 1.0;
     return {e, e - d};
 }
-// Of a counted token with log probability lp: what it adds to the sums, and d loss / d lp.  (In fp32, from differences taken in fp64; more would cost the registers that
-// hold the row.)
-__device__ __forceinline__ TokenPart token_part(const Policy& p, u32 t, double lp, float* slope) {
-    const float w = p.weights[t], a = p.advantages[t];
-    float r = p.old_logp ? exp_of((float)(lp - (double)p.old_logp[t]), 0.0f) : 1.0f;
-    if (r == INFINITY) r = FLT_MAX;                        // a ratio past fp32 times an advantage of zero is zero
-    const float lo = 1.0f - p.low, hi = 1.0f + p.high;
-    const float free_term = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
+// Of a counted token with log probability lp: what it adds to the sums, and d loss / d lp.  In fp64, by one thread a row (a block's other waves and the CU's other row
+// hide it): a ratio may be past fp32 where its product with a small weight is not, and each part is rounded once.
+__device__ __forceinline__ TokenPart token_part(const Policy& p, u32 t, double lp, double* slope) {
+    const double w = p.weights[t], a = p.advantages[t];
+    double r = p.old_logp ? exp_wide(lp - (double)p.old_logp[t]) : 1.0;
+    if (r > DBL_MAX) r = DBL_MAX;                          // a ratio past fp64 times an advantage of zero is zero
+    const double lo = 1.0 - (double)p.low, hi = 1.0 + (double)p.high;
+    const double free_term = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
     const bool clipped = held < free_term;
-    float g = clipped ? 0.0f : -free_term, kl = 0.0f;
+    double g = clipped ? 0.0 : -free_term, kl = 0.0;
     if (p.ref_logp) {
-        const Past past = past_of((float)((double)p.ref_logp[t] - lp));
+        const Past past = past_of((double)p.ref_logp[t] - lp);
         kl = past.k;
-        if (p.kl != 0.0f) g -= p.kl * past.e;              // (watched only: an infinite term is not multiplied by zero)
+        if (p.kl != 0.0f) g -= (double)p.kl * past.e;      // (watched only: an infinite term is not multiplied by zero)
     }
     *slope = w * g;
-    return {w * -(clipped ? held : free_term), w * kl, 1u, clipped ? 1u : 0u};
+    return {(float)(w * -(clipped ? held : free_term)), (float)(w * kl), 1u, clipped ? 1u : 0u};
 }
 
 __device__ __forceinline__ void put_stats(float* stats, const double (&s)[4], float kl_coef) {
@@ -251,12 +261,12 @@ __device__ __forceinline__ void put_stats(float* stats, const double (&s)[4], fl
 // What one thread finds out about a row: its token's part of the sums, and the slope for the row's gradient.  `stats`: of a batch of one token.
 __device__ __forceinline__ float close_row(const Policy& p, u32 t, float x, Soft a, float* logp, TokenPart* parts, float* stats) {
     const double lp = logp_of(x, a);
-    float slope;
+    double slope;
     const TokenPart part = token_part(p, t, lp, &slope);
     parts[t] = part;
     if (logp) logp[t] = (float)lp;
     if (stats) { const double s[4] = {part.policy, part.kl, (double)part.clipped, (double)part.counted}; put_stats(stats, s, p.kl); }
-    return slope * p.grad_scale;
+    return (float)(slope * (double)p.grad_scale);
 }
 // A row that is not counted: `empty`, all its logits are -inf.
 template <class T, int NT>
@@ -437,7 +447,7 @@ __global__ __launch_bounds__(SHARE_NT) void policy_shares(Shares q, Policy p, co
             if (read) for (u32 i = 0; i < q.n; ++i) a = soft_join(a, softs[tid * q.n + i]);
             double lp = read ? -INFINITY : 0.0;
             if (a.s != 0.0f) {
-                float slope;
+                double slope;
                 lp = logp_of(chosen[tid], a);
                 const TokenPart part = token_part(p, tid, lp, &slope);
                 sum[0] = part.policy; sum[1] = part.kl; sum[2] = part.clipped; sum[3] = part.counted;
@@ -457,9 +467,9 @@ __global__ __launch_bounds__(SHARE_NT) void policy_shares(Shares q, Policy p, co
     Soft a = {-INFINITY, 0.0f};
     if (at < vocab && p.weights[t] != 0.0f) a = soft_of_row(softs, t, q.n);
     const bool counted = a.s != 0.0f;
-    float g = 0.0f;
-    if (counted) token_part(p, t, logp_of(chosen[t], a), &g);
-    g *= p.grad_scale;
+    double slope = 0.0;
+    if (counted) token_part(p, t, logp_of(chosen[t], a), &slope);
+    const float g = (float)(slope * (double)p.grad_scale);
     const float k = counted ? -g / a.s : 0.0f;
     const u32 single = s == 0 && tid < c.singles ? place_of_single<W>(c, tid) : 0;
     for (u32 i = lo + tid; i < hi; i += SHARE_NT * STREAM) {

@@ -56,3 +56,26 @@ def test_references_far_below_the_policy(n, vocab, t):
             check_policy(got, {k: v.clone() for k, v in want.items()}, x, t, 1.0)
             if got[2] is not None:                   # (the reference 30 above the policy is past fp16)
                 assert bool(torch.isfinite(got[2].cpu()[want["dlogits"].abs() < torch.finfo(t).max / 2]).all())
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n, vocab", WAYS)
+def test_ratios_past_fp32_whose_products_are_not(n, vocab, t):
+    """exp(lp - old) of 100 and more with a weight that brings it back, for advantages below zero (which are not clipped above)."""
+    t = TYPES[t]
+    g = gen(32 + n)
+    x, target, adv, w, ws = case(g, n, vocab, t)
+    adv, w = -0.1 - 0.9 * torch.rand(n, generator=g, device="cuda"), torch.full((n,), 2.0 ** -110, device="cuda")
+    lp = ref.logprobs(x, target)[0].cuda()
+    for far in (100.0, 130.0, 155.0):
+        old = (lp - far).float()
+        want = ref.policy(x, target, adv, w, old, None, (0.2, 0.3), 0.0, 1.0)
+        assert 2.0 ** -126 < float(want["slope"].abs().min()) and float(want["slope"].abs().max()) < 2.0 ** 127
+        for got in run(x, target, adv, w, ws, old_logp=old, clip=(0.2, 0.3)):
+            check_policy(got, {k: v.clone() for k, v in want.items()}, x, t, 1.0)
+    # past fp64 too: infinite, but an advantage of zero gives zero
+    for old in ((lp - 1000).float(), torch.full((n,), -float("inf"), device="cuda")):
+        for stats, _, d in run(x, target, adv, w, ws, old_logp=old):
+            assert float(stats[0]) == float("inf") and float(stats[3]) == 0 and (d is None or not bool(torch.isfinite(d[torch.arange(n), target]).any()))
+        for stats, _, d in run(x, target, torch.zeros_like(adv), w, ws, old_logp=old):
+            assert stats[:4].tolist() == [0, 0, 0, 0] and (d is None or not bool(d.any()))
