@@ -126,11 +126,16 @@ __device__ __forceinline__ Soft soft_row(const typename T::elem* row, u32 n) {
     return a;
 }
 
-// Log probability of a logit x.  A score is a difference of numbers of ten or twenty, and policies' ratios are differences of scores: the last sums are fp64, and
-// the logarithm is taken of a number in 1/2 .. 1, the exponent of s apart, so that it is off by 2^-24 and not by 2^-20.  The largest value and the logarithm are not added
-// up first: in a row of the type's lowest value the logarithm would be lost.
+// Log probability of a logit x.  A score is a difference of numbers of ten or twenty, and policies' ratios are differences of scores: the last sums are fp64, and so is
+// the logarithm, by the series of 2 artanh f, f = (m - 1) / (m + 1), of a number m in sqrt(1/2) .. sqrt(2) (the first term left out is 2^-39 of the sum).  One thread a row
+// takes it.  The largest value and the logarithm are not added up first: in a row of the type's lowest value the logarithm would be lost.
 __device__ __forceinline__ double log_of(float s) {
-    return ((double)__builtin_amdgcn_frexp_expf(s) + (double)__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(s))) * 0.6931471805599453;
+    double m = __builtin_amdgcn_frexp_mantf(s), e = __builtin_amdgcn_frexp_expf(s);
+    if (m < 0.7071067811865476) { m *= 2.0; e -= 1.0; }
+    const double f = (m - 1.0) / (m + 1.0), q = f * f;
+    double t = 1.0 / 13;
+    t = fma(t, q, 1.0 / 11); t = fma(t, q, 1.0 / 9); t = fma(t, q, 1.0 / 7); t = fma(t, q, 1.0 / 5); t = fma(t, q, 1.0 / 3); t = fma(t, q, 1.0);
+    return fma(e, 0.6931471805599453, 2.0 * f * t);
 }
 __device__ __forceinline__ double logp_of(float x, Soft a) { return ((double)x - (double)a.m) - log_of(a.s); }
 

@@ -58,6 +58,12 @@ def test_references_far_below_the_policy(n, vocab, t):
                 assert bool(torch.isfinite(got[2].cpu()[want["dlogits"].abs() < torch.finfo(t).max / 2]).all())
 
 
+def apart_from_borders(g, n):
+    """log of ratios to an old policy, none within a hundredth of a border of (0.2, 0.3)."""
+    c = torch.tensor([-0.6, -0.3, -0.15, -0.02, 0.04, 0.18, 0.3, 0.9], device="cuda")
+    return c[torch.randint(0, len(c), (n,), generator=g, device="cuda")] + 0.02 * torch.rand(n, generator=g, device="cuda")
+
+
 @pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("n, vocab", WAYS)
 def test_ratios_past_fp32_whose_products_are_not(n, vocab, t):
@@ -79,3 +85,54 @@ def test_ratios_past_fp32_whose_products_are_not(n, vocab, t):
             assert float(stats[0]) == float("inf") and float(stats[3]) == 0 and (d is None or not bool(torch.isfinite(d[torch.arange(n), target]).any()))
         for stats, _, d in run(x, target, torch.zeros_like(adv), w, ws, old_logp=old):
             assert stats[:4].tolist() == [0, 0, 0, 0] and (d is None or not bool(d.any()))
+
+
+@pytest.mark.parametrize("n, vocab", WAYS)
+def test_what_a_token_adds_is_rounded_once(n, vocab):
+    """Rows of k equal logits and masked ones: every exponential is 1, the sum k, and lp = -log k, so that only what is done with the scores is left.  A slope is
+    one rounding to fp32 from its value, a gradient two more (the quotient by k, and at the target the sum with the slope), a part of the loss one and the
+    sums one.  Besides, 2^-30 of the magnitudes is allowed: more than fp64 series of 2^-36 need."""
+    g, rest = gen(33 + n), 2.0 ** -30
+    x, target, adv, w, ws = case(g, n, vocab, torch.float32)
+    on = torch.rand(n, vocab, generator=g, device="cuda") < torch.rand(n, 1, generator=g, device="cuda")
+    on[torch.arange(n), target] = True
+    x = torch.where(on, torch.randn(n, 1, generator=g, device="cuda"), -float("inf"))
+    k = on.sum(1).cpu().double()
+    lp = -k.log()
+    old, back = (lp.cuda() - apart_from_borders(g, n)).float(), (lp.cuda() + apart_from_borders(g, n)).float()
+    want = ref.policy(x, target, adv, w, old, back, (0.2, 0.3), 0.1, 1.0)
+    at = torch.arange(n), target.cpu()
+    for stats, logp, d in run(x, target, adv, w, ws, old_logp=old, ref_logp=back, clip=(0.2, 0.3), kl_coef=0.1):
+        assert bool(((logp.cpu().double() - lp).abs() <= U * lp.abs() * (1 + U) + rest).all())
+        s = stats.cpu().double()
+        assert bool(((s[:3] - want["stats"][:3]).abs() <= 2.1 * U * want["mags"] + rest * want["moves"]).all()) and torch.equal(s[3:], want["stats"][3:])
+        if d is None:
+            continue
+        d, slope, bend = d.cpu().double(), want["slope"], want["bend"]
+        hit = d[at]
+        assert bool(((hit - slope * (1 - 1 / k)).abs() <= 3.1 * U * slope.abs() + rest * bend).all())
+        d[at] = 0.0
+        rows = torch.where(on.cpu(), (-slope / k)[:, None], 0.0)
+        rows[at] = 0.0
+        assert bool(((d - rows).abs() <= 2.1 * U * rows.abs() + (rest * bend / k)[:, None]).all())
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n, vocab", WAYS)
+def test_scores_of_equal_logits_are_rounded_once(n, vocab, t):
+    """lse = c + log k of rows of k logits of one value c, the others masked: the sum is exact, so that lse and lp are one rounding from their values."""
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    g, rest = gen(34 + n), 2.0 ** -30
+    x, target, _, _, ws = case(g, n, vocab, t)
+    logp, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    for share in (0.001, 0.03, 0.2, 0.6, 1.0):
+        on = torch.rand(n, vocab, generator=g, device="cuda") < share * torch.rand(n, 1, generator=g, device="cuda").add_(0.5)
+        on[torch.arange(n), target] = True
+        c = torch.randn(n, 1, generator=g, device="cuda").to(t)
+        x = torch.where(on, c, -float("inf"))
+        dblp.token_logprobs(x, target, logp, ws, lse=lse)
+        log = on.sum(1).cpu().double().log()
+        want = c[:, 0].cpu().double() + log
+        assert bool(((logp.cpu().double() + log).abs() <= U * log * (1 + U) + rest).all())
+        assert bool(((lse.cpu().double() - want).abs() <= U * want.abs() * (1 + U) + rest).all())
