@@ -21,6 +21,7 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
     return {m, a.s * exp_of(a.m, at) + b.s * exp_of(b.m, at)};
 }
 __device__ __forceinline__ Soft soft_wave(Soft a) {
+#pragma clang fp contract(off)                             // a lane's product is rounded before it meets another's: all lanes find the same sum
     float m = a.m;
 #pragma unroll
     for (int d = 1; d < WAVE; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
@@ -194,6 +195,23 @@ __global__ __launch_bounds__(SHARE_NT) void soft_shares(Shares q, const typename
 __device__ __forceinline__ Soft soft_of_row(const Soft* softs, u32 t, u32 n) {
     const u32 lane = threadIdx.x & 63;
     return soft_wave(lane < n ? softs[t * n + lane] : Soft{-INFINITY, 0.0f});
+}
+// The same by one thread, with the same bits: the sums of the butterfly above as a tree (entries past n add zero).
+__device__ __forceinline__ Soft soft_of_row_alone(const Soft* softs, u32 t, u32 n) {
+#pragma clang fp contract(off)
+    Soft part[SHARES_MOST];
+    float m = -INFINITY, s[SHARES_MOST];
+#pragma unroll
+    for (u32 i = 0; i < SHARES_MOST; ++i) part[i] = softs[t * n + (i < n ? i : n - 1)];
+#pragma unroll
+    for (u32 i = 0; i < SHARES_MOST; ++i) m = fmaxf(m, part[i].m);
+#pragma unroll
+    for (u32 i = 0; i < SHARES_MOST; ++i) s[i] = i < n ? part[i].s * exp_of(part[i].m, shift_of(m)) : 0.0f;
+#pragma unroll
+    for (u32 d = 1; d < SHARES_MOST; d <<= 1)
+#pragma unroll
+        for (u32 i = 0; i < SHARES_MOST; i += 2 * d) s[i] += s[i + d];
+    return {m, s[0]};
 }
 __global__ __launch_bounds__(64) void logprob_join(Shares q, u32 vocab, const int64_t* __restrict__ targets, const Soft* __restrict__ softs, const float* __restrict__ chosen,
                                                    float* __restrict__ logp, float* __restrict__ lse) {
@@ -433,7 +451,7 @@ __device__ __forceinline__ bool sum_block(double (&s)[4], double (&sh)[4][NT / W
     return true;
 }
 // Few long rows, the second launch: every block of a row joins its shares and finds the slope for itself; one block more does so for all tokens (at most SHARE_NT) and adds
-// them up.
+// them up, from the same bits: a token is counted as clipped when its gradient is zero.
 template <class T>
 __global__ __launch_bounds__(SHARE_NT) void policy_shares(Shares q, Policy p, const typename T::elem* logits, u64 stride, u32 vocab, typename T::elem* dlogits, u64 dstride, u32 n,
                                                           const Soft* __restrict__ softs, const float* __restrict__ chosen, float* __restrict__ logp, float* __restrict__ stats) {
@@ -449,7 +467,7 @@ __global__ __launch_bounds__(SHARE_NT) void policy_shares(Shares q, Policy p, co
             const u64 at = (u64)p.targets[tid];
             const bool read = at < vocab && p.weights[tid] != 0.0f;
             Soft a = {-INFINITY, 0.0f};
-            if (read) for (u32 i = 0; i < q.n; ++i) a = soft_join(a, softs[tid * q.n + i]);
+            if (read) a = soft_of_row_alone(softs, tid, q.n);
             double lp = read ? -INFINITY : 0.0;
             if (a.s != 0.0f) {
                 double slope;

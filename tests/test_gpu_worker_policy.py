@@ -136,3 +136,26 @@ def test_scores_of_equal_logits_are_rounded_once(n, vocab, t):
         want = c[:, 0].cpu().double() + log
         assert bool(((logp.cpu().double() + log).abs() <= U * log * (1 + U) + rest).all())
         assert bool(((lse.cpu().double() - want).abs() <= U * want.abs() * (1 + U) + rest).all())
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n, vocab", [(100, 40001), (60, 90001), (3, 300001), (140, 9001), (130, 200003)])
+def test_the_sums_and_the_gradient_are_of_one_score(n, vocab, t):
+    """Ratios of all tokens within 2^-19 of a border that is moved through them by single steps of fp32: a token is counted as clipped when, and only when, its row's
+    gradient is zero."""
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    g = gen(35 + n)
+    x, target, _, w, ws = case(g, n, vocab, t)
+    one = torch.ones(n, device="cuda")
+    lp = ref.logprobs(x, target)[0].cuda()
+    old = (lp - torch.tensor(1.3, dtype=torch.float64).log()).float()
+    stats, d, rows = torch.empty(5, device="cuda"), torch.empty_like(x), torch.arange(n, device="cuda")
+    high = torch.tensor(0.3, dtype=torch.float32).view(torch.int32)
+    seen = set()
+    for step in range(-72, 73, 2 if vocab > 100000 else 1):
+        dblp.policy_loss(x, target, one, w, stats, ws, old_logp=old, dlogits=d, clip=(0.2, float((high + step).view(torch.float32))))
+        clipped = int((d[rows, target] == 0).sum())
+        assert int(stats[3]) == clipped, step
+        seen.add(clipped)
+    assert len(seen) > min(n, 8) // 2                # the border did pass through them
