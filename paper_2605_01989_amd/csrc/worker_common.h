@@ -262,10 +262,25 @@ struct OnDevice {
     ~OnDevice() { if (before >= 0 && before != now) (void)hipSetDevice(before); }
 };
 
-static inline int launched(const char* call) {
-    const hipError_t e = hipGetLastError();
-    if (e == hipSuccess) return DBLP_OK;
-    snprintf(worker_err, sizeof worker_err, "%s: %s", call, hipGetErrorString(e));
+// Launches of a call.  A launch's own result is asked for: the thread's last error may be one of the caller's, which is neither this call's failure nor
+// its to clear.  After a failure nothing more is launched.
+struct Launches {
+    hipError_t err = hipSuccess;
+    template <class... P, class... A>
+    void operator()(void (*kernel)(P...), dim3 grid, u32 threads, hipStream_t stream, A... args) {
+        if (err == hipSuccess) err = one<P...>((const void*)kernel, grid, threads, stream, args...);
+    }
+private:
+    template <class... P>
+    static hipError_t one(const void* kernel, dim3 grid, u32 threads, hipStream_t stream, P... params) {
+        void* at[] = {(void*)&params...};
+        return hipLaunchKernel(kernel, grid, dim3(threads), at, 0, stream);
+    }
+};
+static inline int launched(const char* call, const Launches& l) {
+    if (l.err == hipSuccess) return DBLP_OK;
+    snprintf(worker_err, sizeof worker_err, "%s: %s", call, hipGetErrorString(l.err));
+    (void)hipGetLastError();
     return DBLP_EHIP;
 }
 static inline int no_device(const char* call, hipError_t e) {

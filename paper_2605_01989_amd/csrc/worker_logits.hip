@@ -590,13 +590,14 @@ extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, 
     if (n_tokens == 0) return DBLP_OK;
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
+    Launches launch;
     const bool far = n_tokens * vocab * type_bytes(type) > FAR_BYTES;
     by_type(type, [&](auto tt) {
         typedef decltype(tt) T;
         const auto go = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             each_rows<NT>(n_tokens, [&](u64 row0, u32 rows) {
-                hipLaunchKernelGGL(far ? (logprob_rows<T, NT, true>) : (logprob_rows<T, NT, false>), dim3(rows), dim3(NT), 0, (hipStream_t)stream, (const typename T::elem*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
+                launch(far ? (logprob_rows<T, NT, true>) : (logprob_rows<T, NT, false>), dim3(rows), NT, (hipStream_t)stream, (const typename T::elem*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
                                    d_targets + row0, d_logp + row0, d_lse ? d_lse + row0 : nullptr);
             });
         };
@@ -606,8 +607,8 @@ extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, 
             const Shares q = shares_of(n_tokens, vecs);
             Soft* const softs = (Soft*)((uint8_t*)d_workspace + logits_plan(n_tokens).softs);
             float* const chosen = (float*)((uint8_t*)d_workspace + logits_plan(n_tokens).chosen);
-            hipLaunchKernelGGL(soft_shares<T>, dim3(q.n, (u32)n_tokens), dim3(SHARE_NT), 0, (hipStream_t)stream, q, (const typename T::elem*)d_logits, (u64)logits_stride, vocab, d_targets, (const float*)nullptr, softs, chosen);
-            hipLaunchKernelGGL(logprob_join, dim3((u32)n_tokens), dim3(64), 0, (hipStream_t)stream, q, vocab, d_targets, (const Soft*)softs, (const float*)chosen, d_logp, d_lse);
+            launch(soft_shares<T>, dim3(q.n, (u32)n_tokens), SHARE_NT, (hipStream_t)stream, q, (const typename T::elem*)d_logits, (u64)logits_stride, vocab, d_targets, (const float*)nullptr, softs, chosen);
+            launch(logprob_join, dim3((u32)n_tokens), 64, (hipStream_t)stream, q, vocab, d_targets, (const Soft*)softs, (const float*)chosen, d_logp, d_lse);
             return;
         }
         // Threads that end with their row: each has at most six vectors of it, in two steps.  A batch of 160 MB of 2500 16-bit values takes 32 us by 64 threads a row, 38 by 128,
@@ -618,7 +619,7 @@ extern "C" int dblp_token_logprobs(int device, void* stream, uint64_t n_tokens, 
         else if (vecs <= 256 * 6 || (n_tokens >= 256 && n_tokens < 768)) go(Int<256>());
         else go(Int<512>());
     });
-    return launched(call);
+    return launched(call, launch);
 }
 
 extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uint32_t vocab, const void* d_logits,
@@ -639,6 +640,7 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
     REFUSE_IF(!d_workspace || off(d_workspace, 256) || workspace_bytes < dblp_logits_workspace(n_tokens, vocab), "workspace missing, misaligned or too small");
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
+    Launches launch;
     const Policy p = {d_targets, d_advantages, d_weights, d_old_logp, d_ref_logp, clip_low, clip_high, kl_coef, grad_scale};
     TokenPart* const parts = (TokenPart*)d_workspace;
     double* const shares = (double*)((uint8_t*)d_workspace + logits_plan(n_tokens).sums);
@@ -658,14 +660,14 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
             const auto twice = [&](auto nt) {
                 constexpr int NT = decltype(nt)::value;
                 each_rows<NT>(n, [&](u64 row0, u32 rows) {
-                    hipLaunchKernelGGL((policy_twice<T, NT>), dim3(rows), dim3(NT), 0, st, rows_from(p, row0), (const E*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
+                    launch((policy_twice<T, NT>), dim3(rows), NT, st, rows_from(p, row0), (const E*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
                                        d_dlogits ? (E*)d_dlogits + row0 * dlogits_stride : nullptr, (u64)dlogits_stride, d_logp ? d_logp + row0 : nullptr, parts + row0, own_stats);
                 });
             };
             const auto held = [&](auto nt, auto nv) {
                 constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
                 each_rows<NT>(n, [&](u64 row0, u32 rows) {
-                    hipLaunchKernelGGL(far ? (policy_held<T, NT, NV, true>) : (policy_held<T, NT, NV, false>), dim3(rows), dim3(NT), 0, st, rows_from(p, row0), (const E*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
+                    launch(far ? (policy_held<T, NT, NV, true>) : (policy_held<T, NT, NV, false>), dim3(rows), NT, st, rows_from(p, row0), (const E*)d_logits + row0 * logits_stride, (u64)logits_stride, vocab,
                                        (E*)d_dlogits + row0 * dlogits_stride, (u64)dlogits_stride, d_logp ? d_logp + row0 : nullptr, parts + row0, own_stats);
                 });
             };
@@ -673,8 +675,8 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
             // (one token's row, if registers hold it, needs one launch where sharing needs two)
             if (d_dlogits && n < FEW_ROWS && vecs >= MANY_VECS && !(n == 1 && vocab <= 1024 * 18 * W)) {
                 const Shares q = shares_of(n, vecs);
-                hipLaunchKernelGGL(soft_shares<T>, dim3(q.n, n), dim3(SHARE_NT), 0, st, q, (const E*)d_logits, (u64)logits_stride, vocab, d_targets, d_weights, softs, chosen);
-                hipLaunchKernelGGL(policy_shares<T>, dim3(q.n + 1, n), dim3(SHARE_NT), 0, st, q, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, n, (const Soft*)softs, (const float*)chosen, d_logp, d_stats);
+                launch(soft_shares<T>, dim3(q.n, n), SHARE_NT, st, q, (const E*)d_logits, (u64)logits_stride, vocab, d_targets, d_weights, softs, chosen);
+                launch(policy_shares<T>, dim3(q.n + 1, n), SHARE_NT, st, q, p, (const E*)d_logits, (u64)logits_stride, vocab, (E*)d_dlogits, (u64)dlogits_stride, n, (const Soft*)softs, (const float*)chosen, d_logp, d_stats);
                 summed = true;
             }
             else if (!d_dlogits) vocab <= 64 * W * STREAM ? twice(Int<64>()) : twice(Int<512>());
@@ -693,8 +695,8 @@ extern "C" int dblp_policy_loss(int device, void* stream, uint64_t n_tokens, uin
         });
     if (n != 1 && !summed) {
         const u32 blocks = n ? (n + SUM_SHARE - 1) / SUM_SHARE : 1;
-        hipLaunchKernelGGL(policy_sums, dim3(blocks), dim3(1024), 0, st, (const TokenPart*)parts, n, kl_coef, shares, d_stats);
-        if (blocks > 1) hipLaunchKernelGGL(policy_join, dim3(1), dim3(256), 0, st, (const double*)shares, blocks, kl_coef, d_stats);
+        launch(policy_sums, dim3(blocks), 1024, st, (const TokenPart*)parts, n, kl_coef, shares, d_stats);
+        if (blocks > 1) launch(policy_join, dim3(1), 256, st, (const double*)shares, blocks, kl_coef, d_stats);
     }
-    return launched(call);
+    return launched(call, launch);
 }

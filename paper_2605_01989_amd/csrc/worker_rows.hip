@@ -654,6 +654,7 @@ extern "C" int dblp_embed(int device, void* stream, const int64_t* d_tokens, uin
     if (n_tokens == 0) return DBLP_OK;
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
+    Launches launch;
     by_type(table_type, [&](auto st) {
         by_type(out_type, [&](auto tt) {
             typedef decltype(st) S;
@@ -663,12 +664,12 @@ extern "C" int dblp_embed(int device, void* stream, const int64_t* d_tokens, uin
             each_launch<W>(n_tokens, dim, [&](Units s) {
                 const auto pick = [&](auto whole, auto far_out) { return m.on ? embed_units<S, T, W, true, decltype(whole)::value, decltype(far_out)::value> : embed_units<S, T, W, false, decltype(whole)::value, decltype(far_out)::value>; };
                 const auto kernel = dim % 8 ? pick(Int<0>(), Int<0>()) : far ? pick(Int<1>(), Int<1>()) : pick(Int<1>(), Int<0>());
-                hipLaunchKernelGGL(kernel, dim3(blocks_of(s.n, 256 * EMBED_EACH)), dim3(256), 0, (hipStream_t)stream, s, m, d_tokens, (const typename S::elem*)d_table, (u64)table_stride, (u64)vocab, scale,
+                launch(kernel, dim3(blocks_of(s.n, 256 * EMBED_EACH)), 256, (hipStream_t)stream, s, m, d_tokens, (const typename S::elem*)d_table, (u64)table_stride, (u64)vocab, scale,
                                    d_positions, (const typename S::elem*)d_pos_table, (u64)pos_stride, (u64)n_positions, (typename T::elem*)d_out, (u64)out_stride);
             });
         });
     });
-    return launched(call);
+    return launched(call, launch);
 }
 
 // How the places of a batch are sorted and cut, and where its intermediate results lie in the workspace.
@@ -749,6 +750,7 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
     if (const int rc = take_drop(call, h_drop, &m)) return rc;
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
+    Launches launch;
     const hipStream_t st = (hipStream_t)stream;
     // (the hint takes a copy of 154 MB from 55 to 48 us, one of 38 MB from 11 to 14)
     const bool far = vocab * dim * (d_base ? 8 : 4) > FAR_BYTES / 2 && dim % 4 == 0 && !off(d_base, 16) && !off(d_grad, 16) && base_stride % 4 == 0 && grad_stride % 4 == 0;
@@ -764,13 +766,13 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
             const auto go = [&](Units s) {
                 const u32 fill = blocks_of(s.n, 256 * SHORT_FILL);
                 if (lead + fill)
-                    hipLaunchKernelGGL(kernel, dim3(lead + fill), dim3(256), 0, st, d_tokens, n, dim, units, lead, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride);
+                    launch(kernel, dim3(lead + fill), 256, st, d_tokens, n, dim, units, lead, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride);
                 lead = 0;
             };
             if (d_base == d_grad) go(Units{0, 0, dim, Divider::by(units)});
             else each_launch<4>(vocab, dim, go);
         });
-        return launched(call);
+        return launched(call, launch);
     }
     uint8_t* const ws = (uint8_t*)d_workspace;
     u32* const n_chains = (u32*)(ws + p.n_chains);
@@ -781,21 +783,21 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
     // a table whose units do not fit one launch is written before everything else
     const bool beside = !in_place && vocab * units < COUNT_LIMIT;
     if (!in_place && !beside)
-        each_launch<4>(vocab, dim, [&](Units s) { hipLaunchKernelGGL(fill_rows, dim3(fill_blocks(s)), dim3(256), 0, st, s, out); });
+        each_launch<4>(vocab, dim, [&](Units s) { launch(fill_rows, dim3(fill_blocks(s)), 256, st, s, out); });
     Fill fill = {dim, units, 0, beside ? vocab : 0, (u64)dim * (d_base ? 8 : 4)};
     uint8_t* const present = beside && (!one_block || vocab <= MARK_MOST) ? ws + p.present : nullptr;
     int at = 0;
     if (one_block) {
         const Units s = fill.all_but(present ? FILL_PIECES + FILL_CHAINS : 0);
-        hipLaunchKernelGGL(sort_one_block, dim3(1 + fill_blocks(s, 1024)), dim3(1024), 0, st, q, d_tokens, (u32*)(ws + p.keys[0]), (u32*)(ws + p.places[0]), n_chains, present, s, out);
+        launch(sort_one_block, dim3(1 + fill_blocks(s, 1024)), 1024, st, q, d_tokens, (u32*)(ws + p.keys[0]), (u32*)(ws + p.places[0]), n_chains, present, s, out);
     } else {
         for (u32 pass = 0; pass < p.passes; ++pass, at ^= 1) {
             const SortFrom from = {pass ? nullptr : d_tokens, pass ? (u32*)(ws + p.keys[at ^ 1]) : nullptr, pass ? (u32*)(ws + p.places[at ^ 1]) : nullptr};
             const u32 clear = pass == 0 && present ? (u32)(round_up(vocab, 256) / 4) : 0;
             const Units a = fill.take(d_base ? 2 * FILL_COUNT : FILL_COUNT), b = fill.take(FILL_MOVE);
             const u32 others = fill_blocks(a) + (u32)((clear + 1023) / 1024);
-            hipLaunchKernelGGL(sort_count, dim3(p.tiles + others), dim3(256), 0, st, q, from, pass * p.bits, p.tile, p.tiles, (u32*)(ws + p.hist), n_chains, (u32*)present, clear, a, out, (const uint8_t*)(pass ? present : nullptr));
-            hipLaunchKernelGGL(sort_move, dim3(p.tiles + fill_blocks(b)), dim3(256), 0, st, q, from, pass * p.bits, p.tile, p.tiles, (const u32*)(ws + p.hist), (u32*)(ws + p.keys[at]), (u32*)(ws + p.places[at]),
+            launch(sort_count, dim3(p.tiles + others), 256, st, q, from, pass * p.bits, p.tile, p.tiles, (u32*)(ws + p.hist), n_chains, (u32*)present, clear, a, out, (const uint8_t*)(pass ? present : nullptr));
+            launch(sort_move, dim3(p.tiles + fill_blocks(b)), 256, st, q, from, pass * p.bits, p.tile, p.tiles, (const u32*)(ws + p.hist), (u32*)(ws + p.keys[at]), (u32*)(ws + p.places[at]),
                                pass == 0 ? present : (uint8_t*)nullptr, b, out, (const uint8_t*)(pass ? present : nullptr));
         }
         at ^= 1;
@@ -812,15 +814,15 @@ extern "C" int dblp_embed_grad(int device, void* stream, const int64_t* d_tokens
         const auto kernel = p.len == 8 ? by_len(Int<8>()) : by_len(Int<16>());
         each_launch<4>(p.pieces, dim, [&](Units s) {
             const u32 blocks = blocks_of(s.n, 256);
-            hipLaunchKernelGGL(kernel, dim3(blocks + fill_blocks(beside_pieces)), dim3(256), 0, st, keys, places, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride, chain, chains, n_chains, blocks, beside_pieces, (const uint8_t*)present);
+            launch(kernel, dim3(blocks + fill_blocks(beside_pieces)), 256, st, keys, places, s, out, m, (const typename T::elem*)d_dy, (u64)dy_stride, chain, chains, n_chains, blocks, beside_pieces, (const uint8_t*)present);
             beside_pieces.n = 0;
         });
     });
     const u64 most = (u64)p.pieces * ((units + 31) / 32);
     const u32 chain_blocks = most < 4096 ? (u32)most : 4096;
     const Units beside_chains = fill.take(fill.left());
-    hipLaunchKernelGGL(grad_chains, dim3(chain_blocks + fill_blocks(beside_chains)), dim3(256), 0, st, keys, p.len, p.pieces, dim, units, out, (const float*)chain, (const uint2*)chains, (const u32*)n_chains, chain_blocks, beside_chains, (const uint8_t*)present);
-    return launched(call);
+    launch(grad_chains, dim3(chain_blocks + fill_blocks(beside_chains)), 256, st, keys, p.len, p.pieces, dim, units, out, (const float*)chain, (const uint2*)chains, (const u32*)n_chains, chain_blocks, beside_chains, (const uint8_t*)present);
+    return launched(call, launch);
 }
 
 extern "C" int dblp_dropout(int device, void* stream, uint64_t rows, uint32_t cols, const void* d_x, uint64_t x_stride,
@@ -838,6 +840,7 @@ extern "C" int dblp_dropout(int device, void* stream, uint64_t rows, uint32_t co
     if (rows == 0) return DBLP_OK;
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
+    Launches launch;
     const bool far = rows * cols * type_bytes(type) * (d_residual ? 3 : 2) >= FAR_BYTES;
     by_type(type, [&](auto tt) {
         typedef decltype(tt) T;
@@ -846,8 +849,8 @@ extern "C" int dblp_dropout(int device, void* stream, uint64_t rows, uint32_t co
         each_launch<W>(rows, cols, [&](Units s) {
             const auto pick = [&](auto whole, auto past) { return d_residual ? dropout_units<T, W, true, decltype(whole)::value, decltype(past)::value> : dropout_units<T, W, false, decltype(whole)::value, decltype(past)::value>; };
             const auto kernel = cols % 8 ? pick(Int<0>(), Int<0>()) : far ? pick(Int<1>(), Int<1>()) : pick(Int<1>(), Int<0>());
-            hipLaunchKernelGGL(kernel, dim3(blocks_of(s.n, 256 * InFlight<W>::N)), dim3(256), 0, (hipStream_t)stream, s, m, (in)d_x, (u64)x_stride, (in)d_residual, (u64)residual_stride, (typename T::elem*)d_y, (u64)y_stride);
+            launch(kernel, dim3(blocks_of(s.n, 256 * InFlight<W>::N)), 256, (hipStream_t)stream, s, m, (in)d_x, (u64)x_stride, (in)d_residual, (u64)residual_stride, (typename T::elem*)d_y, (u64)y_stride);
         });
     });
-    return launched(call);
+    return launched(call, launch);
 }
