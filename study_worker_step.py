@@ -22,6 +22,7 @@ import torch
 import paper_2605_01989_amd as dblp
 
 CLIP, KL = (0.2, 0.28), 0.002
+MOST_PASSES = 1000              # of sending again in one round: more than a loss of 0.99 takes to a tolerance of 2 %
 PROMPT = 4                      # leading tokens of a sequence that are given: no answer, no loss
 
 
@@ -116,6 +117,8 @@ class Receiver:
     """One communication round: packets, losses, what is asked for again, the mean."""
 
     def __init__(self, policy, workers, loss, bound_ppm, payload=366):
+        if not 0 <= loss < 1:
+            raise ValueError(f"loss: {loss} is no share of packets of which some arrive")
         off, cnt = policy.buckets()
         self.agg = dblp.Aggregator(workers, policy.n, payload, off, cnt)
         self.workers, self.loss, self.bound = workers, loss, bound_ppm
@@ -125,6 +128,7 @@ class Receiver:
         self.list = torch.empty(n, dtype=torch.int64, device="cuda")
         self.missing = torch.empty(workers * len(off), dtype=torch.int32, device="cuda")
         self.mean = torch.empty(policy.n, device="cuda")
+        self.of_worker = torch.arange(workers, device="cuda").repeat_interleave(self.agg.n_pkts)
         self.gen = torch.Generator(device="cuda").manual_seed(77)
 
     def arrivals(self, of_worker):
@@ -139,10 +143,10 @@ class Receiver:
         agg.begin_round(number)
         for w, g in enumerate(grads):
             agg.packetize(w, number, g, 0, 0, agg.n_pkts, self.packets, self.src, slot_base=w * agg.n_pkts)
-        queue = self.arrivals(torch.arange(self.workers, device="cuda").repeat_interleave(agg.n_pkts))
+        queue = self.arrivals(self.of_worker)
         agg.apply_arrivals_queue(self.packets, n, queue)
         again = 0
-        while True:
+        for _ in range(MOST_PASSES):
             count, met, _ = agg.loss_account(self.bound, self.missing, self.list)
             if met:
                 break
@@ -151,6 +155,8 @@ class Receiver:
             queue = self.arrivals(self.list[:count] >> 32)
             if queue.numel():
                 agg.apply_arrivals_queue(self.packets, count, queue)
+        else:
+            raise RuntimeError(f"round {number}: after {MOST_PASSES} passes of sending again {count} packets are missing still")
         agg.finalize(self.mean)
         return again, agg.phase_signal()[0]
 
