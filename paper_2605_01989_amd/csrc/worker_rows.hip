@@ -122,8 +122,9 @@ __global__ __launch_bounds__(256) void embed_units(Units s, Mask m, const int64_
 // (stably: a row is summed in the order of its places) and the sorted list is cut into pieces of equal length.  Every value of dy is read
 // once and every row of the result written once, by whichever launch has the memory idle: the rows without a token are most of the bytes.
 // 8192 x 768 16-bit values on a base of 50257 rows: 71 us (sort 47, of which 22 alone, with 263 of the 309 MB beside it; pieces 18, chains 7), 4.5 TB/s where a
-// large copy reaches 5.4.  65536 x 1024, no base: 100 us (four launches of sort 33, pieces 54, chains 10), 3.4 TB/s: what is left is that pieces take
-// two to four steps of eight rows one after the other, five waves a SIMD (six, with registers spilled, 106 us).
+// large copy reaches 5.4.  65536 x 1024, no base: 100 us (four launches of sort 38, pieces 52, chains 10), 3.4 TB/s: what is left is that pieces take
+// two to four steps of eight rows one after the other, five waves a SIMD of 16-bit values under a mask (six, with registers spilled, 106 us).  Floats take 86 to 137 registers, three to five waves:
+// 8192 x 768 on a base 75 us where the bytes take 62, 65536 x 1024 116 where they take 88.
 // ------------------------------------------------------------------------------------------
 // far: base and gradient are more than the memory-side cache should hold, and lie on multiples of 16 bytes
 struct Result { const float* base; u64 base_stride; float* grad; u64 grad_stride; u64 vocab; float scale; bool far; };
