@@ -45,60 +45,55 @@ __device__ __forceinline__ float gated(int act, float z, float dy) {
 // ------------------------------------------------------------------------------------------
 // what becomes of a product's sums
 // ------------------------------------------------------------------------------------------
-struct Bias { const void* p; int type; };
+// A matrix of a type that is known when the kernel runs: four columns of a row.
+struct Matrix { void* p; u64 stride; };
 
-__device__ __forceinline__ void bias4(const Bias& b, u32 n, u32 cols, float (&v)[4]) {
-    if (!b.p) { v[0] = v[1] = v[2] = v[3] = 0.0f; return; }
-    if (b.type == DBLP_F32) get4<F32>((const float*)b.p, n, cols, v);
-    else if (b.type == DBLP_BF16) get4<BF16>((const __bf16*)b.p, n, cols, v);
-    else get4<F16>((const _Float16*)b.p, n, cols, v);
+__device__ __forceinline__ void load4(int type, const void* p, u64 at, u32 left, float (&v)[4]) {
+    if (type == DBLP_F32) get4<F32>((const float*)p + at, 0, left, v);
+    else if (type == DBLP_BF16) get4<BF16>((const __bf16*)p + at, 0, left, v);
+    else get4<F16>((const _Float16*)p + at, 0, left, v);
+}
+__device__ __forceinline__ void store4(int type, void* p, u64 at, u32 left, const float (&v)[4]) {
+    if (type == DBLP_F32) store_cols<Vec<F32, 4>, 4>((float*)p + at, 0, left, v);
+    else if (type == DBLP_BF16) store_cols<Vec<BF16, 4>, 4>((__bf16*)p + at, 0, left, v);
+    else store_cols<Vec<F16, 4>, 4>((_Float16*)p + at, 0, left, v);
 }
 
-template <class T> struct LayerOut {
-    typedef typename T::elem elem;
-    Bias bias;
-    int act;
-    const elem* residual;
-    u64 residual_stride;
-    elem* y;
-    u64 y_stride;
-    elem* z;
-    u64 z_stride;
+struct LayerOut {
+    int type, act, bias_type;
+    const void* bias;
+    Matrix residual, y, z;
     __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc) const {
-        float v[4], b[4];
-        bias4(bias, n, cols, b);
-        for (int i = 0; i < 4; ++i) v[i] = acc[i] + b[i];
-        if (z) store_cols<Vec<T, 4>, 4>(z + m * z_stride, n, cols, v);
-        for (int i = 0; i < 4; ++i) v[i] = act_of(act, v[i]);
-        if (residual) {
-            get4<T>(residual + m * residual_stride, n, cols, b);
+        float v[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4];
+        if (bias) {
+            load4(bias_type, bias, n, cols - n, b);
             for (int i = 0; i < 4; ++i) v[i] += b[i];
         }
-        store_cols<Vec<T, 4>, 4>(y + m * y_stride, n, cols, v);
+        if (z.p) store4(type, z.p, m * z.stride + n, cols - n, v);
+        for (int i = 0; i < 4; ++i) v[i] = act_of(act, v[i]);
+        if (residual.p) {
+            load4(type, residual.p, m * residual.stride + n, cols - n, b);
+            for (int i = 0; i < 4; ++i) v[i] += b[i];
+        }
+        store4(type, y.p, m * y.stride + n, cols - n, v);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
 
-template <class T> struct GateOut {
-    typedef typename T::elem elem;
-    int act;
-    const elem* z;
-    u64 z_stride;
-    const elem* base;
-    u64 base_stride;
-    elem* dx;
-    u64 dx_stride;
+struct GateOut {
+    int type, act;
+    Matrix z, base, dx;
     __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc) const {
         float v[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4];
-        if (z) {
-            get4<T>(z + m * z_stride, n, cols, b);
+        if (z.p) {
+            load4(type, z.p, m * z.stride + n, cols - n, b);
             for (int i = 0; i < 4; ++i) v[i] = gated(act, b[i], v[i]);
         }
-        if (base) {
-            get4<T>(base + m * base_stride, n, cols, b);
+        if (base.p) {
+            load4(type, base.p, m * base.stride + n, cols - n, b);
             for (int i = 0; i < 4; ++i) v[i] += b[i];
         }
-        store_cols<Vec<T, 4>, 4>(dx + m * dx_stride, n, cols, v);
+        store4(type, dx.p, m * dx.stride + n, cols - n, v);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
@@ -118,7 +113,7 @@ struct WeightOut {
         }
         store_cols<Vec<F32, 4>, 4>(dw + m * dw_stride, n, cols, v);
     }
-    __device__ __forceinline__ void sums(u32, u32, u32 m, float s) const { dbias[m] = bias_base ? bias_base[m] + s : s; }
+    __device__ __forceinline__ void sums(u32, u32, u32 m, float s) const { if (dbias) dbias[m] = bias_base ? bias_base[m] + s : s; }
 };
 
 // ------------------------------------------------------------------------------------------
@@ -153,25 +148,25 @@ template <class T, bool P_BY_K, bool Q_BY_K, bool SUMS, class Out>
 static void products(Launches& launch, hipStream_t stream, Product a, Out out) {
     a.part = (u32)round_up(a.depth ? a.depth : 1, 64);
     a.parts = 1;
-    const auto go = [&](auto bm, auto bn) {
-        constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
-        each_tiles<BM, BN>(a.rows, a.cols, 1, 1, [&](u64 tile0, u32 tile_cols, dim3 grid, u64) {
-            a.tile0 = tile0;
-            a.tile_cols = tile_cols;
-            launch(tile_products<T, P_BY_K, Q_BY_K, BM, BN, SUMS, Out>, grid, TILE_THREADS, stream, a, out);
+    const u64 area = (u64)a.rows * a.cols;
+    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) {
+        each_tiles<64, 64>(a, 1, [&](const Product& p, dim3 grid, u64) { launch(tile_products<T, P_BY_K, Q_BY_K, 64, 64, SUMS, Out>, grid, TILE_THREADS, stream, p, out); });
+        return;
+    }
+    const auto go = [&](auto n, auto p_staged, auto q_staged) {
+        constexpr int N = decltype(n)::value;
+        each_tiles<32 * N, 32 * N>(a, 1, [&](const Product& p, dim3 grid, u64) {
+            launch(ring_products<T, P_BY_K, Q_BY_K, decltype(p_staged)::value, decltype(q_staged)::value, N, N, SUMS, Out>, grid, 256, stream, p, out);
         });
     };
-    if ((u64)a.rows * a.cols < (u64)256 * 128 * 128) go(Int<64>(), Int<64>());
-    else go(Int<128>(), Int<128>());
-}
-
-// The result's type: the operands' or floats.
-template <class F>
-static void by_types(int type, int out_type, F f) {
-    by_type(type, [&](auto t) {
-        if (out_type == type) f(t, t);
-        else if constexpr (sizeof(typename decltype(t)::elem) == 2) f(t, F32());
-    });
+    const auto by_rows = [&](auto n) {
+        const bool p = in_chunks<T>(a.P), q = in_chunks<T>(a.Q);
+        if (p && q) go(n, Int<0>(), Int<0>());
+        else if (q) go(n, Int<1>(), Int<0>());
+        else go(n, Int<1>(), Int<1>());
+    };
+    if (area < (u64)256 * 128 * 128) by_rows(Int<2>());
+    else by_rows(Int<4>());
 }
 
 extern "C" int dblp_linear(int device, void* stream, uint64_t n_tokens, uint32_t in, uint32_t out, const void* d_x, uint64_t x_stride,
@@ -194,12 +189,9 @@ extern "C" int dblp_linear(int device, void* stream, uint64_t n_tokens, uint32_t
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
     Launches launch;
-    by_types(type, out_type, [&](auto tt, auto ot) {
-        typedef decltype(tt) T;
-        typedef decltype(ot) O;
-        typedef typename O::elem elem;
-        const LayerOut<O> o = {{d_bias, bias_type}, activation, (const elem*)d_residual, residual_stride, (elem*)d_y, y_stride, (elem*)d_z, z_stride};
-        products<T, false, false, false>(launch, (hipStream_t)stream, Product{{d_x, x_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, out, in, 0, 0, 0, 0}, o);
+    const LayerOut o = {out_type, activation, bias_type, d_bias, {(void*)d_residual, residual_stride}, {d_y, y_stride}, {d_z, z_stride}};
+    by_type(type, [&](auto tt) {
+        products<decltype(tt), false, false, false>(launch, (hipStream_t)stream, Product{{d_x, x_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, out, in}, o);
     });
     return launched(call, launch);
 }
@@ -224,12 +216,9 @@ extern "C" int dblp_linear_grad_input(int device, void* stream, uint64_t n_token
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
     Launches launch;
-    by_types(type, out_type, [&](auto tt, auto ot) {
-        typedef decltype(tt) T;
-        typedef decltype(ot) O;
-        typedef typename O::elem elem;
-        const GateOut<O> o = {activation, (const elem*)d_z, z_stride, (const elem*)d_base, base_stride, (elem*)d_dx, dx_stride};
-        products<T, false, true, false>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, in, out, 0, 0, 0, 0}, o);
+    const GateOut o = {out_type, activation, {(void*)d_z, z_stride}, {(void*)d_base, base_stride}, {d_dx, dx_stride}};
+    by_type(type, [&](auto tt) {
+        products<decltype(tt), false, true, false>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, in, out}, o);
     });
     return launched(call, launch);
 }
@@ -253,13 +242,9 @@ extern "C" int dblp_linear_grad_weight(int device, void* stream, uint64_t n_toke
     OnDevice on(device);
     if (on.err != hipSuccess) return no_device(call, on.err);
     Launches launch;
+    const WeightOut o = {d_base, base_stride, d_dw, dw_stride, d_bias_base, d_dbias};
     by_type(type, [&](auto tt) {
-        typedef decltype(tt) T;
-        const WeightOut o = {d_base, base_stride, d_dw, dw_stride, d_bias_base, d_dbias};
-        // (without a column of dw there is one tile for each of the bias' rows all the same: of no column, nothing is put)
-        const Product a = {{d_dy, dy_stride, 0}, {d_x, x_stride, 0}, out, in, (u32)n_tokens, 0, 0, 0, 0};
-        if (d_dbias) products<T, true, true, true>(launch, (hipStream_t)stream, a, o);
-        else products<T, true, true, false>(launch, (hipStream_t)stream, a, o);
+        products<decltype(tt), true, true, true>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_x, x_stride, 0}, out, in, (u32)n_tokens}, o);
     });
     return launched(call, launch);
 }

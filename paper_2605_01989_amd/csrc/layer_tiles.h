@@ -42,7 +42,8 @@ struct Operand { const void* p; u64 stride, step; };
 struct Product {
     Operand P, Q;
     u32 rows, cols, depth, tile_cols, part, parts;   // part: k of one part, a multiple of 64; tile_cols: tiles of a row of tiles
-    u64 tile0;                                       // first tile of this launch
+    u32 tile_rows;
+    u64 tiles, tile0;                                // of the whole result; first one of this launch
 };
 
 #define TILE_THREADS 256
@@ -159,6 +160,281 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out
     }
 }
 
+// ------------------------------------------------------------------------------------------
+// The same products with operands copied from memory to LDS past the registers.
+//
+// LDS holds four steps of 64 bytes of k (32 16-bit values, 16 floats).  While a step's fragments are multiplied, those of the next are read from LDS and the step
+// four further on is on its way into the place that the present one has left: one barrier a step, and a step's copies have three steps' time.
+// A copy writes 64 lanes' 16 bytes one after the other, so an order in LDS other than memory's is made by what each lane asks for:
+//   by rows  a row is 64 bytes, chunk c of row r at place c ^ (r / 2 & 3): eight rows' chunks, which eight lanes read at once, lie in all banks.
+//   by k     a row is one k of BT rows, in granules of 16 rows; granule g of k lies at g ^ turn(k), so that the rows of k that one transposing read of four k
+//            takes lie in different banks.  16-bit values are transposed on the way out (ds_read_b64_tr_b16: of 16 lanes with
+//            four values each, lane i gets value i % 4 of lanes i / 4, i / 4 + 4, ...), floats are read one by one.
+// ------------------------------------------------------------------------------------------
+#define RING 4
+#define STEP_BYTES 64
+
+typedef u32 rsrc_t __attribute__((ext_vector_type(4)));
+#define PAST_ALL 0x80000000u                     // an offset that no buffer here reaches: a copy of it writes zeros
+
+// 64 lanes' 16 bytes at `offset` of a buffer to 1024 bytes of LDS at `to`.  No register is written, so nothing can be overwritten by it, and the compiler waits
+// for it nowhere: by a builtin it would before each read of LDS.  m0 is nobody's else in these kernels.
+__device__ __forceinline__ void copy_to_lds(rsrc_t from, u32 offset, u32 to) {
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from));
+}
+template <int N> __device__ __forceinline__ void arrived_and_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ u32 lds_address(const void* p) { return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
+
+// An operand's way to LDS: BT rows and 64 bytes of k a step, shared by four waves.  STAGED: through registers, for rows that do not begin at multiples of 16 bytes.
+template <class T, int BT, bool BY_K, bool STAGED>
+struct Feed {
+    typedef typename T::elem elem;
+    static constexpr u32 E = 16 / sizeof(elem), KS = STEP_BYTES / sizeof(elem);   // elements of a chunk, k of a step
+    static constexpr u32 BYTES = BT * STEP_BYTES, N = BYTES / 4096;               // of a step; copies of a wave
+    static constexpr u32 ROW = BY_K ? BT * sizeof(elem) : STEP_BYTES, CG = sizeof(elem);   // bytes of a row in LDS; chunks of 16 values
+    static constexpr u32 COPIES = STAGED ? 0 : N;
+    typedef Vec<T, E> V;
+
+    const elem* base;            // of the block's first row, at the step that is copied next
+    u64 left;                    // bytes from there to the operand's end
+    u64 stride;
+    u32 k, depth;                // of that step; end of the sum
+    u32 rows;                    // of the operand from the block's first
+    u32 offset[N], kk[N];        // a lane's chunk: from the base, its first k in a step
+    u32 r[N];                    // its row
+    u32 wave;
+    u4v v[STAGED ? N : 1];
+
+    static __device__ __forceinline__ u32 turn(u32 k) {
+        const u32 t = sizeof(elem) == 2 ? (k & 3) | (k >> 3 & 1) << 2 : k >> 2 & 3;
+        return t & (BT / 16 - 1);
+    }
+    __device__ __forceinline__ Feed(const elem* p, u64 stride_, u32 row0, u32 rows_, u32 k0, u32 depth_) : stride(stride_), k(k0), depth(depth_), rows(rows_ - row0) {
+        base = p + (BY_K ? (u64)k0 * stride + row0 : (u64)row0 * stride + k0);
+        left = (BY_K ? (u64)(depth - 1 - k0) * stride + rows : (u64)(rows - 1) * stride + depth - k0) * sizeof(elem);
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const u32 lane = threadIdx.x & 63;
+#pragma unroll
+        for (u32 i = 0; i < N; ++i) {
+            const u32 at = (wave * N + i) * 1024 + lane * 16, line = at / ROW, place = at % ROW / 16;
+            if (BY_K) {
+                const u32 chunk = (place / CG ^ turn(line)) * CG + place % CG;
+                kk[i] = line;
+                r[i] = chunk * E;
+                offset[i] = (u32)(line * stride + (r[i] < rows ? r[i] : 0)) * sizeof(elem);      // (a chunk of rows past the end: any)
+            } else {
+                const u32 chunk = place ^ (line >> 1 & 3);
+                kk[i] = chunk * E;
+                r[i] = line < rows ? line : rows - 1;
+                offset[i] = (u32)(r[i] * stride + kk[i]) * sizeof(elem);
+            }
+        }
+    }
+    __device__ __forceinline__ void next() {
+        const u64 by = BY_K ? KS * stride : KS;
+        base += by;
+        left -= by * sizeof(elem);
+        k += KS;
+    }
+    // The step's copy number i of this wave, to LDS at `to`; k past the end as zeros.
+    __device__ __forceinline__ void copy(u32 i, u32 to) const {
+        const u64 at = (u64)base;
+        const u32 bytes = left < PAST_ALL - 16 ? ((u32)left + 15) & ~15u : PAST_ALL;      // (a chunk that begins inside ends in the same 16 bytes of memory)
+        const rsrc_t from = {(u32)at, (u32)(at >> 32), k < depth ? bytes : 0, 0x00020000u};
+        u32 o = offset[i];
+        if (k < depth && depth - k < KS) o = kk[i] < depth - k ? o : PAST_ALL;
+        copy_to_lds(from, o, to + (wave * N + i) * 1024);
+    }
+    // Through registers: asked for, and put down later.
+    __device__ __forceinline__ void ask(u32 i) {
+        if (k >= depth) return;
+        const u32 n = depth - k;
+        const elem* const at = base + offset[i] / sizeof(elem);
+        v[i] = (u4v)(0u);
+        if (BY_K) {
+            if (kk[i] < n && r[i] < rows) v[i] = __builtin_bit_cast(u4v, r[i] + E <= rows ? V::load(at) : V::some(at, rows - r[i]));
+        } else if (kk[i] < n) {
+            v[i] = __builtin_bit_cast(u4v, kk[i] + E <= n ? V::load(at) : V::some(at, n - kk[i]));
+        }
+    }
+    __device__ __forceinline__ void put(u32 i, uint8_t* step) const { *(u4v*)(step + (wave * N + i) * 1024 + (threadIdx.x & 63) * 16) = v[i]; }
+    // A chunk that holds the end of the sum, in a row whose k do not end with it: zeros behind.  Done by who copied it.
+    __device__ __forceinline__ void trim(uint8_t* step, u32 n) const {
+        if (BY_K || STAGED) return;
+#pragma unroll
+        for (u32 i = 0; i < N; ++i)
+            for (u32 e = 1; e < E; ++e)
+                if (kk[i] < n && kk[i] + e >= n) *(elem*)(step + (wave * N + i) * 1024 + (threadIdx.x & 63) * 16 + e * sizeof(elem)) = (elem)0.0f;
+    }
+};
+
+// A wave's fragments of an operand: 16 rows each, from row w0 of the tile.
+template <class T, int BT, bool BY_K>
+struct Reader {
+    typedef typename T::elem elem;
+    typedef Feed<T, BT, BY_K, false> F;
+    u32 base, w0, t;
+    __device__ __forceinline__ explicit Reader(u32 w) : w0(w) {
+        const u32 lane = threadIdx.x & 63, group = lane >> 4, in = lane & 15;
+        if (!BY_K) base = (w + in) * STEP_BYTES + ((group ^ (in >> 1 & 3)) << 4);
+        else if (sizeof(elem) == 2) base = (8 * group + (in >> 2)) * F::ROW + (in & 3) * 8;
+        else base = 4 * group * F::ROW + in * 4;
+        t = sizeof(elem) == 2 ? F::turn(8 * group + (in >> 2)) : F::turn(4 * group);
+    }
+    __device__ __forceinline__ u4v get(const uint8_t* step, u32 i) const {
+        if (!BY_K) return *(const u4v*)(step + base + i * 16 * STEP_BYTES);
+        const uint8_t* const at = step + base + (((w0 / 16 + i) ^ t) << (sizeof(elem) == 2 ? 5 : 6));
+        if (sizeof(elem) == 2) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4* lds;
+            const u2v a = __builtin_bit_cast(u2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(at))), b = __builtin_bit_cast(u2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(at + 4 * F::ROW)));
+            return (u4v){a.x, a.y, b.x, b.y};
+        }
+        u4v v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = *(const u32*)(at + j * F::ROW);
+        return v;
+    }
+};
+
+// Block number b's tile.  Blocks go to the eight dies in turn; each die gets tiles that lie together, rows of tiles in bands of eight, so that its L2 holds
+// what its blocks read at the same time.
+__device__ __forceinline__ void tile_of(u64 b, u64 n, u32 tile_rows, u32 tile_cols, u32& m, u32& c) {
+    const u64 each = n / 8, more = n % 8, die = b % 8;
+    const u64 id = die * each + (die < more ? die : more) + b / 8;
+    const u64 band = id / (8ull * tile_cols), in_band = id % (8ull * tile_cols);
+    const u32 first = (u32)band * 8, high = tile_rows - first < 8 ? tile_rows - first : 8;
+    m = first + (u32)(in_band % high);
+    c = (u32)(in_band / high);
+}
+
+// Four waves, two by two, each 16 NM x 16 NN of the tile.
+template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, int NM, int NN, bool SUMS, class Out>
+__global__ __launch_bounds__(256, NM * NN > 16 ? 1 : 2) void ring_products(Product a, Out out) {
+    typedef typename T::elem elem;
+    constexpr int BM = 32 * NM, BN = 32 * NN;
+    typedef Feed<T, BM, P_BY_K, P_STAGED> FP;
+    typedef Feed<T, BN, Q_BY_K, Q_STAGED> FQ;
+    constexpr u32 KS = FP::KS, STEP = FP::BYTES + FQ::BYTES, COPIES = FP::COPIES + FQ::COPIES;
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[RING * STEP];
+    u32 tm, tn;
+    tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, a.tile_cols, tm, tn);
+    const u32 m0 = tm * BM, n0 = tn * BN;
+    const u32 matrix = blockIdx.z / a.parts, part = blockIdx.z % a.parts;
+    const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, in_group = lane & 15;
+    const u32 wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+    const u32 k_first = part * a.part, k_end = a.depth - k_first > a.part ? k_first + a.part : a.depth;
+    const u32 steps = (k_end - k_first + KS - 1) / KS;
+    const bool summing = SUMS && n0 == 0 && wn == 0;
+    f4 acc[NM][NN] = {}, sum[SUMS ? NM : 1] = {};
+    FP fp((const elem*)a.P.p + matrix * a.P.step, a.P.stride, m0, a.rows, k_first, k_end);
+    FQ fq((const elem*)a.Q.p + matrix * a.Q.step, a.Q.stride, n0, a.cols, k_first, k_end);
+    const Reader<T, BM, P_BY_K> rp(wm);
+    const Reader<T, BN, Q_BY_K> rq(wn);
+    const u32 ring_at = __builtin_amdgcn_readfirstlane(lds_address(ring));
+    const auto copy = [&](u32 slot) {
+        if (!P_STAGED)
+#pragma unroll
+            for (u32 i = 0; i < FP::N; ++i) fp.copy(i, ring_at + slot * STEP);
+        if (!Q_STAGED)
+#pragma unroll
+            for (u32 i = 0; i < FQ::N; ++i) fq.copy(i, ring_at + slot * STEP + FP::BYTES);
+    };
+    const auto ask = [&] {
+        if (P_STAGED)
+#pragma unroll
+            for (u32 i = 0; i < FP::N; ++i) fp.ask(i);
+        if (Q_STAGED)
+#pragma unroll
+            for (u32 i = 0; i < FQ::N; ++i) fq.ask(i);
+    };
+    const auto put = [&](u32 slot) {
+        if (P_STAGED)
+#pragma unroll
+            for (u32 i = 0; i < FP::N; ++i) fp.put(i, ring + slot * STEP);
+        if (Q_STAGED)
+#pragma unroll
+            for (u32 i = 0; i < FQ::N; ++i) fq.put(i, ring + slot * STEP + FP::BYTES);
+    };
+    const auto next_copied = [&] { if (!P_STAGED) fp.next(); if (!Q_STAGED) fq.next(); };
+    const auto next_asked = [&] { if (P_STAGED) fp.next(); if (Q_STAGED) fq.next(); };
+    const auto trim = [&](u32 step) {              // of the last step, where it does not end with a chunk
+        const u32 n = k_end - k_first - step * KS;
+        if (n >= KS || n % (16 / sizeof(elem)) == 0) return;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        fp.trim(ring + step % RING * STEP, n);
+        fq.trim(ring + step % RING * STEP + FP::BYTES, n);
+    };
+    u4v b[2][NM], c[2][NN];
+    if (steps) {
+        for (u32 i = 0; i < RING; ++i) {
+            copy(i);
+            next_copied();
+        }
+        for (u32 i = 0; i < 2; ++i) {
+            ask();
+            put(i);
+            next_asked();
+        }
+        ask();
+        next_asked();
+        if (steps == 1) trim(0);
+        arrived_and_barrier<3 * COPIES>();
+#pragma unroll
+        for (int i = 0; i < NM; ++i) b[0][i] = rp.get(ring, i);
+#pragma unroll
+        for (int j = 0; j < NN; ++j) c[0][j] = rq.get(ring + FP::BYTES, j);
+    }
+    const auto step = [&](u32 s, const u4v (&b)[NM], const u4v (&c)[NN], u4v (&b1)[NM], u4v (&c1)[NN]) {
+        if (s + 2 == steps) trim(s + 1);
+        arrived_and_barrier<2 * COPIES>();
+        const u32 here = s % RING, then = (s + 1) % RING;
+        copy(here);
+        next_copied();
+        put((s + 2) % RING);
+        ask();
+        next_asked();
+#pragma unroll
+        for (int i = 0; i < NM; ++i) b1[i] = rp.get(ring + then * STEP, i);
+#pragma unroll
+        for (int j = 0; j < NN; ++j) c1[j] = rq.get(ring + then * STEP + FP::BYTES, j);
+#pragma unroll
+        for (int j = 0; j < NN; ++j)
+#pragma unroll
+            for (int i = 0; i < NM; ++i) acc[i][j] = mfma<T>(c[j], b[i], acc[i][j]);
+        if (SUMS && summing)
+#pragma unroll
+            for (int i = 0; i < NM; ++i) sum[i] = mfma<T>(ones<T>(), b[i], sum[i]);
+    };
+    for (u32 s = 0; s < steps; s += 2) {
+        step(s, b[0], c[0], b[1], c[1]);
+        if (s + 1 < steps) step(s + 1, b[1], c[1], b[0], c[0]);
+    }
+    // the result's tile through LDS, a quarter of a wave's rows at a time: rows leave whole, and what is done with them stands here once
+    arrived_and_barrier<0>();
+    constexpr u32 WIDTH = 16 * NN, LINE = WIDTH * 4 + 16;                            // (16 bytes more: the four rows of a lane's group in different banks)
+    uint8_t* const mine = ring + wave * (RING * STEP / 4);
+    constexpr int AT_ONCE = NM * 16 * LINE <= RING * STEP / 4 ? NM : NM / 2 * 16 * LINE <= RING * STEP / 4 ? NM / 2 : NM / 4;
+#pragma unroll
+    for (int i0 = 0; i0 < NM; i0 += AT_ONCE) {
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+            for (int j = 0; j < NN; ++j) *(f4*)(mine + (i * 16 + in_group) * LINE + (j * 16 + group * 4) * 4) = acc[i0 + i][j];
+        for (u32 u = lane; u < AT_ONCE * 16 * (WIDTH / 4); u += 64) {
+            const u32 line = u / (WIDTH / 4), q = u % (WIDTH / 4) * 4, m = m0 + wm + i0 * 16 + line, n = n0 + wn + q;
+            if (m < a.rows && n < a.cols) out.put(matrix, part, m, n, a.cols, *(const f4*)(mine + line * LINE + q * 4));
+        }
+    }
+    if (SUMS && summing && group == 0)
+#pragma unroll
+        for (int i = 0; i < NM; ++i)
+            if (m0 + wm + i * 16 + in_group < a.rows) out.sums(matrix, part, m0 + wm + i * 16 + in_group, sum[i][0]);
+}
+
 // Columns [n, n + 4) of a row, as floats.
 template <class T>
 __device__ __forceinline__ void get4(const typename T::elem* row, u32 n, u32 cols, float (&v)[4]) {
@@ -169,11 +445,20 @@ __device__ __forceinline__ void get4(const typename T::elem* row, u32 n, u32 col
 // Launches of a product's tiles: at most 2^20 tiles and 2^15 matrices' parts each (a grid's threads stay below 2^32, its z below 2^16).  Rows
 // have a tile even where there is no column: for their own sums.
 template <int BM, int BN, class F>
-static void each_tiles(u32 rows, u32 cols, u32 parts, u64 matrices, F f) {
-    const u64 tile_cols = cols ? (cols + (u64)BN - 1) / BN : 1, tiles = (rows + (u64)BM - 1) / BM * tile_cols;
-    for (u64 m = 0; m < matrices; m += 32768 / parts) {
-        const u64 here = matrices - m < 32768 / parts ? matrices - m : 32768 / parts;
-        for (u64 t = 0; t < tiles; t += 1u << 20)
-            f(t, (u32)tile_cols, dim3((u32)(tiles - t < (1u << 20) ? tiles - t : 1u << 20), 1, (u32)here * parts), m);
+static void each_tiles(Product a, u64 matrices, F f) {
+    a.tile_cols = a.cols ? (u32)((a.cols + (u64)BN - 1) / BN) : 1;
+    a.tile_rows = (u32)((a.rows + (u64)BM - 1) / BM);
+    a.tiles = (u64)a.tile_rows * a.tile_cols;
+    for (u64 m = 0; m < matrices; m += 32768 / a.parts) {
+        const u64 here = matrices - m < 32768 / a.parts ? matrices - m : 32768 / a.parts;
+        for (a.tile0 = 0; a.tile0 < a.tiles; a.tile0 += 1u << 20)
+            f(a, dim3((u32)(a.tiles - a.tile0 < (1u << 20) ? a.tiles - a.tile0 : 1u << 20), 1, (u32)here * a.parts), m);
     }
 }
+
+// Whether an operand can be copied to LDS chunk by chunk, and whether a tile's offsets fit 31 bits.
+template <class T> static bool in_chunks(const Operand& o) {
+    const u64 e = sizeof(typename T::elem);
+    return !off(o.p, 16) && o.stride * e % 16 == 0 && o.step * e % 16 == 0;
+}
+template <class T> static bool in_reach(const Operand& o) { return o.stride < (1ull << 31) / 256 / sizeof(typename T::elem); }

@@ -212,10 +212,12 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
     const auto product = [&](auto p_by_k, auto q_by_k, Operand P, Operand Q, u32 m_rows, u32 m_cols, u32 depth, auto out) {
         constexpr bool PK = decltype(p_by_k)::value, QK = decltype(q_by_k)::value;
         typedef decltype(out) Out;
-        each_tiles<64, 64>(m_rows, m_cols, 1, count, [&](u64 tile0, u32 tile_cols, dim3 grid, u64 m) {
+        const Product a = {P, Q, m_rows, m_cols, depth, 0, (u32)round_up(depth, 64), 1};
+        each_tiles<64, 64>(a, count, [&](Product p, dim3 grid, u64 m) {
             out.matrix0 = m;
-            const Operand p = {(const float*)P.p + m * P.step, P.stride, P.step}, q = {(const float*)Q.p + m * Q.step, Q.stride, Q.step};
-            launch(tile_products<F32, PK, QK, 64, 64, false, Out>, grid, TILE_THREADS, st, Product{p, q, m_rows, m_cols, depth, tile_cols, (u32)round_up(depth, 64), 1, tile0}, out);
+            p.P.p = (const float*)P.p + m * P.step;
+            p.Q.p = (const float*)Q.p + m * Q.step;
+            launch(tile_products<F32, PK, QK, 64, 64, false, Out>, grid, TILE_THREADS, st, p, out);
         });
     };
     by_type(out_type, [&](auto tt) {
