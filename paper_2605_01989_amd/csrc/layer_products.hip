@@ -153,20 +153,21 @@ static void products(Launches& launch, hipStream_t stream, Product a, Out out) {
         each_tiles<64, 64>(a, 1, [&](const Product& p, dim3 grid, u64) { launch(tile_products<T, P_BY_K, Q_BY_K, 64, 64, SUMS, Out>, grid, TILE_THREADS, stream, p, out); });
         return;
     }
-    const auto go = [&](auto n, auto p_staged, auto q_staged) {
-        constexpr int N = decltype(n)::value;
-        each_tiles<32 * N, 32 * N>(a, 1, [&](const Product& p, dim3 grid, u64) {
-            launch(ring_products<T, P_BY_K, Q_BY_K, decltype(p_staged)::value, decltype(q_staged)::value, N, N, SUMS, Out>, grid, 256, stream, p, out);
+    const auto go = [&](auto waves, auto p_staged, auto q_staged) {
+        typedef decltype(waves) W;
+        each_tiles<W::BM, W::BN>(a, 1, [&](const Product& p, dim3 grid, u64) {
+            launch(ring_products<T, P_BY_K, Q_BY_K, decltype(p_staged)::value, decltype(q_staged)::value, W, SUMS && (W::ALL == 4), Out>, grid, 64 * W::ALL, stream, p, out);
         });
     };
-    const auto by_rows = [&](auto n) {
+    const auto by_rows = [&](auto waves) {
         const bool p = in_chunks<T>(a.P), q = in_chunks<T>(a.Q);
-        if (p && q) go(n, Int<0>(), Int<0>());
-        else if (q) go(n, Int<1>(), Int<0>());
-        else go(n, Int<1>(), Int<1>());
+        if (p && q) go(waves, Int<0>(), Int<0>());
+        else if (q) go(waves, Int<1>(), Int<0>());
+        else go(waves, Int<1>(), Int<1>());
     };
-    if (area < (u64)256 * 128 * 128) by_rows(Int<2>());
-    else by_rows(Int<4>());
+    if (area < (u64)256 * 128 * 128) by_rows(Waves<2, 2, 2, 2, 3>());
+    else if (sizeof(typename T::elem) == 4 || area < (u64)200 * 256 * 256) by_rows(Waves<2, 2, 4, 4, 2>());
+    else if constexpr (sizeof(typename T::elem) == 2) by_rows(Waves<2, 4, 8, 4, 2>());
 }
 
 extern "C" int dblp_linear(int device, void* stream, uint64_t n_tokens, uint32_t in, uint32_t out, const void* d_x, uint64_t x_stride,

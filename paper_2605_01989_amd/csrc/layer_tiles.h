@@ -163,16 +163,16 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out
 // ------------------------------------------------------------------------------------------
 // The same products with operands copied from memory to LDS past the registers.
 //
-// LDS holds four steps of 64 bytes of k (32 16-bit values, 16 floats).  While a step's fragments are multiplied, those of the next are read from LDS and the step
-// four further on is on its way into the place that the present one has left: one barrier a step, and a step's copies have three steps' time.
+// LDS holds RING stages of 128 bytes of k (64 16-bit values, 32 floats): whole lines of memory.  A stage is multiplied in two halves, and while one half's
+// fragments are multiplied the next half's are read from LDS.  Behind the barrier between the halves nothing of the stage is read any more: a later stage
+// is copied into its place, and has two halves' time to arrive.
 // A copy writes 64 lanes' 16 bytes one after the other, so an order in LDS other than memory's is made by what each lane asks for:
-//   by rows  a row is 64 bytes, chunk c of row r at place c ^ (r / 2 & 3): eight rows' chunks, which eight lanes read at once, lie in all banks.
+//   by rows  a row is 128 bytes, chunk c of row r at place c ^ (r & 7): eight rows' chunks, which eight lanes read at once, lie in all banks.
 //   by k     a row is one k of BT rows, in granules of 16 rows; granule g of k lies at g ^ turn(k), so that the rows of k that one transposing read of four k
 //            takes lie in different banks.  16-bit values are transposed on the way out (ds_read_b64_tr_b16: of 16 lanes with
 //            four values each, lane i gets value i % 4 of lanes i / 4, i / 4 + 4, ...), floats are read one by one.
 // ------------------------------------------------------------------------------------------
-#define RING 4
-#define STEP_BYTES 64
+#define STAGE_BYTES 128
 
 typedef u32 rsrc_t __attribute__((ext_vector_type(4)));
 #define PAST_ALL 0x80000000u                     // an offset that no buffer here reaches: a copy of it writes zeros
@@ -188,23 +188,23 @@ template <int N> __device__ __forceinline__ void arrived_and_barrier() {
 
 __device__ __forceinline__ u32 lds_address(const void* p) { return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
 
-// An operand's way to LDS: BT rows and 64 bytes of k a step, shared by four waves.  STAGED: through registers, for rows that do not begin at multiples of 16 bytes.
-template <class T, int BT, bool BY_K, bool STAGED>
+// An operand's way to LDS: BT rows and 128 bytes of k a stage, shared by WAVES waves.  STAGED: through registers, for rows that do not begin at multiples of 16 bytes.
+template <class T, int BT, bool BY_K, bool STAGED, int WAVES>
 struct Feed {
     typedef typename T::elem elem;
-    static constexpr u32 E = 16 / sizeof(elem), KS = STEP_BYTES / sizeof(elem);   // elements of a chunk, k of a step
-    static constexpr u32 BYTES = BT * STEP_BYTES, N = BYTES / 4096;               // of a step; copies of a wave
-    static constexpr u32 ROW = BY_K ? BT * sizeof(elem) : STEP_BYTES, CG = sizeof(elem);   // bytes of a row in LDS; chunks of 16 values
-    static constexpr u32 COPIES = STAGED ? 0 : N;
+    static constexpr u32 E = 16 / sizeof(elem), KS = STAGE_BYTES / sizeof(elem);  // elements of a chunk, k of a stage
+    static constexpr u32 BYTES = BT * STAGE_BYTES, N = BYTES / (1024 * WAVES);    // of a stage; copies of a wave
+    static constexpr u32 ROW = BY_K ? BT * sizeof(elem) : STAGE_BYTES, CG = sizeof(elem);  // bytes of a row in LDS; chunks of 16 values
+    static constexpr u32 COPIES = STAGED ? 0 : N, KD = BY_K ? 1024 / ROW : 0;
     typedef Vec<T, E> V;
 
-    const elem* base;            // of the block's first row, at the step that is copied next
+    const elem* base;            // of the block's first row, at the stage that is copied next
     u64 left;                    // bytes from there to the operand's end
     u64 stride;
-    u32 k, depth;                // of that step; end of the sum
+    u32 k, depth;                // of that stage; end of the sum
     u32 rows;                    // of the operand from the block's first
-    u32 offset[N], kk[N];        // a lane's chunk: from the base, its first k in a step
-    u32 r[N];                    // its row
+    u32 offset[N], kk;           // a lane's chunks: from the base; the first one's first k in a stage, KD before the next one's
+    u32 r[BY_K && STAGED ? N : 1];                       // their rows
     u32 wave;
     u4v v[STAGED ? N : 1];
 
@@ -221,15 +221,14 @@ struct Feed {
         for (u32 i = 0; i < N; ++i) {
             const u32 at = (wave * N + i) * 1024 + lane * 16, line = at / ROW, place = at % ROW / 16;
             if (BY_K) {
-                const u32 chunk = (place / CG ^ turn(line)) * CG + place % CG;
-                kk[i] = line;
-                r[i] = chunk * E;
-                offset[i] = (u32)(line * stride + (r[i] < rows ? r[i] : 0)) * sizeof(elem);      // (a chunk of rows past the end: any)
+                const u32 chunk = (place / CG ^ turn(line)) * CG + place % CG, row = chunk * E;
+                if (i == 0) kk = line;
+                if (STAGED) r[i] = row;
+                offset[i] = (u32)(line * stride + (row < rows ? row : 0)) * sizeof(elem);      // (a chunk of rows past the end: any)
             } else {
-                const u32 chunk = place ^ (line >> 1 & 3);
-                kk[i] = chunk * E;
-                r[i] = line < rows ? line : rows - 1;
-                offset[i] = (u32)(r[i] * stride + kk[i]) * sizeof(elem);
+                const u32 chunk = place ^ (line & 7), row = line < rows ? line : rows - 1;
+                if (i == 0) kk = chunk * E;
+                offset[i] = (u32)(row * stride + chunk * E) * sizeof(elem);
             }
         }
     }
@@ -239,35 +238,32 @@ struct Feed {
         left -= by * sizeof(elem);
         k += KS;
     }
-    // The step's copy number i of this wave, to LDS at `to`; k past the end as zeros.
+    // The stage's copy number i of this wave, to LDS at `to`; k past the end as zeros.
     __device__ __forceinline__ void copy(u32 i, u32 to) const {
         const u64 at = (u64)base;
         const u32 bytes = left < PAST_ALL - 16 ? ((u32)left + 15) & ~15u : PAST_ALL;      // (a chunk that begins inside ends in the same 16 bytes of memory)
-        const rsrc_t from = {(u32)at, (u32)(at >> 32), k < depth ? bytes : 0, 0x00020000u};
-        u32 o = offset[i];
-        if (k < depth && depth - k < KS) o = kk[i] < depth - k ? o : PAST_ALL;
-        copy_to_lds(from, o, to + (wave * N + i) * 1024);
+        const u32 rest = k < depth ? depth - k : 0;
+        const rsrc_t from = {(u32)at, (u32)(at >> 32), bytes, 0x00020000u};
+        copy_to_lds(from, kk + i * KD < rest ? offset[i] : PAST_ALL, to + (wave * N + i) * 1024);
     }
     // Through registers: asked for, and put down later.
     __device__ __forceinline__ void ask(u32 i) {
+        v[i] = (u4v)(0u);
         if (k >= depth) return;
         const u32 n = depth - k;
         const elem* const at = base + offset[i] / sizeof(elem);
-        v[i] = (u4v)(0u);
         if (BY_K) {
-            if (kk[i] < n && r[i] < rows) v[i] = __builtin_bit_cast(u4v, r[i] + E <= rows ? V::load(at) : V::some(at, rows - r[i]));
-        } else if (kk[i] < n) {
-            v[i] = __builtin_bit_cast(u4v, kk[i] + E <= n ? V::load(at) : V::some(at, n - kk[i]));
+            if (kk + i * KD < n && r[i] < rows) v[i] = __builtin_bit_cast(u4v, r[i] + E <= rows ? V::load(at) : V::some(at, rows - r[i]));
+        } else if (kk < n) {
+            v[i] = __builtin_bit_cast(u4v, kk + E <= n ? V::load(at) : V::some(at, n - kk));
         }
     }
-    __device__ __forceinline__ void put(u32 i, uint8_t* step) const { *(u4v*)(step + (wave * N + i) * 1024 + (threadIdx.x & 63) * 16) = v[i]; }
-    // A chunk that holds the end of the sum, in a row whose k do not end with it: zeros behind.  Done by who copied it.
-    __device__ __forceinline__ void trim(uint8_t* step, u32 n) const {
+    __device__ __forceinline__ void put(u32 i, uint8_t* stage) const { *(u4v*)(stage + (wave * N + i) * 1024 + (threadIdx.x & 63) * 16) = v[i]; }
+    // The chunks that hold the end of the sum, n k into a stage, in rows whose k do not end with it: zeros behind.
+    static __device__ __forceinline__ void trim(uint8_t* stage, u32 n) {
         if (BY_K || STAGED) return;
-#pragma unroll
-        for (u32 i = 0; i < N; ++i)
-            for (u32 e = 1; e < E; ++e)
-                if (kk[i] < n && kk[i] + e >= n) *(elem*)(step + (wave * N + i) * 1024 + (threadIdx.x & 63) * 16 + e * sizeof(elem)) = (elem)0.0f;
+        for (u32 row = threadIdx.x; row < BT; row += 64 * WAVES)
+            for (u32 e = n % E; e < E; ++e) *(elem*)(stage + row * STAGE_BYTES + ((n / E ^ (row & 7)) << 4) + e * sizeof(elem)) = (elem)0.0f;
     }
 };
 
@@ -275,18 +271,19 @@ struct Feed {
 template <class T, int BT, bool BY_K>
 struct Reader {
     typedef typename T::elem elem;
-    typedef Feed<T, BT, BY_K, false> F;
-    u32 base, w0, t;
-    __device__ __forceinline__ explicit Reader(u32 w) : w0(w) {
+    typedef Feed<T, BT, BY_K, false, 1> F;
+    u32 base;                    // of fragment 0
+    __device__ __forceinline__ explicit Reader(u32 w) {
         const u32 lane = threadIdx.x & 63, group = lane >> 4, in = lane & 15;
-        if (!BY_K) base = (w + in) * STEP_BYTES + ((group ^ (in >> 1 & 3)) << 4);
-        else if (sizeof(elem) == 2) base = (8 * group + (in >> 2)) * F::ROW + (in & 3) * 8;
-        else base = 4 * group * F::ROW + in * 4;
-        t = sizeof(elem) == 2 ? F::turn(8 * group + (in >> 2)) : F::turn(4 * group);
+        if (!BY_K) base = (w + in) * STAGE_BYTES + ((group ^ (in & 7)) << 4);
+        else if (sizeof(elem) == 2) base = (8 * group + (in >> 2)) * F::ROW + (in & 3) * 8 + ((w / 16 ^ F::turn(8 * group + (in >> 2))) << 5);
+        else base = 4 * group * F::ROW + in * 4 + ((w / 16 ^ F::turn(4 * group)) << 6);
     }
-    __device__ __forceinline__ u4v get(const uint8_t* step, u32 i) const {
-        if (!BY_K) return *(const u4v*)(step + base + i * 16 * STEP_BYTES);
-        const uint8_t* const at = step + base + (((w0 / 16 + i) ^ t) << (sizeof(elem) == 2 ? 5 : 6));
+    // Fragment i of half `half` of the stage at `stage`, a multiple of 1024.  By k, a wave's first granule is a multiple of the number of its fragments (a power of
+    // two), so that (first + i) ^ turn is first ^ turn ^ i.
+    __device__ __forceinline__ u4v get(const uint8_t* ring, u32 stage, u32 half, u32 i) const {
+        if (!BY_K) return *(const u4v*)(ring + ((stage + base) ^ (half << 6)) + i * 16 * STAGE_BYTES);
+        const uint8_t* const at = ring + ((stage + base) ^ (i << (sizeof(elem) == 2 ? 5 : 6))) + half * (F::KS / 2) * F::ROW;
         if (sizeof(elem) == 2) {
             typedef short s4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s4* lds;
@@ -311,37 +308,35 @@ __device__ __forceinline__ void tile_of(u64 b, u64 n, u32 tile_rows, u32 tile_co
     c = (u32)(in_band / high);
 }
 
-// Four waves, two by two, each 16 NM x 16 NN of the tile.
-template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, int NM, int NN, bool SUMS, class Out>
-__global__ __launch_bounds__(256, NM * NN > 16 ? 1 : 2) void ring_products(Product a, Out out) {
+// WR x WC waves, each 16 NM x 16 NN of the tile.
+template <int WR_, int WC_, int NM_, int NN_, int RING_> struct Waves { static constexpr int WR = WR_, WC = WC_, NM = NM_, NN = NN_, RING = RING_, BM = 16 * NM * WR, BN = 16 * NN * WC, ALL = WR * WC; };
+
+template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, class W, bool SUMS, class Out>
+__global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out out) {
     typedef typename T::elem elem;
-    constexpr int BM = 32 * NM, BN = 32 * NN;
-    typedef Feed<T, BM, P_BY_K, P_STAGED> FP;
-    typedef Feed<T, BN, Q_BY_K, Q_STAGED> FQ;
-    constexpr u32 KS = FP::KS, STEP = FP::BYTES + FQ::BYTES, COPIES = FP::COPIES + FQ::COPIES;
-    __shared__ __attribute__((aligned(1024))) uint8_t ring[RING * STEP];
+    constexpr int BM = W::BM, BN = W::BN, NM = W::NM, NN = W::NN, RING = W::RING;
+    typedef Feed<T, BM, P_BY_K, P_STAGED, W::ALL> FP;
+    typedef Feed<T, BN, Q_BY_K, Q_STAGED, W::ALL> FQ;
+    constexpr u32 KS = FP::KS, STAGE = FP::BYTES + FQ::BYTES, COPIES = FP::COPIES + FQ::COPIES;
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[RING * STAGE];
     u32 tm, tn;
     tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, a.tile_cols, tm, tn);
     const u32 m0 = tm * BM, n0 = tn * BN;
     const u32 matrix = blockIdx.z / a.parts, part = blockIdx.z % a.parts;
     const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, in_group = lane & 15;
-    const u32 wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+    const u32 wm = wave / W::WC * (16 * NM), wn = wave % W::WC * (16 * NN);
     const u32 k_first = part * a.part, k_end = a.depth - k_first > a.part ? k_first + a.part : a.depth;
-    const u32 steps = (k_end - k_first + KS - 1) / KS;
-    const bool summing = SUMS && n0 == 0 && wn == 0;
-    f4 acc[NM][NN] = {}, sum[SUMS ? NM : 1] = {};
+    const u32 stages = (k_end - k_first + KS - 1) / KS;
+    const bool summing = SUMS && __builtin_amdgcn_readfirstlane(n0 == 0 && wn == 0);
+    f4 acc[NM][NN] = {}, sum = {};
     FP fp((const elem*)a.P.p + matrix * a.P.step, a.P.stride, m0, a.rows, k_first, k_end);
     FQ fq((const elem*)a.Q.p + matrix * a.Q.step, a.Q.stride, n0, a.cols, k_first, k_end);
     const Reader<T, BM, P_BY_K> rp(wm);
     const Reader<T, BN, Q_BY_K> rq(wn);
     const u32 ring_at = __builtin_amdgcn_readfirstlane(lds_address(ring));
-    const auto copy = [&](u32 slot) {
-        if (!P_STAGED)
-#pragma unroll
-            for (u32 i = 0; i < FP::N; ++i) fp.copy(i, ring_at + slot * STEP);
-        if (!Q_STAGED)
-#pragma unroll
-            for (u32 i = 0; i < FQ::N; ++i) fq.copy(i, ring_at + slot * STEP + FP::BYTES);
+    const auto copy = [&](u32 e, u32 slot) {
+        if (e < FP::COPIES) fp.copy(e, ring_at + slot * STAGE);
+        else fq.copy(e - FP::COPIES, ring_at + slot * STAGE + FP::BYTES);
     };
     const auto ask = [&] {
         if (P_STAGED)
@@ -350,89 +345,102 @@ __global__ __launch_bounds__(256, NM * NN > 16 ? 1 : 2) void ring_products(Produ
         if (Q_STAGED)
 #pragma unroll
             for (u32 i = 0; i < FQ::N; ++i) fq.ask(i);
+        if (P_STAGED) fp.next();
+        if (Q_STAGED) fq.next();
     };
     const auto put = [&](u32 slot) {
         if (P_STAGED)
 #pragma unroll
-            for (u32 i = 0; i < FP::N; ++i) fp.put(i, ring + slot * STEP);
+            for (u32 i = 0; i < FP::N; ++i) fp.put(i, ring + slot * STAGE);
         if (Q_STAGED)
 #pragma unroll
-            for (u32 i = 0; i < FQ::N; ++i) fq.put(i, ring + slot * STEP + FP::BYTES);
+            for (u32 i = 0; i < FQ::N; ++i) fq.put(i, ring + slot * STAGE + FP::BYTES);
     };
     const auto next_copied = [&] { if (!P_STAGED) fp.next(); if (!Q_STAGED) fq.next(); };
-    const auto next_asked = [&] { if (P_STAGED) fp.next(); if (Q_STAGED) fq.next(); };
-    const auto trim = [&](u32 step) {              // of the last step, where it does not end with a chunk
-        const u32 n = k_end - k_first - step * KS;
-        if (n >= KS || n % (16 / sizeof(elem)) == 0) return;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        fp.trim(ring + step % RING * STEP, n);
-        fq.trim(ring + step % RING * STEP + FP::BYTES, n);
+    const u32 end = (k_end - k_first) % KS;        // of the last stage, where it is no whole one
+    const auto trim = [&](u32 slot) {
+        if (end % (16 / sizeof(elem)) == 0 || (P_BY_K && Q_BY_K)) return;
+        arrived_and_barrier<0>();
+        fp.trim(ring + slot * STAGE, end);
+        fq.trim(ring + slot * STAGE + FP::BYTES, end);
     };
-    u4v b[2][NM], c[2][NN];
-    if (steps) {
+    u4v b[2][NM], c[NN];
+    if (stages) {
         for (u32 i = 0; i < RING; ++i) {
-            copy(i);
+#pragma unroll
+            for (u32 e = 0; e < COPIES; ++e) copy(e, i);
             next_copied();
         }
         for (u32 i = 0; i < 2; ++i) {
             ask();
             put(i);
-            next_asked();
         }
         ask();
-        next_asked();
-        if (steps == 1) trim(0);
-        arrived_and_barrier<3 * COPIES>();
+        if (stages == 1) trim(0);
+        arrived_and_barrier<(RING - 1) * COPIES>();
 #pragma unroll
-        for (int i = 0; i < NM; ++i) b[0][i] = rp.get(ring, i);
+        for (int i = 0; i < NM; ++i) b[0][i] = rp.get(ring, 0, 0, i);
 #pragma unroll
-        for (int j = 0; j < NN; ++j) c[0][j] = rq.get(ring + FP::BYTES, j);
+        for (int j = 0; j < NN; ++j) c[j] = rq.get(ring, FP::BYTES, 0, j);
     }
-    const auto step = [&](u32 s, const u4v (&b)[NM], const u4v (&c)[NN], u4v (&b1)[NM], u4v (&c1)[NN]) {
-        if (s + 2 == steps) trim(s + 1);
-        arrived_and_barrier<2 * COPIES>();
-        const u32 here = s % RING, then = (s + 1) % RING;
-        copy(here);
-        next_copied();
-        put((s + 2) % RING);
-        ask();
-        next_asked();
+    // Multiplies one half's fragments; between rows of matrix instructions, which take longer, the next half's are read and, COPYING, a stage is copied.
+    const auto half = [&](auto copying, const u4v (&b)[NM], u4v (&b1)[NM], u32 slot1, u32 half1, u32 to) {
+        constexpr int EACH = (COPIES + NN - 1) / NN;
 #pragma unroll
-        for (int i = 0; i < NM; ++i) b1[i] = rp.get(ring + then * STEP, i);
+        for (int j = 0; j < NN; ++j) {
 #pragma unroll
-        for (int j = 0; j < NN; ++j) c1[j] = rq.get(ring + then * STEP + FP::BYTES, j);
+            for (int i = j * NM / NN; i < (j + 1) * NM / NN; ++i) b1[i] = rp.get(ring, slot1 * STAGE, half1, i);
+            if (decltype(copying)::value)
 #pragma unroll
-        for (int j = 0; j < NN; ++j)
+                for (u32 e = j * EACH; e < (j + 1) * EACH && e < COPIES; ++e) copy(e, to);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < NM; ++i) acc[i][j] = mfma<T>(c[j], b[i], acc[i][j]);
-        if (SUMS && summing)
+            __builtin_amdgcn_sched_barrier(0);
+            c[j] = rq.get(ring, slot1 * STAGE + FP::BYTES, half1, j);
+        }
+        // sums over k: products with ones, those of fragment i in rows 16 / NM i and up of one result
+        if (SUMS && summing) {
+            asm volatile("");                      // (or the compiler computes them everywhere and chooses)
 #pragma unroll
-            for (int i = 0; i < NM; ++i) sum[i] = mfma<T>(ones<T>(), b[i], sum[i]);
+            for (int i = 0; i < NM; ++i) sum = mfma<T>(in_group * NM / 16 == i ? ones<T>() : (u4v)(0u), b[i], sum);
+        }
     };
-    for (u32 s = 0; s < steps; s += 2) {
-        step(s, b[0], c[0], b[1], c[1]);
-        if (s + 1 < steps) step(s + 1, b[1], c[1], b[0], c[0]);
+    u32 slot = 0;
+    for (u32 s = 0; s < stages; ++s) {
+        const u32 then = slot + 1 == RING ? 0 : slot + 1;
+        half(Int<0>(), b[0], b[1], slot, 1, 0);
+        if (s + 2 == stages) trim(then);
+        arrived_and_barrier<(RING - 2) * COPIES>();
+        put((s + 2) % RING);
+        ask();
+        half(Int<1>(), b[1], b[0], then, 0, slot);
+        next_copied();
+        slot = then;
     }
-    // the result's tile through LDS, a quarter of a wave's rows at a time: rows leave whole, and what is done with them stands here once
+    // the result's tile through LDS, some of a wave's rows at a time: rows leave whole, and what is done with them stands here once
     arrived_and_barrier<0>();
-    constexpr u32 WIDTH = 16 * NN, LINE = WIDTH * 4 + 16;                            // (16 bytes more: the four rows of a lane's group in different banks)
-    uint8_t* const mine = ring + wave * (RING * STEP / 4);
-    constexpr int AT_ONCE = NM * 16 * LINE <= RING * STEP / 4 ? NM : NM / 2 * 16 * LINE <= RING * STEP / 4 ? NM / 2 : NM / 4;
+    constexpr u32 WIDTH = 16 * NN, LINE = WIDTH * 4 + 16;                            // (16 bytes more: the rows of a lane's group in different banks)
+    uint8_t* const mine = ring + wave * (RING * STAGE / W::ALL);
+    constexpr int AT_ONCE = NM * 16 * LINE <= RING * STAGE / W::ALL ? NM : NM / 2 * 16 * LINE <= RING * STAGE / W::ALL ? NM / 2 : NM / 4;
+#pragma nounroll
+    for (int turn = 0; turn < NM / AT_ONCE; ++turn) {
 #pragma unroll
-    for (int i0 = 0; i0 < NM; i0 += AT_ONCE) {
+        for (int t = 0; t < NM / AT_ONCE; ++t)
+            if (t == turn)
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i)
+                for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
-            for (int j = 0; j < NN; ++j) *(f4*)(mine + (i * 16 + in_group) * LINE + (j * 16 + group * 4) * 4) = acc[i0 + i][j];
+                    for (int j = 0; j < NN; ++j) *(f4*)(mine + (i * 16 + in_group) * LINE + (j * 16 + group * 4) * 4) = acc[t * AT_ONCE + i][j];
         for (u32 u = lane; u < AT_ONCE * 16 * (WIDTH / 4); u += 64) {
-            const u32 line = u / (WIDTH / 4), q = u % (WIDTH / 4) * 4, m = m0 + wm + i0 * 16 + line, n = n0 + wn + q;
+            const u32 line = u / (WIDTH / 4), q = u % (WIDTH / 4) * 4, m = m0 + wm + turn * AT_ONCE * 16 + line, n = n0 + wn + q;
             if (m < a.rows && n < a.cols) out.put(matrix, part, m, n, a.cols, *(const f4*)(mine + line * LINE + q * 4));
         }
     }
-    if (SUMS && summing && group == 0)
+    if (SUMS && summing)
 #pragma unroll
         for (int i = 0; i < NM; ++i)
-            if (m0 + wm + i * 16 + in_group < a.rows) out.sums(matrix, part, m0 + wm + i * 16 + in_group, sum[i][0]);
+            if (group == i * 16 / NM / 4 && m0 + wm + i * 16 + in_group < a.rows) out.sums(matrix, part, m0 + wm + i * 16 + in_group, sum[i * 16 / NM % 4]);
 }
 
 // Columns [n, n + 4) of a row, as floats.
