@@ -4,23 +4,42 @@
 // ------------------------------------------------------------------------------------------
 // activations and their slopes
 // ------------------------------------------------------------------------------------------
-#define ROOT_HALF 0.70710678118654752f
+#define LOG2E 1.4426950408889634f
 #define ROOT_TWO_OVER_PI 0.79788456080286536f
 #define CUBE 0.044715f
 
 __device__ __forceinline__ float one_over(float x) { return __builtin_amdgcn_rcpf(x); }
-// tanh's argument of GELU_TANH, twice and negated.  Past 30 the exponential has long been zero or infinity: the cube of a
-// larger z would pass fp32 where zero times it is wanted.
-__device__ __forceinline__ float tanh_power(float z) {
-    const float t = fminf(fmaxf(z, -30.0f), 30.0f);
-    return -2.0f * ROOT_TWO_OVER_PI * t * (1.0f + CUBE * t * t);
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The normal distribution's density over its value at 0, exp(-z z / 2), and its integral from -|z|, Phi(-|z|) = exp(-z z / 2) t R(t), t = 1 / (1 + 0.35 |z|): R is a
+// polynomial of degree 8, fitted to the least largest relative error over |z| <= 15, 3.2e-8 (2.9e-7 as it is computed, five roundings), where exp(-z z / 2) has long been zero.
+struct Normal { float bell, tail; };
+__device__ __forceinline__ Normal normal_of(float z) {
+    const float t = one_over(1.0f + 0.35f * fabsf(z)), bell = exp2_of(-0.5f * LOG2E * z * z);
+    float r = -0.02916385f;
+    r = r * t + 0.14406044f;
+    r = r * t - 0.25590114f;
+    r = r * t + 0.15939213f;
+    r = r * t - 0.02326333f;
+    r = r * t + 0.10557461f;
+    r = r * t + 0.11981554f;
+    r = r * t + 0.13986433f;
+    r = r * t + 0.13962126f;
+    return {bell, bell * (t * r)};
 }
+// tanh's argument of GELU_TANH, twice, negated and for a power of two.
+__device__ __forceinline__ float tanh_power(float z) { return z * (-2.0f * LOG2E * ROOT_TWO_OVER_PI - 2.0f * LOG2E * ROOT_TWO_OVER_PI * CUBE * z * z); }
+
+// An exponential is a power of two, whose argument's rounding is worth w U of a result with exp(w) in it: as much as the fp32 argument itself.
 __device__ __forceinline__ float act_of(int act, float z) {
     switch (act) {
         case DBLP_ACT_RELU: return z <= 0.0f ? 0.0f : z;
-        case DBLP_ACT_GELU: return 0.5f * z * erfcf(-z * ROOT_HALF);
-        case DBLP_ACT_GELU_TANH: return z * one_over(1.0f + expf(tanh_power(z)));
-        case DBLP_ACT_SILU: return z * one_over(1.0f + expf(-z));
+        case DBLP_ACT_GELU: {
+            const float tail = normal_of(z).tail;
+            return z * (z < 0.0f ? tail : 1.0f - tail);
+        }
+        case DBLP_ACT_GELU_TANH: return z * one_over(1.0f + exp2_of(tanh_power(z)));
+        case DBLP_ACT_SILU: return z * one_over(1.0f + exp2_of(-LOG2E * z));
         default: return z;
     }
 }
@@ -28,14 +47,17 @@ __device__ __forceinline__ float act_of(int act, float z) {
 __device__ __forceinline__ float gated(int act, float z, float dy) {
     switch (act) {
         case DBLP_ACT_RELU: return z > 0.0f ? dy : 0.0f;
-        case DBLP_ACT_GELU: return dy * (0.5f * erfcf(-z * ROOT_HALF) + z * (expf(-0.5f * z * z) * (0.5f * ROOT_TWO_OVER_PI)));
+        case DBLP_ACT_GELU: {
+            const Normal n = normal_of(z);
+            return dy * ((z < 0.0f ? n.tail : 1.0f - n.tail) + z * (n.bell * (0.5f * ROOT_TWO_OVER_PI)));
+        }
         case DBLP_ACT_GELU_TANH: {
-            const float e = expf(tanh_power(z)), p = one_over(1.0f + e), t = fminf(fmaxf(z, -30.0f), 30.0f);
-            const float rest = e < 1e30f ? e * p : 1.0f;                        // 1 - p
-            return dy * (p + z * (p * rest * (2.0f * ROOT_TWO_OVER_PI * (1.0f + 3.0f * CUBE * t * t))));
+            // (past 30 the exponential has long been zero or infinity: a larger z' square would be infinite where zero times it is wanted)
+            const float t = fminf(fmaxf(z, -30.0f), 30.0f), e = exp2_of(tanh_power(t)), p = one_over(1.0f + e), rest = e < 1e30f ? e * p : 1.0f;      // 1 - p
+            return dy * (p + z * (p * rest * (2.0f * ROOT_TWO_OVER_PI + 6.0f * ROOT_TWO_OVER_PI * CUBE * t * t)));
         }
         case DBLP_ACT_SILU: {
-            const float e = expf(-z), p = one_over(1.0f + e), rest = e < 1e30f ? e * p : 1.0f;
+            const float e = exp2_of(-LOG2E * z), p = one_over(1.0f + e), rest = e < 1e30f ? e * p : 1.0f;
             return dy * (p + z * (p * rest));
         }
         default: return dy;
@@ -45,34 +67,29 @@ __device__ __forceinline__ float gated(int act, float z, float dy) {
 // ------------------------------------------------------------------------------------------
 // what becomes of a product's sums
 // ------------------------------------------------------------------------------------------
-// A matrix of a type that is known when the kernel runs: four columns of a row.
-struct Matrix { void* p; u64 stride; };
-
-__device__ __forceinline__ void load4(int type, const void* p, u64 at, u32 left, float (&v)[4]) {
-    if (type == DBLP_F32) get4<F32>((const float*)p + at, 0, left, v);
-    else if (type == DBLP_BF16) get4<BF16>((const __bf16*)p + at, 0, left, v);
-    else get4<F16>((const _Float16*)p + at, 0, left, v);
-}
-__device__ __forceinline__ void store4(int type, void* p, u64 at, u32 left, const float (&v)[4]) {
-    if (type == DBLP_F32) store_cols<Vec<F32, 4>, 4>((float*)p + at, 0, left, v);
-    else if (type == DBLP_BF16) store_cols<Vec<BF16, 4>, 4>((__bf16*)p + at, 0, left, v);
-    else store_cols<Vec<F16, 4>, 4>((_Float16*)p + at, 0, left, v);
-}
+struct Matrix { void* p; u64 stride; };          // of a type that is known when the kernel runs
 
 struct LayerOut {
     int type, act, bias_type;
     const void* bias;
     Matrix residual, y, z;
-    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc) const {
+    struct Met { u4v bias, residual; };
+    __device__ __forceinline__ Met get(u32, u32 m, u32 n, u32 cols) const {
+        Met r = {};
+        if (bias) r.bias = raw4(bias_type, bias, n, cols - n);
+        if (residual.p) r.residual = raw4(type, residual.p, m * residual.stride + n, cols - n);
+        return r;
+    }
+    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc, const Met& met) const {
         float v[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4];
         if (bias) {
-            load4(bias_type, bias, n, cols - n, b);
+            open4(bias_type, met.bias, b);
             for (int i = 0; i < 4; ++i) v[i] += b[i];
         }
         if (z.p) store4(type, z.p, m * z.stride + n, cols - n, v);
         for (int i = 0; i < 4; ++i) v[i] = act_of(act, v[i]);
         if (residual.p) {
-            load4(type, residual.p, m * residual.stride + n, cols - n, b);
+            open4(type, met.residual, b);
             for (int i = 0; i < 4; ++i) v[i] += b[i];
         }
         store4(type, y.p, m * y.stride + n, cols - n, v);
@@ -83,14 +100,21 @@ struct LayerOut {
 struct GateOut {
     int type, act;
     Matrix z, base, dx;
-    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc) const {
+    struct Met { u4v z, base; };
+    __device__ __forceinline__ Met get(u32, u32 m, u32 n, u32 cols) const {
+        Met r = {};
+        if (z.p) r.z = raw4(type, z.p, m * z.stride + n, cols - n);
+        if (base.p) r.base = raw4(type, base.p, m * base.stride + n, cols - n);
+        return r;
+    }
+    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc, const Met& met) const {
         float v[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4];
         if (z.p) {
-            load4(type, z.p, m * z.stride + n, cols - n, b);
+            open4(type, met.z, b);
             for (int i = 0; i < 4; ++i) v[i] = gated(act, b[i], v[i]);
         }
         if (base.p) {
-            load4(type, base.p, m * base.stride + n, cols - n, b);
+            open4(type, met.base, b);
             for (int i = 0; i < 4; ++i) v[i] += b[i];
         }
         store4(type, dx.p, m * dx.stride + n, cols - n, v);
@@ -105,16 +129,57 @@ struct WeightOut {
     u64 dw_stride;
     const float* bias_base;
     float* dbias;
-    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc) const {
-        float v[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4];
-        if (base) {
-            get4<F32>(base + m * base_stride, n, cols, b);
-            for (int i = 0; i < 4; ++i) v[i] += b[i];
-        }
-        store_cols<Vec<F32, 4>, 4>(dw + m * dw_stride, n, cols, v);
+    __device__ __forceinline__ u4v get(u32, u32 m, u32 n, u32 cols) const { return base ? raw4(DBLP_F32, base, m * base_stride + n, cols - n) : (u4v)(0u); }
+    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc, u4v met) const {
+        const f4 b = __builtin_bit_cast(f4, met);
+        const float v[4] = {acc[0] + b[0], acc[1] + b[1], acc[2] + b[2], acc[3] + b[3]};
+        store4(DBLP_F32, dw, m * dw_stride + n, cols - n, v);
     }
     __device__ __forceinline__ void sums(u32, u32, u32 m, float s) const { if (dbias) dbias[m] = bias_base ? bias_base[m] + s : s; }
 };
+
+// ------------------------------------------------------------------------------------------
+// the bias' gradient where large tiles make the weight's: sums of columns, eight rows of threads a block, blockIdx.y one of gridDim.y slices of the rows
+// ------------------------------------------------------------------------------------------
+template <class T>
+__global__ __launch_bounds__(256) void column_sums(const typename T::elem* p, u64 stride, u32 rows, u32 cols, u32 slice, PartOut out, WeightOut last) {
+    constexpr int E = 16 / sizeof(typename T::elem);
+    typedef Vec<T, E> V;
+    __shared__ float sh[8][32 * E + 4];
+    const u32 x = threadIdx.x & 31, y = threadIdx.x >> 5, c = (blockIdx.x * 32 + x) * E;
+    const u32 first = blockIdx.y * slice, end = rows - first < slice ? rows : first + slice;
+    float sum[E] = {};
+    if (c < cols)
+        for (u32 r = first + y; r < end; r += 32) {
+            typename V::raw v[4];
+#pragma unroll
+            for (u32 i = 0; i < 4; ++i) if (r + 8 * i < end) v[i] = c + E <= cols ? V::load(p + (r + 8 * i) * stride + c) : V::some(p + (r + 8 * i) * stride + c, cols - c);
+#pragma unroll
+            for (u32 i = 0; i < 4; ++i)
+                if (r + 8 * i < end) {
+                    float f[E];
+                    V::open(v[i], f);
+                    for (int e = 0; e < E; ++e) sum[e] += f[e];
+                }
+        }
+    for (int e = 0; e < E; ++e) sh[y][x * E + e] = sum[e];
+    __syncthreads();
+    for (u32 i = threadIdx.x; i < 32 * E; i += 256) {
+        float all = 0.0f;
+        for (u32 j = 0; j < 8; ++j) all += sh[j][i];
+        const u32 m = blockIdx.x * 32 * E + i;
+        if (m >= cols) continue;
+        if (gridDim.y == 1) last.sums(0, 0, m, all);
+        else out.sums(0, blockIdx.y, m, all);
+    }
+}
+__global__ __launch_bounds__(256) void join_sums(PartOut in, u32 cols, u32 parts, WeightOut last) {
+    const u32 m = blockIdx.x * 256 + threadIdx.x;
+    if (m >= cols) return;
+    float sum = 0.0f;
+    for (u32 i = 0; i < parts; ++i) sum += in.row_sums[(u64)i * in.rows + m];
+    last.sums(0, 0, m, sum);
+}
 
 // ------------------------------------------------------------------------------------------
 // activation_grad: a thread takes 16 bytes
@@ -140,34 +205,104 @@ __global__ __launch_bounds__(256) void activation_units(Units s, int act, const 
 static bool bad_act(int act) { return act < DBLP_ACT_NONE || act > DBLP_ACT_SILU; }
 static bool bad_sizes(u64 tokens, u64 in, u64 out) { return tokens >= COUNT_LIMIT || in >= COUNT_LIMIT || out >= COUNT_LIMIT; }
 
+// Parts of a sum over k: at most this many, and as many as fit these bytes.
+#define PARTS_MOST 64
+#define PARTS_BYTES (128ull << 20)
+static u64 parts_bytes(u64 rows, u64 cols) {
+    const u64 one = rows * round_up(cols, 4) * 4;                                    // (below 2^64: both are below 2^31)
+    return one >= PARTS_BYTES / PARTS_MOST ? PARTS_BYTES : one * PARTS_MOST;
+}
+
 extern "C" uint64_t dblp_linear_workspace(uint64_t n_tokens, uint32_t in, uint32_t out) {
-    return bad_sizes(n_tokens, in, out) ? 0 : 256;
+    if (bad_sizes(n_tokens, in, out)) return 0;
+    u64 most = parts_bytes(n_tokens, out);
+    for (const u64 other : {parts_bytes(n_tokens, in), parts_bytes(out, in)}) if (other > most) most = other;
+    return 256 + most + round_up((u64)PARTS_MOST * out * 4, 256);
+}
+
+// A way to make a product: tiles of one kind, the sum over k in `parts` parts.
+enum Kind { TILES_64, TILES_128, TILES_256, KINDS };
+struct Way { Kind kind; u32 parts, part; };
+
+// Chosen by an estimate of the time: rounds of tiles over the 256 CUs, each a fixed time and one for each stage of 128 bytes of k.  Microseconds, as measured: a CU holds three, two or
+// one block of a kind, and a stage takes longer with more of them.
+static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
+    static const struct { u32 tile, blocks; double fixed, stage[2]; } K[KINDS] = {{64, 3, 3.0, {0.45, 1.3}}, {128, 2, 6.0, {1.23, 3.4}}, {256, 1, 14.0, {1.65, 1e9}}};
+    Way best = {TILES_64, 1, 0};
+    double least = 1e30;
+    const u64 ks = 128 / elem, stages = (depth + ks - 1) / ks, bytes = rows * round_up(cols, 4) * 4;
+    for (int i = 0; i < KINDS; ++i) {
+        if (i == TILES_256 && elem == 4) continue;
+        const u64 tiles = ((rows + K[i].tile - 1) / K[i].tile) * ((cols + K[i].tile - 1) / K[i].tile);
+        for (u64 p = 1; p <= PARTS_MOST && (p == 1 || (p * bytes <= PARTS_BYTES && stages / p >= 4)); ++p) {
+            const u64 each = (stages + p - 1) / p;
+            if (p > 1 && (stages + each - 1) / each != p) continue;
+            const double blocks = (double)tiles * p, rounds = ceil(blocks / (256.0 * K[i].blocks)), held = blocks < 256.0 * K[i].blocks ? ceil(blocks / 256.0) : K[i].blocks;
+            const double t = rounds * (K[i].fixed + each * K[i].stage[elem == 4] * (0.5 + 0.5 * held / K[i].blocks)) + (p > 1 ? 4.0 + p * bytes * 2 / 4e6 : 0.0);
+            if (t < least) {
+                least = t;
+                best = {(Kind)i, (u32)p, (u32)(each * ks)};
+            }
+        }
+    }
+    if (best.parts == 1) best.part = 0;
+    return best;
 }
 
 template <class T, bool P_BY_K, bool Q_BY_K, bool SUMS, class Out>
-static void products(Launches& launch, hipStream_t stream, Product a, Out out) {
-    a.part = (u32)round_up(a.depth ? a.depth : 1, 64);
-    a.parts = 1;
-    const u64 area = (u64)a.rows * a.cols;
-    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) {
-        each_tiles<64, 64>(a, 1, [&](const Product& p, dim3 grid, u64) { launch(tile_products<T, P_BY_K, Q_BY_K, 64, 64, SUMS, Out>, grid, TILE_THREADS, stream, p, out); });
-        return;
-    }
+static void tiles(Launches& launch, hipStream_t stream, Product a, Kind kind, Out out) {
     const auto go = [&](auto waves, auto p_staged, auto q_staged) {
         typedef decltype(waves) W;
         each_tiles<W::BM, W::BN>(a, 1, [&](const Product& p, dim3 grid, u64) {
-            launch(ring_products<T, P_BY_K, Q_BY_K, decltype(p_staged)::value, decltype(q_staged)::value, W, SUMS && (W::ALL == 4), Out>, grid, 64 * W::ALL, stream, p, out);
+            launch(ring_products<T, P_BY_K, Q_BY_K, decltype(p_staged)::value, decltype(q_staged)::value, W, SUMS && W::ALL == 4, Out>, grid, 64 * W::ALL, stream, p, out);
         });
     };
-    const auto by_rows = [&](auto waves) {
+    const auto by_place = [&](auto waves) {
         const bool p = in_chunks<T>(a.P), q = in_chunks<T>(a.Q);
         if (p && q) go(waves, Int<0>(), Int<0>());
         else if (q) go(waves, Int<1>(), Int<0>());
         else go(waves, Int<1>(), Int<1>());
     };
-    if (area < (u64)256 * 128 * 128) by_rows(Waves<2, 2, 2, 2, 3>());
-    else if (sizeof(typename T::elem) == 4 || area < (u64)200 * 256 * 256) by_rows(Waves<2, 2, 4, 4, 2>());
-    else if constexpr (sizeof(typename T::elem) == 2) by_rows(Waves<2, 4, 8, 4, 2>());
+    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q))
+        each_tiles<64, 64>(a, 1, [&](const Product& p, dim3 grid, u64) { launch(tile_products<T, P_BY_K, Q_BY_K, 64, 64, SUMS, Out>, grid, TILE_THREADS, stream, p, out); });
+    else if (kind == TILES_64) by_place(Waves<2, 2, 2, 2, 3>());
+    else if (kind == TILES_128) by_place(Waves<2, 2, 4, 4, 2>());
+    else if constexpr (sizeof(typename T::elem) == 2) by_place(Waves<2, 4, 8, 4, 2>());
+}
+
+template <class T, bool P_BY_K, bool Q_BY_K, bool SUMS, class Out>
+static void products(Launches& launch, hipStream_t stream, Product a, Out out, void* workspace) {
+    Way w = way_of(a.rows, a.cols, a.depth, sizeof(typename T::elem));
+    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0};
+    a.parts = w.parts;
+    a.part = w.parts > 1 ? w.part : (u32)round_up(a.depth ? a.depth : 1, 64);
+    PartOut parts = {(float*)workspace, round_up(a.cols, 4), 0, nullptr, a.rows};
+    parts.step = a.rows * parts.stride;
+    bool row_sums = false;
+    if constexpr (SUMS) {
+        parts.row_sums = (float*)((uint8_t*)workspace + round_up(parts_bytes(a.rows, a.cols), 256));
+        row_sums = out.dbias != nullptr;
+        if (row_sums && (w.kind == TILES_256 || a.cols == 0)) {
+            // in slices of 64 rows and more, as many as make a thousand blocks
+            typedef const typename T::elem* in;
+            constexpr u32 WIDTH = 512 / sizeof(typename T::elem);
+            const u32 across = (a.rows + WIDTH - 1) / WIDTH;
+            u32 slices = 1024 / across < PARTS_MOST ? 1024 / across : PARTS_MOST;
+            if (slices > a.depth / 64) slices = a.depth / 64;
+            if (slices < 1) slices = 1;
+            const u32 slice = (u32)round_up((a.depth + slices - 1) / slices, 8);
+            slices = a.depth ? (a.depth + slice - 1) / slice : 1;
+            launch(column_sums<T>, dim3(across, slices), 256, stream, (in)a.P.p, a.P.stride, a.depth, a.rows, slice, parts, out);
+            if (slices > 1) launch(join_sums, dim3((a.rows + 255) / 256), 256, stream, parts, a.rows, slices, out);
+            row_sums = false;
+            out.dbias = nullptr;
+        }
+    }
+    if (a.cols == 0) return;
+    if (!row_sums) parts.row_sums = nullptr;
+    if (w.parts == 1) return tiles<T, P_BY_K, Q_BY_K, SUMS>(launch, stream, a, w.kind, out);
+    tiles<T, P_BY_K, Q_BY_K, SUMS>(launch, stream, a, w.kind, parts);
+    each_launch<4>(a.rows, a.cols, [&](Units s) { launch(join_parts<Out>, dim3(blocks_of(s.n, 256)), 256, stream, parts, s, w.parts, out); });
 }
 
 extern "C" int dblp_linear(int device, void* stream, uint64_t n_tokens, uint32_t in, uint32_t out, const void* d_x, uint64_t x_stride,
@@ -192,7 +327,7 @@ extern "C" int dblp_linear(int device, void* stream, uint64_t n_tokens, uint32_t
     Launches launch;
     const LayerOut o = {out_type, activation, bias_type, d_bias, {(void*)d_residual, residual_stride}, {d_y, y_stride}, {d_z, z_stride}};
     by_type(type, [&](auto tt) {
-        products<decltype(tt), false, false, false>(launch, (hipStream_t)stream, Product{{d_x, x_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, out, in}, o);
+        products<decltype(tt), false, false, false>(launch, (hipStream_t)stream, Product{{d_x, x_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, out, in}, o, d_workspace);
     });
     return launched(call, launch);
 }
@@ -219,7 +354,7 @@ extern "C" int dblp_linear_grad_input(int device, void* stream, uint64_t n_token
     Launches launch;
     const GateOut o = {out_type, activation, {(void*)d_z, z_stride}, {(void*)d_base, base_stride}, {d_dx, dx_stride}};
     by_type(type, [&](auto tt) {
-        products<decltype(tt), false, true, false>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, in, out}, o);
+        products<decltype(tt), false, true, false>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, in, out}, o, d_workspace);
     });
     return launched(call, launch);
 }
@@ -245,7 +380,7 @@ extern "C" int dblp_linear_grad_weight(int device, void* stream, uint64_t n_toke
     Launches launch;
     const WeightOut o = {d_base, base_stride, d_dw, dw_stride, d_bias_base, d_dbias};
     by_type(type, [&](auto tt) {
-        products<decltype(tt), true, true, true>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_x, x_stride, 0}, out, in, (u32)n_tokens}, o);
+        products<decltype(tt), true, true, true>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_x, x_stride, 0}, out, in, (u32)n_tokens}, o, d_workspace);
     });
     return launched(call, launch);
 }

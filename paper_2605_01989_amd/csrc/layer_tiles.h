@@ -41,7 +41,7 @@ struct Operand { const void* p; u64 stride, step; };
 // What a launch computes: rows x cols results of sums over `depth` k, of which block z takes part z % parts of matrix z / parts.
 struct Product {
     Operand P, Q;
-    u32 rows, cols, depth, tile_cols, part, parts;   // part: k of one part, a multiple of 64; tile_cols: tiles of a row of tiles
+    u32 rows, cols, depth, tile_cols, part, parts;   // part: k of one part, a multiple of 128 bytes' (a stage's); tile_cols: tiles of a row of tiles
     u32 tile_rows;
     u64 tiles, tile0;                                // of the whole result; first one of this launch
 };
@@ -98,8 +98,8 @@ struct Staged {
 
 __device__ __forceinline__ u4v chunk_of(const uint8_t* tile, u32 row, u32 chunk) { return *(const u4v*)(tile + row * 128 + (chunk ^ (row & 7)) * 16); }
 
-// Four waves, two by two, each a quarter of a BM x BN tile.  SUMS: of the first column of tiles, also P's own sums over k.  `out` gets the results, four columns of
-// a row at a time; `sums` a row's sum.
+// Four waves, two by two, each a quarter of a BM x BN tile: operands of any place and stride.  SUMS: of the first column of tiles, also P's own sums over k.  `out` gets the
+// results, four columns of a row at a time, and what its `get` has found in memory for them; `sums` gets a row's sum.
 template <class T, bool P_BY_K, bool Q_BY_K, int BM, int BN, bool SUMS, class Out>
 __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out) {
     typedef typename T::elem elem;
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out
 #pragma unroll
         for (int j = 0; j < NN; ++j) {
             const u32 n = n0 + wn + j * 16 + group * 4;
-            if (n < a.cols) out.put(matrix, part, m, n, a.cols, acc[i][j]);
+            if (n < a.cols) out.put(matrix, part, m, n, a.cols, acc[i][j], out.get(matrix, m, n, a.cols));
         }
     }
 }
@@ -432,9 +432,19 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
                     for (int j = 0; j < NN; ++j) *(f4*)(mine + (i * 16 + in_group) * LINE + (j * 16 + group * 4) * 4) = acc[t * AT_ONCE + i][j];
-        for (u32 u = lane; u < AT_ONCE * 16 * (WIDTH / 4); u += 64) {
-            const u32 line = u / (WIDTH / 4), q = u % (WIDTH / 4) * 4, m = m0 + wm + turn * AT_ONCE * 16 + line, n = n0 + wn + q;
-            if (m < a.rows && n < a.cols) out.put(matrix, part, m, n, a.cols, *(const f4*)(mine + line * LINE + q * 4));
+        // four at a time, so that what they meet in memory is asked for together
+        constexpr u32 LINES = 64 / (WIDTH / 4);
+        const u32 q = lane % (WIDTH / 4) * 4, n = n0 + wn + q;
+#pragma nounroll
+        for (u32 line = lane / (WIDTH / 4); line < AT_ONCE * 16; line += 4 * LINES) {
+            const u32 m = m0 + wm + turn * AT_ONCE * 16 + line;
+            decltype(out.get(0, 0, 0, 0)) met[4];
+#pragma unroll
+            for (u32 e = 0; e < 4; ++e)
+                if (m + e * LINES < a.rows && n < a.cols) met[e] = out.get(matrix, m + e * LINES, n, a.cols);
+#pragma unroll
+            for (u32 e = 0; e < 4; ++e)
+                if (m + e * LINES < a.rows && n < a.cols) out.put(matrix, part, m + e * LINES, n, a.cols, *(const f4*)(mine + (line + e * LINES) * LINE + q * 4), met[e]);
         }
     }
     if (SUMS && summing)
@@ -450,11 +460,62 @@ __device__ __forceinline__ void get4(const typename T::elem* row, u32 n, u32 col
     V::open(n + 4 <= cols ? V::load(row + n) : V::some(row + n, cols - n), v);
 }
 
-// Launches of a product's tiles: at most 2^20 tiles and 2^15 matrices' parts each (a grid's threads stay below 2^32, its z below 2^16).  Rows
-// have a tile even where there is no column: for their own sums.
+// What memory holds for four columns of a row, as it lies there, so that several can be on their way: 16 bytes of floats or 8 of 16-bit values, by a type that is known
+// when the kernel runs.
+__device__ __forceinline__ u4v raw4(int type, const void* p, u64 at, u32 left) {
+    if (type == DBLP_F32) {
+        const float* const f = (const float*)p + at;
+        return __builtin_bit_cast(u4v, left >= 4 ? Vec<F32, 4>::load(f) : Vec<F32, 4>::some(f, left));
+    }
+    const __bf16* const h = (const __bf16*)p + at;                                   // (either type's: bits)
+    const u2v r = left >= 4 ? Vec<BF16, 4>::load(h) : Vec<BF16, 4>::some(h, left);
+    return (u4v){r.x, r.y, 0, 0};
+}
+__device__ __forceinline__ void open4(int type, u4v r, float (&v)[4]) {
+    if (type == DBLP_F32) Vec<F32, 4>::open(__builtin_bit_cast(f4v, r), v);
+    else if (type == DBLP_BF16) Vec<BF16, 4>::open((u2v){r.x, r.y}, v);
+    else Vec<F16, 4>::open((u2v){r.x, r.y}, v);
+}
+__device__ __forceinline__ void store4(int type, void* p, u64 at, u32 left, const float (&v)[4]) {
+    if (type == DBLP_F32) store_cols<Vec<F32, 4>, 4>((float*)p + at, 0, left, v);
+    else if (type == DBLP_BF16) store_cols<Vec<BF16, 4>, 4>((__bf16*)p + at, 0, left, v);
+    else store_cols<Vec<F16, 4>, 4>((_Float16*)p + at, 0, left, v);
+}
+struct None {};
+
+// Parts of a sum over k, each a matrix of floats of its own, to be joined.
+struct PartOut {
+    float* p;
+    u64 stride, step;            // of rows, a multiple of four; of parts
+    float* row_sums;
+    u32 rows;
+    __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
+    __device__ __forceinline__ void put(u32, u32 part, u32 m, u32 n, u32, f4 acc, None) const { *(f4*)(p + part * step + m * stride + n) = acc; }
+    __device__ __forceinline__ void sums(u32, u32 part, u32 m, float s) const { if (row_sums) row_sums[(u64)part * rows + m] = s; }
+};
+
+// Adds the parts up, one after the other, and hands the results on: a thread takes four columns.
+template <class Out>
+__global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, u32 parts, Out out) {
+    const u32 u = blockIdx.x * 256 + threadIdx.x;
+    if (u >= s.n) return;
+    const u32 row = s.per_row.of(u), c = (u - row * s.per_row.d) * 4, m = (u32)s.row0 + row;
+    if (in.row_sums && c == 0) {
+        float sum = 0.0f;
+        for (u32 i = 0; i < parts; ++i) sum += in.row_sums[(u64)i * in.rows + m];
+        out.sums(0, 0, m, sum);
+    }
+    if (c >= s.cols) return;
+    const auto met = out.get(0, m, c, s.cols);
+    f4 sum = {};
+    for (u32 i = 0; i < parts; ++i) sum += *(const f4*)(in.p + i * in.step + m * in.stride + c);
+    out.put(0, 0, m, c, s.cols, sum, met);
+}
+
+// Launches of a product's tiles: at most 2^20 tiles and 2^15 matrices' parts each (a grid's threads stay below 2^32, its z below 2^16).
 template <int BM, int BN, class F>
 static void each_tiles(Product a, u64 matrices, F f) {
-    a.tile_cols = a.cols ? (u32)((a.cols + (u64)BN - 1) / BN) : 1;
+    a.tile_cols = (u32)((a.cols + (u64)BN - 1) / BN);
     a.tile_rows = (u32)((a.rows + (u64)BM - 1) / BM);
     a.tiles = (u64)a.tile_rows * a.tile_cols;
     for (u64 m = 0; m < matrices; m += 32768 / a.parts) {

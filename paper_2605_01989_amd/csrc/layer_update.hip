@@ -65,7 +65,8 @@ __global__ __launch_bounds__(256) void scale_in(const typename T::elem* g, u64 s
 struct GramOut {
     float* a;
     u64 stride, step, matrix0;
-    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc) const {
+    __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
+    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc, None) const {
         const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
         store_cols<Vec<F32, 4>, 4>(a + (matrix0 + matrix) * step + m * stride, n, cols, v);
     }
@@ -77,7 +78,8 @@ struct PolyOut {
     float* poly;
     u64 stride, step, matrix0;
     float a, b, c;
-    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc) const {
+    __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
+    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc, None) const {
         const u64 at = (matrix0 + matrix) * step + m * stride;
         float v[4];
         get4<F32>(gram + at, n, cols, v);
@@ -93,7 +95,8 @@ template <class T> struct UpdateOut {
     u64 base_stride, base_step;
     elem* out;
     u64 out_stride, out_step, matrix0;
-    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc) const {
+    __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
+    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc, None) const {
         float v[4], b[4];
         for (int i = 0; i < 4; ++i) v[i] = scale * acc[i];
         if (base) {
@@ -115,7 +118,7 @@ __global__ __launch_bounds__(256) void update_plain(const float* x, Shape s, Upd
         const u32 m = (u32)(i / units), c = (u32)(i % units) * 4;
         f4 v = {};
         for (u32 e = 0; e < 4; ++e) if (c + e < cols) v[e] = s.tall ? x[(u64)(c + e) * s.cols + m] : x[(u64)m * s.cols + c + e];
-        out.put(blockIdx.z, 0, m, c, cols, v);
+        out.put(blockIdx.z, 0, m, c, cols, v, None());
     }
 }
 

@@ -121,6 +121,58 @@ def test_linear_grad_weight(t):
         assert untouched(buf, dw)
 
 
+def big(t):
+    return t.double()
+
+
+# tokens, in, out, padding: whole large tiles, ragged ones on aligned rows, odd rows, sums in many parts, sums that end inside a chunk
+LARGE = [(4096, 128, 4096, 0), (3333, 200, 4600, 0), (4000, 77, 4099, 3), (4099, 65, 4000, 0), (700, 5000, 800, 0), (129, 9001, 130, 7), (2050, 100, 9000, 1), (260, 3000, 50257, 0)]
+
+
+@pytest.mark.parametrize("n, inner, outer, pad", LARGE)
+@pytest.mark.parametrize("t", TYPES)
+def test_large_products(t, n, inner, outer, pad):
+    """The same bounds, the definition computed on the GPU in 64 bits.  Fp32 sums of `depth` products in any order."""
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    g = gen(n + inner)
+
+    def near(got, want, mag, depth, o):
+        got, half = big(got), torch.finfo(o).eps / 2
+        tol = half * want.abs() * (1 + half) + 2 * (depth + 4) * U * mag + 2.0 ** -25 * (o == torch.float16)
+        bad = ~((got - want).abs() <= tol)
+        assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4], want[bad][:4])
+    rand = lambda r, c, to=t: torch.randn(r, c + pad, generator=g, device="cuda").to(to)[:, :c]  # noqa: E731
+    x, w, dy = rand(n, inner), rand(outer, inner), rand(n, outer)
+    ws = space(dblp.linear_workspace(n, inner, outer))
+    bias, r = torch.randn(outer, generator=g, device="cuda"), rand(n, outer)
+    y, z = torch.empty(n, outer, dtype=t, device="cuda"), torch.empty(n, outer, dtype=t, device="cuda")
+    dblp.linear(x, w, y, ws, bias=bias, activation="relu", residual=r, pre=z)
+    want, mag = big(x) @ big(w).T + big(bias), big(x).abs() @ big(w).abs().T + big(bias).abs()
+    near(z, want, mag, inner, t)
+    near(y, want.clamp(min=0) + big(r), mag + big(r).abs(), inner, t)
+    dx, base, pre = torch.empty(n, inner, dtype=t, device="cuda"), rand(n, inner), rand(n, inner)
+    dblp.linear_grad_input(dy, w, dx, ws, pre=pre, activation="relu", base=base)
+    on = (pre > 0).double()
+    near(dx, (big(dy) @ big(w)) * on + big(base), (big(dy).abs() @ big(w).abs()) * on + big(base).abs(), outer, t)
+    dw, db = torch.empty(outer, inner, device="cuda"), torch.empty(outer, device="cuda")
+    dblp.linear_grad_weight(dy, x, dw, ws, bias_grad=db)
+    near(dw, big(dy).T @ big(x), big(dy).abs().T @ big(x).abs(), n, torch.float32)
+    near(db, big(dy).sum(0), big(dy).abs().sum(0), n, torch.float32)
+    again, again_b = torch.empty_like(dw), torch.empty_like(db)
+    ws.fill_(255)
+    dblp.linear_grad_weight(dy, x, again, ws, bias_grad=again_b)
+    assert torch.equal(again, dw) and torch.equal(again_b, db)
+
+
+def test_a_weight_without_columns_has_a_bias():
+    import paper_2605_01989_amd as dblp
+    dy = torch.randn(300, 70, generator=gen(1), device="cuda")
+    db, ws = torch.empty(70, device="cuda"), space(dblp.linear_workspace(300, 0, 70))
+    dblp.linear_grad_weight(dy, torch.empty(300, 0, device="cuda"), torch.empty(70, 0, device="cuda"), ws, bias_grad=db)
+    close(db, d(dy).sum(0), 2 * 304 * U * d(dy).abs().sum(0), torch.float32)
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("t", TYPES)
 def test_activation_grad(t, act):
