@@ -18,7 +18,7 @@
  *
  * Products are summed in fp32 (of 16-bit values each product is exact), everything behind them is computed in fp32, and a result
  * is rounded once, to nearest even, when it is stored.  NaN and infinities go through the formulas.
- * Limits: tokens, columns and rows below 2^31.  Zero tokens, columns or rows are allowed: a sum of nothing is zero.
+ * Limits: tokens, columns and rows below 2^31, those of dblp_orthogonalize below 2^24.  Zero tokens, columns or rows are allowed: a sum of nothing is zero.
  * A workspace is DEVICE memory of the size that dblp_*_workspace gives, 256-byte aligned, of any contents; it is free
  * again when the stream has passed the call.  One of a larger call (more of any size) is large enough for a smaller one.
  */
@@ -82,8 +82,8 @@ int dblp_activation_grad(int device, void* stream, uint64_t rows, uint32_t cols,
  * with a, b, c = h_coefficients[3 k ...] in step k (NULL: 3.4445, -4.7750, 2.0315 in each, which take singular values of 0.01 and
  * above to 0.7 to 1.2 in five steps), and out = base_scale base + scale X (d_base NULL: scale X).  The orthogonalised update
  * of the Muon optimiser is this call on a momentum of gradients, with the weights as base and out.  G is of g_type, base and out of out_type.
- * X, A and b A + c A A are held with 22 significant bits.  Refused are steps above 16 and coefficients under which a singular value could
- * pass 32.  In place: out may be the base or G, with the same stride and step; out's matrices do not overlap. */
+ * X, A and a + b A + c A A are held with 22 significant bits, or to 2^-40 of the largest value that they can have, and multiplied so.  Refused are
+ * steps above 16 and coefficients under which a singular value could pass 32.  In place: out may be the base or G, with the same stride and step; out's matrices do not overlap. */
 int dblp_orthogonalize(int device, void* stream, uint64_t count, uint32_t rows, uint32_t cols, const void* d_g, uint64_t g_stride,
                        uint64_t g_step, int g_type, const double* h_coefficients, uint32_t steps, float scale, const void* d_base,
                        uint64_t base_stride, uint64_t base_step, float base_scale, void* d_out, uint64_t out_stride,

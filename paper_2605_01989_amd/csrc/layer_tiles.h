@@ -35,8 +35,10 @@ template <> __device__ __forceinline__ u4v ones<BF16>() { return (u4v)(0x3F803F8
 template <> __device__ __forceinline__ u4v ones<F16>() { return (u4v)(0x3C003C00u); }
 template <> __device__ __forceinline__ u4v ones<F32>() { return (u4v)(0x3F800000u); }
 
-// One operand of a batch of products: element (row, k) at row * stride + k, or at k * stride + row where it lies by k.
-struct Operand { const void* p; u64 stride, step; };
+// One operand of a batch of products: element (row, k) at row * stride + k, or at k * stride + row where it lies by k.  An operand in halves is two such matrices of
+// fp16, `low` elements apart, whose sum it is: 22 significant bits.  A product of two of those is three of the halves', high by high, high by low and low by
+// high, one behind the other in one sum over 3 k; what is left out is below the halves' own rounding.
+struct Operand { const void* p; u64 stride, step, low; };
 
 // What a launch computes: rows x cols results of sums over `depth` k, of which block z takes part z % parts of matrix z / parts.
 struct Product {
@@ -175,6 +177,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out
 #define STAGE_BYTES 128
 
 typedef u32 rsrc_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_readfirstlane((int)v); }
 #define PAST_ALL 0x80000000u                     // an offset that no buffer here reaches: a copy of it writes zeros
 
 // 64 lanes' 16 bytes at `offset` of a buffer to 1024 bytes of LDS at `to`.  No register is written, so nothing can be overwritten by it, and the compiler waits
@@ -189,7 +192,7 @@ template <int N> __device__ __forceinline__ void arrived_and_barrier() {
 __device__ __forceinline__ u32 lds_address(const void* p) { return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
 
 // An operand's way to LDS: BT rows and 128 bytes of k a stage, shared by WAVES waves.  STAGED: through registers, for rows that do not begin at multiples of 16 bytes.
-template <class T, int BT, bool BY_K, bool STAGED, int WAVES>
+template <class T, int BT, bool BY_K, bool STAGED, int WAVES, int HALVES = 0>
 struct Feed {
     typedef typename T::elem elem;
     static constexpr u32 E = 16 / sizeof(elem), KS = STAGE_BYTES / sizeof(elem);  // elements of a chunk, k of a stage
@@ -207,6 +210,20 @@ struct Feed {
     u32 r[BY_K && STAGED ? N : 1];                       // their rows
     u32 wave;
     u4v v[STAGED ? N : 1];
+    // HALVES 1, 2: as the first, the second operand of a product of halves, all of whose matrices end with whole stages
+    const elem* whole;
+    u64 low;
+    u32 third, k_in, product;    // k of one product of halves, where in it, and which
+    __device__ __forceinline__ void of_halves(const elem* p, u64 low_, u32 row0, u32 k0, u32 depth_) {
+        whole = p + (BY_K ? row0 : (u64)row0 * stride);
+        low = low_;
+        third = depth_ / 3;
+        product = k0 / third;
+        k_in = k0 - product * third;
+        left = ~0ull >> 1;
+        place();
+    }
+    __device__ __forceinline__ void place() { base = whole + (product == (HALVES == 1 ? 2 : 1) ? low : 0) + (BY_K ? (u64)k_in * stride : k_in); }
 
     static __device__ __forceinline__ u32 turn(u32 k) {
         const u32 t = sizeof(elem) == 2 ? (k & 3) | (k >> 3 & 1) << 2 : k >> 2 & 3;
@@ -234,6 +251,15 @@ struct Feed {
     }
     __device__ __forceinline__ void next() {
         const u64 by = BY_K ? KS * stride : KS;
+        if (HALVES) {
+            k += KS;
+            k_in += KS;
+            base += by;
+            if (k_in != third) return;
+            k_in = 0;
+            ++product;
+            return place();
+        }
         base += by;
         left -= by * sizeof(elem);
         k += KS;
@@ -243,7 +269,8 @@ struct Feed {
         const u64 at = (u64)base;
         const u32 bytes = left < PAST_ALL - 16 ? ((u32)left + 15) & ~15u : PAST_ALL;      // (a chunk that begins inside ends in the same 16 bytes of memory)
         const u32 rest = k < depth ? depth - k : 0;
-        const rsrc_t from = {(u32)at, (u32)(at >> 32), bytes, 0x00020000u};
+        // (the same in all lanes: the compiler does not see it through the turns of halves)
+        const rsrc_t from = {uniform((u32)at), uniform((u32)(at >> 32)), uniform(bytes), 0x00020000u};
         copy_to_lds(from, kk + i * KD < rest ? offset[i] : PAST_ALL, to + (wave * N + i) * 1024);
     }
     // Through registers: asked for, and put down later.
@@ -311,12 +338,12 @@ __device__ __forceinline__ void tile_of(u64 b, u64 n, u32 tile_rows, u32 tile_co
 // WR x WC waves, each 16 NM x 16 NN of the tile.
 template <int WR_, int WC_, int NM_, int NN_, int RING_> struct Waves { static constexpr int WR = WR_, WC = WC_, NM = NM_, NN = NN_, RING = RING_, BM = 16 * NM * WR, BN = 16 * NN * WC, ALL = WR * WC; };
 
-template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, class W, bool SUMS, class Out>
+template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, class W, bool SUMS, class Out, bool HALVES = false>
 __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out out) {
     typedef typename T::elem elem;
     constexpr int BM = W::BM, BN = W::BN, NM = W::NM, NN = W::NN, RING = W::RING;
-    typedef Feed<T, BM, P_BY_K, P_STAGED, W::ALL> FP;
-    typedef Feed<T, BN, Q_BY_K, Q_STAGED, W::ALL> FQ;
+    typedef Feed<T, BM, P_BY_K, P_STAGED, W::ALL, HALVES ? 1 : 0> FP;
+    typedef Feed<T, BN, Q_BY_K, Q_STAGED, W::ALL, HALVES ? 2 : 0> FQ;
     constexpr u32 KS = FP::KS, STAGE = FP::BYTES + FQ::BYTES, COPIES = FP::COPIES + FQ::COPIES;
     __shared__ __attribute__((aligned(1024))) uint8_t ring[RING * STAGE];
     u32 tm, tn;
@@ -331,6 +358,10 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
     f4 acc[NM][NN] = {}, sum = {};
     FP fp((const elem*)a.P.p + matrix * a.P.step, a.P.stride, m0, a.rows, k_first, k_end);
     FQ fq((const elem*)a.Q.p + matrix * a.Q.step, a.Q.stride, n0, a.cols, k_first, k_end);
+    if (HALVES) {
+        fp.of_halves((const elem*)a.P.p + matrix * a.P.step, a.P.low, m0, k_first, a.depth);
+        fq.of_halves((const elem*)a.Q.p + matrix * a.Q.step, a.Q.low, n0, k_first, a.depth);
+    }
     const Reader<T, BM, P_BY_K> rp(wm);
     const Reader<T, BN, Q_BY_K> rq(wn);
     const u32 ring_at = __builtin_amdgcn_readfirstlane(lds_address(ring));

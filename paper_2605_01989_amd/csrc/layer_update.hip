@@ -48,101 +48,136 @@ __device__ __forceinline__ double one_over_norm(const double* parts, u32 n) {
     return sum == 0.0 ? 0.0 : sum <= DBL_MAX ? 1.0 / sqrt(sum) : NAN;
 }
 
+// A value in halves: the nearest fp16 value, and the nearest one to what that leaves.  Both are of the value times a power of two that takes the largest one possible to 2^15, so that
+// a value keeps 22 bits, or 2^-40 of that largest one.
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+struct Halves { half4 high, low; };
+__device__ __forceinline__ Halves halves_of(const float (&v)[4]) {
+    Halves h;
+    for (int i = 0; i < 4; ++i) {
+        h.high[i] = (_Float16)v[i];
+        h.low[i] = (_Float16)(v[i] - (float)h.high[i]);
+    }
+    return h;
+}
+struct HalvesAt {
+    _Float16* p;
+    u64 stride, step, low;       // of rows, of matrices, from the high halves to the low ones
+    __device__ __forceinline__ void put(u64 matrix, u32 m, u32 n, const float (&v)[4]) const {
+        const Halves h = halves_of(v);
+        _Float16* const at = p + matrix * step + m * stride + n;
+        *(half4*)at = h.high;
+        *(half4*)(at + low) = h.low;
+    }
+    __device__ __forceinline__ Halves get(u64 matrix, u32 m, u32 n) const {
+        const _Float16* const at = p + matrix * step + m * stride + n;
+        return {*(const half4*)at, *(const half4*)(at + low)};
+    }
+};
+
+// X in halves, zeros behind its rows and columns.
 template <class T>
-__global__ __launch_bounds__(256) void scale_in(const typename T::elem* g, u64 stride, u64 step, Shape s, u64 matrix0, const double* parts, u32 n_parts, float* x) {
+__global__ __launch_bounds__(256) void scale_in(const typename T::elem* g, u64 stride, u64 step, Shape s, u64 matrix0, const double* parts, u32 n_parts, u32 rows, float up, HalvesAt x) {
     const u64 matrix = matrix0 + blockIdx.z;
-    const double q = one_over_norm(parts + matrix * n_parts, n_parts);
-    const u64 n = (u64)s.rows * s.cols;
+    const double q = one_over_norm(parts + matrix * n_parts, n_parts) * up;
+    const u32 units = (u32)(x.stride / 4);
+    const u64 n = (u64)rows * units;
     for (u64 i = (u64)blockIdx.x * 256 + threadIdx.x; i < n; i += (u64)gridDim.x * 256) {
-        const u64 row = i / s.cols, col = i % s.cols;
-        x[matrix * n + i] = (float)((double)(float)(s.tall ? g[matrix * step + col * stride + row] : g[matrix * step + row * stride + col]) * q);
+        const u32 row = (u32)(i / units), col = (u32)(i % units) * 4;
+        float v[4];
+        for (u32 e = 0; e < 4; ++e) v[e] = row < s.rows && col + e < s.cols ? (float)((double)(float)(s.tall ? g[matrix * step + (u64)(col + e) * stride + row] : g[matrix * step + (u64)row * stride + col + e]) * q) : 0.0f;
+        x.put(matrix, row, col, v);
     }
 }
 
 // ------------------------------------------------------------------------------------------
-// what becomes of the products' sums
+// what becomes of the products' sums: everything of X, A and b A + c A A is in halves, of padded rows and columns, whose sums are zeros
 // ------------------------------------------------------------------------------------------
 struct GramOut {
-    float* a;
-    u64 stride, step, matrix0;
+    HalvesAt a;
+    float by;                    // from the operands' powers of two to the result's
+    u64 matrix0;
     __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
-    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc, None) const {
-        const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-        store_cols<Vec<F32, 4>, 4>(a + (matrix0 + matrix) * step + m * stride, n, cols, v);
+    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32, f4 acc, None) const {
+        const float v[4] = {acc[0] * by, acc[1] * by, acc[2] * by, acc[3] * by};
+        a.put(matrix0 + matrix, m, n, v);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
 // a I + b A + c A A
 struct PolyOut {
-    const float* gram;
-    float* poly;
-    u64 stride, step, matrix0;
-    float a, b, c;
-    __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
-    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc, None) const {
-        const u64 at = (matrix0 + matrix) * step + m * stride;
+    HalvesAt gram, poly;
+    float a, b, c;               // (with the powers of two)
+    u32 rows;                    // without the padding
+    u64 matrix0;
+    __device__ __forceinline__ Halves get(u32 matrix, u32 m, u32 n, u32) const { return gram.get(matrix0 + matrix, m, n); }
+    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32, f4 acc, const Halves& g) const {
         float v[4];
-        get4<F32>(gram + at, n, cols, v);
-        for (int i = 0; i < 4; ++i) v[i] = b * v[i] + c * acc[i] + (n + i == m ? a : 0.0f);
-        store_cols<Vec<F32, 4>, 4>(poly + at, n, cols, v);
+        for (int i = 0; i < 4; ++i) v[i] = b * ((float)g.high[i] + (float)g.low[i]) + c * acc[i] + (n + i == m && m < rows ? a : 0.0f);
+        poly.put(matrix0 + matrix, m, n, v);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
-template <class T> struct UpdateOut {
-    typedef typename T::elem elem;
+struct UpdateOut {
+    int type;
     float scale, base_scale;
-    const elem* base;
+    const void* base;
     u64 base_stride, base_step;
-    elem* out;
+    void* out;
     u64 out_stride, out_step, matrix0;
-    __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
-    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc, None) const {
+    __device__ __forceinline__ u4v get(u32 matrix, u32 m, u32 n, u32 cols) const { return base ? raw4(type, base, (matrix0 + matrix) * base_step + m * base_stride + n, cols - n) : (u4v)(0u); }
+    __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32 cols, f4 acc, u4v met) const {
         float v[4], b[4];
         for (int i = 0; i < 4; ++i) v[i] = scale * acc[i];
         if (base) {
-            get4<T>(base + (matrix0 + matrix) * base_step + m * base_stride, n, cols, b);
+            open4(type, met, b);
             for (int i = 0; i < 4; ++i) v[i] += base_scale * b[i];
         }
-        store_cols<Vec<T, 4>, 4>(out + (matrix0 + matrix) * out_step + m * out_stride, n, cols, v);
+        store4(type, out, (matrix0 + matrix) * out_step + m * out_stride + n, cols - n, v);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
 
 // No step: X itself.
-template <class T>
-__global__ __launch_bounds__(256) void update_plain(const float* x, Shape s, UpdateOut<T> out) {
+__global__ __launch_bounds__(256) void update_plain(HalvesAt x, Shape s, UpdateOut out) {
     const u32 rows = s.tall ? s.cols : s.rows, cols = s.tall ? s.rows : s.cols;
-    const u64 units = (cols + 3ull) / 4, n = rows * units;
-    x += (out.matrix0 + blockIdx.z) * (u64)s.rows * s.cols;
+    const u64 units = (cols + 3ull) / 4, n = rows * units, matrix = out.matrix0 + blockIdx.z;
     for (u64 i = (u64)blockIdx.x * 256 + threadIdx.x; i < n; i += (u64)gridDim.x * 256) {
         const u32 m = (u32)(i / units), c = (u32)(i % units) * 4;
         f4 v = {};
-        for (u32 e = 0; e < 4; ++e) if (c + e < cols) v[e] = s.tall ? x[(u64)(c + e) * s.cols + m] : x[(u64)m * s.cols + c + e];
-        out.put(blockIdx.z, 0, m, c, cols, v, None());
+        for (u32 e = 0; e < 4; ++e)
+            if (c + e < cols) {
+                const _Float16* const at = x.p + matrix * x.step + (s.tall ? (c + e) * x.stride + m : m * x.stride + c + e);
+                v[e] = (float)at[0] + (float)at[x.low];
+            }
+        out.put(blockIdx.z, 0, m, c, cols, v, out.get(blockIdx.z, m, c, cols));
     }
 }
 
 // ------------------------------------------------------------------------------------------
 // C-ABI
 // ------------------------------------------------------------------------------------------
-struct Space { u64 parts, x[2], gram, poly, bytes; };
+// Where the matrices lie in the workspace, each as high and low halves of padded rows and columns, and the partial norms.
+struct Space { u64 rows, cols, parts, x[2], gram, poly, bytes; };
 
 static Space space_of(u64 count, u64 rows, u64 cols) {
     Space s = {};
     u64 at = 0;
-    const u64 r = rows < cols ? rows : cols;
     const auto take = [&](u64 bytes) { const u64 here = at; at += round_up(bytes, 256); return here; };
+    s.rows = round_up(rows < cols ? rows : cols, 64);
+    s.cols = round_up(rows < cols ? cols : rows, 64);
     s.parts = take(count * norm_blocks(rows * cols) * 8);
-    for (int i = 0; i < 2; ++i) s.x[i] = take(count * rows * cols * 4);
-    s.gram = take(count * r * r * 4);
-    s.poly = take(count * r * r * 4);
+    for (int i = 0; i < 2; ++i) s.x[i] = take(count * s.rows * s.cols * 4);
+    s.gram = take(count * s.rows * s.rows * 4);
+    s.poly = take(count * s.rows * s.rows * 4);
     s.bytes = at + 256;
     return s;
 }
 
-// Workspaces are held below 2^62 bytes: larger ones do not exist.
+// 64 rows' offsets fit 31 bits; workspaces are held below 2^60 bytes: larger ones do not exist.
+#define SIDE_LIMIT (1ull << 24)
 static bool out_of_range(u64 count, u64 rows, u64 cols) {
-    return count >= COUNT_LIMIT || rows >= COUNT_LIMIT || cols >= COUNT_LIMIT || (double)count * rows * cols > 1e16;
+    return count >= COUNT_LIMIT || rows >= SIDE_LIMIT || cols >= SIDE_LIMIT || (double)count * (rows + 64.0) * (cols + 64.0) > 1e16;
 }
 
 extern "C" uint64_t dblp_orthogonalize_workspace(uint64_t count, uint32_t rows, uint32_t cols) {
@@ -165,6 +200,17 @@ static double bound_after(const double* k, double most) {
     at((-3 * k[1] - sqrt(d)) / (10 * k[2]));
     return best;
 }
+
+// ... and |a + b q + c q^2|.
+static double poly_bound(const double* k, double most) {
+    const auto value = [&](double q) { return fabs(k[0] + q * (k[1] + q * k[2])); };
+    const double end = most * most, turn = k[2] != 0.0 ? -k[1] / (2 * k[2]) : 0.0;
+    double best = fmax(value(0.0), value(end));
+    if (turn > 0 && turn < end) best = fmax(best, value(turn));
+    return best;
+}
+// The power of two that takes values up to `most` to 2^15 and less: fp16 reaches past it.
+static double power_for(double most) { return most > 0 ? exp2(floor(15 - log2(most * (1 + 1e-5)))) : 1.0; }
 
 extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint32_t rows, uint32_t cols, const void* d_g, uint64_t g_stride,
                                   uint64_t g_step, int g_type, const double* h_coefficients, uint32_t steps, float scale, const void* d_base,
@@ -197,56 +243,65 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
     const Space at = space_of(count, rows, cols);
     uint8_t* const ws = (uint8_t*)d_workspace;
     double* const parts = (double*)(ws + at.parts);
-    float *x = (float*)(ws + at.x[0]), *next = (float*)(ws + at.x[1]);
-    float *const gram = (float*)(ws + at.gram), *const poly = (float*)(ws + at.poly);
+    const u64 values = at.rows * at.cols, square = at.rows * at.rows;
+    const auto halves = [&](u64 place, u64 cols) { return HalvesAt{(_Float16*)(ws + place), cols, 2 * at.rows * cols, at.rows * cols}; };
+    HalvesAt x = halves(at.x[0], at.cols), next = halves(at.x[1], at.cols);
+    const HalvesAt gram = halves(at.gram, at.rows), poly = halves(at.poly, at.rows);
     const bool tall = rows > cols;
     const Shape s = {tall ? cols : rows, tall ? rows : cols, tall};
-    const u64 values = (u64)rows * cols, square = (u64)s.rows * s.rows;
-    const u32 n_parts = norm_blocks(values);
+    const u32 n_parts = norm_blocks((u64)rows * cols);
     const auto each_matrix = [&](auto f) { for (u64 m = 0; m < count; m += 32768) f(m, (u32)(count - m < 32768 ? count - m : 32768)); };
+    double up = power_for(bounds[0]);
     each_matrix([&](u64 m, u32 n) {
         by_type(g_type, [&](auto tt) {
             typedef decltype(tt) T;
             typedef const typename T::elem* in;
             launch(norm_parts<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, rows, cols, m, parts);
-            launch(scale_in<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, x);
+            launch(scale_in<T>, dim3(norm_blocks(values), 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, (u32)at.rows, (float)up, x);
         });
     });
-    const auto product = [&](auto p_by_k, auto q_by_k, Operand P, Operand Q, u32 m_rows, u32 m_cols, u32 depth, auto out) {
+    // R = P Q^T for all matrices, summed over all k of the halves
+    const auto product = [&](auto p_by_k, auto q_by_k, const HalvesAt& P, const HalvesAt& Q, u64 m_rows, u64 m_cols, u64 depth, auto out) {
         constexpr bool PK = decltype(p_by_k)::value, QK = decltype(q_by_k)::value;
         typedef decltype(out) Out;
-        const Product a = {P, Q, m_rows, m_cols, depth, 0, (u32)round_up(depth, 64), 1};
-        each_tiles<64, 64>(a, count, [&](Product p, dim3 grid, u64 m) {
-            out.matrix0 = m;
-            p.P.p = (const float*)P.p + m * P.step;
-            p.Q.p = (const float*)Q.p + m * Q.step;
-            launch(tile_products<F32, PK, QK, 64, 64, false, Out>, grid, TILE_THREADS, st, p, out);
-        });
-    };
-    by_type(out_type, [&](auto tt) {
-        typedef decltype(tt) T;
-        typedef typename T::elem elem;
-        const UpdateOut<T> update = {scale, base_scale, (const elem*)d_base, base_stride, base_step, (elem*)d_out, out_stride, out_step, 0};
-        if (steps == 0) {
-            each_matrix([&](u64 m, u32 n) {
-                UpdateOut<T> u = update;
-                u.matrix0 = m;
-                launch(update_plain<T>, dim3(n_parts, 1, n), 256, st, (const float*)x, s, u);
+        const Product a = {{P.p, P.stride, P.step, P.low}, {Q.p, Q.stride, Q.step, Q.low}, (u32)m_rows, (u32)m_cols, (u32)(3 * depth), 0, (u32)(3 * depth), 1};
+        const auto go = [&](auto waves) {
+            typedef decltype(waves) W;
+            each_tiles<W::BM, W::BN>(a, count, [&](Product p, dim3 grid, u64 m) {
+                out.matrix0 = m;
+                p.P.p = P.p + m * P.step;
+                p.Q.p = Q.p + m * Q.step;
+                launch(ring_products<F16, PK, QK, false, false, W, false, Out, true>, grid, 64 * W::ALL, st, p, out);
             });
-            return;
-        }
-        for (u32 i = 0; i < steps; ++i) {
-            const double* k = h_coefficients ? h_coefficients + 3 * i : USUAL;
-            const Operand X = {x, s.cols, values}, A = {gram, s.rows, square}, P = {poly, s.rows, square};
-            product(Int<0>(), Int<0>(), X, X, s.rows, s.rows, s.cols, GramOut{gram, s.rows, square, 0});
-            product(Int<0>(), Int<0>(), A, A, s.rows, s.rows, s.rows, PolyOut{gram, poly, s.rows, square, 0, (float)k[0], (float)k[1], (float)k[2]});
-            if (i + 1 < steps) product(Int<0>(), Int<1>(), P, X, s.rows, s.cols, s.rows, GramOut{next, s.cols, values, 0});
-            else if (tall) product(Int<1>(), Int<0>(), X, P, s.cols, s.rows, s.rows, update);
-            else product(Int<0>(), Int<1>(), P, X, s.rows, s.cols, s.rows, update);
-            float* const t = x;
-            x = next;
-            next = t;
-        }
-    });
+        };
+        const u64 area = m_rows * m_cols * count;
+        const bool far = !in_reach<F16>(a.P) || !in_reach<F16>(a.Q);                      // (a tile of more rows would be out of reach)
+        if (far || area < 200ull * 128 * 128) go(Waves<2, 2, 2, 2, 3>());
+        else if (area < 120ull * 256 * 256) go(Waves<2, 2, 4, 4, 2>());
+        else go(Waves<2, 4, 8, 4, 2>());
+    };
+    UpdateOut update = {out_type, scale, base_scale, d_base, base_stride, base_step, d_out, out_stride, out_step, 0};
+    if (steps == 0) {
+        each_matrix([&](u64 m, u32 n) {
+            update.matrix0 = m;
+            update.scale = (float)(scale / up);
+            launch(update_plain, dim3(n_parts, 1, n), 256, st, x, s, update);
+        });
+        return launched(call, launch);
+    }
+    for (u32 i = 0; i < steps; ++i) {
+        const double* k = h_coefficients ? h_coefficients + 3 * i : USUAL;
+        const double gram_up = power_for(bounds[i] * bounds[i]), poly_up = power_for(poly_bound(k, bounds[i])), next_up = power_for(bounds[i + 1]);
+        product(Int<0>(), Int<0>(), x, x, at.rows, at.rows, at.cols, GramOut{gram, (float)(gram_up / (up * up)), 0});
+        product(Int<0>(), Int<0>(), gram, gram, at.rows, at.rows, at.rows, PolyOut{gram, poly, (float)(poly_up * k[0]), (float)(poly_up / gram_up * k[1]), (float)(poly_up / (gram_up * gram_up) * k[2]), s.rows, 0});
+        update.scale = (float)(scale / (poly_up * up));
+        if (i + 1 < steps) product(Int<0>(), Int<1>(), poly, x, at.rows, at.cols, at.rows, GramOut{next, (float)(next_up / (poly_up * up)), 0});
+        else if (tall) product(Int<1>(), Int<0>(), x, poly, s.cols, s.rows, at.rows, update);
+        else product(Int<0>(), Int<1>(), poly, x, s.rows, s.cols, at.rows, update);
+        up = next_up;
+        const HalvesAt t = x;
+        x = next;
+        next = t;
+    }
     return launched(call, launch);
 }
