@@ -173,11 +173,17 @@ __global__ __launch_bounds__(256) void column_sums(const typename T::elem* p, u6
         else out.sums(0, blockIdx.y, m, all);
     }
 }
-__global__ __launch_bounds__(256) void join_sums(PartOut in, u32 cols, u32 parts, WeightOut last) {
-    const u32 m = blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(64) void join_sums(PartOut in, u32 cols, u32 parts, WeightOut last) {
+    const u32 m = blockIdx.x * 64 + threadIdx.x;
     if (m >= cols) return;
     float sum = 0.0f;
-    for (u32 i = 0; i < parts; ++i) sum += in.row_sums[(u64)i * in.rows + m];
+    for (u32 i = 0; i < parts; i += 16) {
+        float v[16];
+#pragma unroll
+        for (u32 j = 0; j < 16; ++j) v[j] = i + j < parts ? in.row_sums[(u64)(i + j) * in.rows + m] : 0.0f;
+#pragma unroll
+        for (u32 j = 0; j < 16; ++j) sum += v[j];
+    }
     last.sums(0, 0, m, sum);
 }
 
@@ -258,10 +264,12 @@ static void tiles(Launches& launch, hipStream_t stream, Product a, Kind kind, Ou
         });
     };
     const auto by_place = [&](auto waves) {
-        const bool p = in_chunks<T>(a.P), q = in_chunks<T>(a.Q);
-        if (p && q) go(waves, Int<0>(), Int<0>());
-        else if (q) go(waves, Int<1>(), Int<0>());
-        else go(waves, Int<1>(), Int<1>());
+        const bool p = copied<T>(a.P), q = copied<T>(a.Q);
+        if (p && q) return go(waves, Int<0>(), Int<0>());
+        if constexpr (sizeof(typename T::elem) == 2) {
+            if (q) go(waves, Int<1>(), Int<0>());
+            else go(waves, Int<1>(), Int<1>());
+        }
     };
     if (!in_reach<T>(a.P) || !in_reach<T>(a.Q))
         each_tiles<64, 64>(a, 1, [&](const Product& p, dim3 grid, u64) { launch(tile_products<T, P_BY_K, Q_BY_K, 64, 64, SUMS, Out>, grid, TILE_THREADS, stream, p, out); });
@@ -293,7 +301,7 @@ static void products(Launches& launch, hipStream_t stream, Product a, Out out, v
             const u32 slice = (u32)round_up((a.depth + slices - 1) / slices, 8);
             slices = a.depth ? (a.depth + slice - 1) / slice : 1;
             launch(column_sums<T>, dim3(across, slices), 256, stream, (in)a.P.p, a.P.stride, a.depth, a.rows, slice, parts, out);
-            if (slices > 1) launch(join_sums, dim3((a.rows + 255) / 256), 256, stream, parts, a.rows, slices, out);
+            if (slices > 1) launch(join_sums, dim3((a.rows + 63) / 64), 64, stream, parts, a.rows, slices, out);
             row_sums = false;
             out.dbias = nullptr;
         }

@@ -191,7 +191,7 @@ template <int N> __device__ __forceinline__ void arrived_and_barrier() {
 
 __device__ __forceinline__ u32 lds_address(const void* p) { return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
 
-// An operand's way to LDS: BT rows and 128 bytes of k a stage, shared by WAVES waves.  STAGED: through registers, for rows that do not begin at multiples of 16 bytes.
+// An operand's way to LDS: BT rows and 128 bytes of k a stage, shared by WAVES waves.  STAGED: through registers, for rows of 16-bit values that do not begin at multiples of four bytes.
 template <class T, int BT, bool BY_K, bool STAGED, int WAVES, int HALVES = 0>
 struct Feed {
     typedef typename T::elem elem;
@@ -267,7 +267,7 @@ struct Feed {
     // The stage's copy number i of this wave, to LDS at `to`; k past the end as zeros.
     __device__ __forceinline__ void copy(u32 i, u32 to) const {
         const u64 at = (u64)base;
-        const u32 bytes = left < PAST_ALL - 16 ? ((u32)left + 15) & ~15u : PAST_ALL;      // (a chunk that begins inside ends in the same 16 bytes of memory)
+        const u32 bytes = left < PAST_ALL - 4 ? ((u32)left + 3) & ~3u : PAST_ALL;        // (a chunk that goes past the operand's end brings zeros from there)
         const u32 rest = k < depth ? depth - k : 0;
         // (the same in all lanes: the compiler does not see it through the turns of halves)
         const rsrc_t from = {uniform((u32)at), uniform((u32)(at >> 32)), uniform(bytes), 0x00020000u};
@@ -556,9 +556,9 @@ static void each_tiles(Product a, u64 matrices, F f) {
     }
 }
 
-// Whether an operand can be copied to LDS chunk by chunk, and whether a tile's offsets fit 31 bits.
-template <class T> static bool in_chunks(const Operand& o) {
+// Whether an operand can be copied to LDS (its chunks begin at multiples of four bytes, as any float does), and whether a tile's offsets fit 31 bits.
+template <class T> static bool copied(const Operand& o) {
     const u64 e = sizeof(typename T::elem);
-    return !off(o.p, 16) && o.stride * e % 16 == 0 && o.step * e % 16 == 0;
+    return !off(o.p, 4) && o.stride * e % 4 == 0 && o.step * e % 4 == 0;
 }
 template <class T> static bool in_reach(const Operand& o) { return o.stride < (1ull << 31) / 256 / sizeof(typename T::elem); }

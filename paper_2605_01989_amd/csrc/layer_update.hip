@@ -13,7 +13,7 @@ struct Matrices { const void* p; u64 stride, step; };
 // ------------------------------------------------------------------------------------------
 // X = G / |G|
 // ------------------------------------------------------------------------------------------
-#define NORM_EACH 16384                          // values of a block
+#define NORM_EACH 4096                           // values of a block
 #define NORM_MOST 256                            // blocks of a matrix
 static u32 norm_blocks(u64 values) {
     const u64 n = (values + NORM_EACH - 1) / NORM_EACH;
@@ -28,16 +28,31 @@ __device__ __forceinline__ double block_sum(double v) {
     return sh[0] + sh[1] + sh[2] + sh[3];
 }
 
-// Sums of squares of rows blockIdx.x, + gridDim.x, ...: in fp64, where neither a square nor a sum of them leaves the range.
+// Sums of squares, in fp64, where neither a square nor a sum of them leaves the range.  `across` threads, a power of two, take a row, four values each at a time; a
+// thread has four rows' on their way.
 template <class T>
-__global__ __launch_bounds__(256) void norm_parts(const typename T::elem* g, u64 stride, u64 step, u32 rows, u32 cols, u64 matrix0, double* parts) {
+__global__ __launch_bounds__(256) void norm_parts(const typename T::elem* g, u64 stride, u64 step, u32 rows, u32 cols, u32 across, u64 matrix0, double* parts) {
+    typedef Vec<T, 4> V;
     const u64 matrix = matrix0 + blockIdx.z;
-    const u64 n = (u64)rows * cols;
+    const u32 down = 256 / across, x = threadIdx.x % across, y = threadIdx.x / across, turn = gridDim.x * down;
+    g += matrix * step;
     double sum = 0;
-    for (u64 i = (u64)blockIdx.x * 256 + threadIdx.x; i < n; i += (u64)gridDim.x * 256) {
-        const double v = (double)(float)g[matrix * step + i / cols * stride + i % cols];
-        sum += v * v;
-    }
+    for (u64 row = blockIdx.x * down + y; row < rows; row += 4ull * turn)
+        for (u32 c = x * 4; c < cols; c += across * 4) {
+            typename V::raw r[4];
+#pragma unroll
+            for (u32 i = 0; i < 4; ++i) {
+                r[i] = (typename V::raw)(0);
+                const u64 at = row + (u64)i * turn;
+                if (at < rows) r[i] = c + 4 <= cols ? V::load(g + at * stride + c) : V::some(g + at * stride + c, cols - c);
+            }
+#pragma unroll
+            for (u32 i = 0; i < 4; ++i) {
+                float v[4];
+                V::open(r[i], v);
+                for (int e = 0; e < 4; ++e) sum += (double)v[e] * (double)v[e];
+            }
+        }
     sum = block_sum(sum);
     if (threadIdx.x == 0) parts[matrix * gridDim.x + blockIdx.x] = sum;
 }
@@ -75,18 +90,41 @@ struct HalvesAt {
     }
 };
 
-// X in halves, zeros behind its rows and columns.
+// X in halves, zeros behind its rows and columns: a block takes 64 x 64 of them, through LDS where G is turned.
 template <class T>
-__global__ __launch_bounds__(256) void scale_in(const typename T::elem* g, u64 stride, u64 step, Shape s, u64 matrix0, const double* parts, u32 n_parts, u32 rows, float up, HalvesAt x) {
+__global__ __launch_bounds__(256) void scale_in(const typename T::elem* g, u64 stride, u64 step, Shape s, u64 matrix0, const double* parts, u32 n_parts, float up, HalvesAt x) {
+    typedef Vec<T, 4> V;
+    __shared__ float turned[64][65];
     const u64 matrix = matrix0 + blockIdx.z;
+    const u32 row0 = blockIdx.y * 64, col0 = blockIdx.x * 64, down = threadIdx.x / 16, across = threadIdx.x % 16 * 4;
+    const u32 g_rows = s.tall ? s.cols : s.rows, g_cols = s.tall ? s.rows : s.cols, g_row = (s.tall ? col0 : row0) + down, g_col = (s.tall ? row0 : col0) + across;
+    g += matrix * step;
+    typename V::raw r[4];
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+        r[i] = (typename V::raw)(0);
+        const typename T::elem* const at = g + (u64)(g_row + 16 * i) * stride + g_col;
+        if (g_row + 16 * i < g_rows && g_col < g_cols) r[i] = g_col + 4 <= g_cols ? V::load(at) : V::some(at, g_cols - g_col);
+    }
     const double q = one_over_norm(parts + matrix * n_parts, n_parts) * up;
-    const u32 units = (u32)(x.stride / 4);
-    const u64 n = (u64)rows * units;
-    for (u64 i = (u64)blockIdx.x * 256 + threadIdx.x; i < n; i += (u64)gridDim.x * 256) {
-        const u32 row = (u32)(i / units), col = (u32)(i % units) * 4;
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
         float v[4];
-        for (u32 e = 0; e < 4; ++e) v[e] = row < s.rows && col + e < s.cols ? (float)((double)(float)(s.tall ? g[matrix * step + (u64)(col + e) * stride + row] : g[matrix * step + (u64)row * stride + col + e]) * q) : 0.0f;
-        x.put(matrix, row, col, v);
+        V::open(r[i], v);
+        // (zeros behind the matrix stay zeros where the norm is NaN)
+        for (int e = 0; e < 4; ++e) v[e] = g_row + 16 * i < g_rows && g_col + e < g_cols ? (float)((double)v[e] * q) : 0.0f;
+        if (s.tall)
+            for (int e = 0; e < 4; ++e) turned[across + e][down + 16 * i] = v[e];
+        else
+            x.put(matrix, row0 + down + 16 * i, col0 + across, v);
+    }
+    if (!s.tall) return;
+    __syncthreads();
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+        float v[4];
+        for (int e = 0; e < 4; ++e) v[e] = turned[down + 16 * i][across + e];
+        x.put(matrix, row0 + down + 16 * i, col0 + across, v);
     }
 }
 
@@ -252,12 +290,15 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
     const u32 n_parts = norm_blocks((u64)rows * cols);
     const auto each_matrix = [&](auto f) { for (u64 m = 0; m < count; m += 32768) f(m, (u32)(count - m < 32768 ? count - m : 32768)); };
     double up = power_for(bounds[0]);
+    u32 across = 1;
+    while (across < 256 && across * 4 < cols) across *= 2;
     each_matrix([&](u64 m, u32 n) {
         by_type(g_type, [&](auto tt) {
             typedef decltype(tt) T;
             typedef const typename T::elem* in;
-            launch(norm_parts<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, rows, cols, m, parts);
-            launch(scale_in<T>, dim3(norm_blocks(values), 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, (u32)at.rows, (float)up, x);
+            launch(norm_parts<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, rows, cols, across, m, parts);
+            // (a grid has at most 2^16 blocks that way: 64 rows each are more than there are of the shorter side)
+            launch(scale_in<T>, dim3((u32)(at.cols / 64), (u32)(at.rows / 64), n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, (float)up, x);
         });
     });
     // R = P Q^T for all matrices, summed over all k of the halves
@@ -285,7 +326,7 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
         each_matrix([&](u64 m, u32 n) {
             update.matrix0 = m;
             update.scale = (float)(scale / up);
-            launch(update_plain, dim3(n_parts, 1, n), 256, st, x, s, update);
+            launch(update_plain, dim3(norm_blocks(values), 1, n), 256, st, x, s, update);
         });
         return launched(call, launch);
     }
