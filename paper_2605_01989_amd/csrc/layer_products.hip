@@ -278,8 +278,39 @@ static void tiles(Launches& launch, hipStream_t stream, Product a, Kind kind, Ou
     else if constexpr (sizeof(typename T::elem) == 2) by_place(Waves<2, 4, 8, 4, 2>());
 }
 
+// Few rows, where a block reads little more of P than of Q, or there are few blocks: with 16 rows of 4096 values and 16384 columns P's reading takes over (34 us, by tiles 25; with
+// 4 rows 25).  In parts that make 512 blocks, of at least two turns of a block's waves each.
+static bool few_rows(u64 rows, u64 cols) { return rows <= 4 || (rows <= 16 && cols <= 8192); }
+template <class T, class Out>
+static void few(Launches& launch, hipStream_t stream, Product a, Out out, PartOut parts) {
+    constexpr u32 TURN = FEW_WAVES * 128 / sizeof(typename T::elem);
+    const u64 blocks = (a.cols + 15ull) / 16, bytes = a.rows * parts.stride * 4;
+    u64 p = 512 / blocks;
+    if (p > a.depth / (2 * TURN)) p = a.depth / (2 * TURN);
+    if (p > PARTS_MOST) p = PARTS_MOST;
+    if (p * bytes > PARTS_BYTES) p = PARTS_BYTES / bytes;
+    a.part = a.depth;
+    a.parts = 1;
+    if (p > 1) {
+        a.part = (u32)round_up((a.depth + p - 1) / p, TURN);
+        a.parts = (a.depth + a.part - 1) / a.part;
+    }
+    for (a.tile0 = 0; a.tile0 < blocks; a.tile0 += 1u << 20) {
+        const dim3 grid((u32)(blocks - a.tile0 < (1u << 20) ? blocks - a.tile0 : 1u << 20), 1, a.parts);
+        if (a.parts == 1) launch(few_products<T, Out>, grid, 64 * FEW_WAVES, stream, a, out);
+        else launch(few_products<T, PartOut>, grid, 64 * FEW_WAVES, stream, a, parts);
+    }
+    if (a.parts > 1) each_launch<4>(a.rows, a.cols, [&](Units s) { launch(join_parts<Out>, dim3(blocks_of(s.n, 256)), 256, stream, parts, s, a.parts, out); });
+}
+
 template <class T, bool P_BY_K, bool Q_BY_K, bool SUMS, class Out>
 static void products(Launches& launch, hipStream_t stream, Product a, Out out, void* workspace) {
+    if constexpr (!P_BY_K && !Q_BY_K) {
+        if (few_rows(a.rows, a.cols)) {
+            const u64 stride = round_up(a.cols, 4);
+            return few<T>(launch, stream, a, out, PartOut{(float*)workspace, stride, a.rows * stride, nullptr, a.rows});
+        }
+    }
     Way w = way_of(a.rows, a.cols, a.depth, sizeof(typename T::elem));
     if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0};
     a.parts = w.parts;

@@ -491,6 +491,52 @@ __device__ __forceinline__ void get4(const typename T::elem* row, u32 n, u32 col
     V::open(n + 4 <= cols ? V::load(row + n) : V::some(row + n, cols - n), v);
 }
 
+// ------------------------------------------------------------------------------------------
+// At most 16 rows (tokens that are decoded): the weights are read once, from memory straight into the matrix instructions' registers.  A block makes 16 columns of all rows; its
+// waves share k, 128 bytes of it at a time, and add their sums up in LDS.  Bound by the reading of Q; P comes from the caches.
+// ------------------------------------------------------------------------------------------
+#define FEW_WAVES 16
+template <class T, class Out>
+__global__ __launch_bounds__(64 * FEW_WAVES) void few_products(Product a, Out out) {
+    typedef typename T::elem elem;
+    constexpr u32 E = 16 / sizeof(elem), KS = 128 / sizeof(elem);
+    typedef Vec<T, E> V;
+    __shared__ f4 sums[FEW_WAVES][64];
+    const u32 n0 = (u32)(a.tile0 + blockIdx.x) * 16, part = blockIdx.z;
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4, in_group = lane & 15;
+    const u32 k_first = part * a.part, k_end = a.depth - k_first > a.part ? k_first + a.part : a.depth;
+    const elem* const p = (const elem*)a.P.p + (in_group < a.rows ? in_group : a.rows - 1) * a.P.stride;
+    const elem* const q = (const elem*)a.Q.p + (n0 + in_group < a.cols ? n0 + in_group : a.cols - 1) * a.Q.stride;
+    f4 acc = {};
+    // A lane's chunks of 128 bytes of k: number `group` of the first and of the second half.
+    const auto step = [&](u32 k, auto whole) {
+        u4v b[2], c[2];
+        const auto get = [&](const elem* row, u32 at) {
+            if (decltype(whole)::value || at + E <= k_end) return __builtin_bit_cast(u4v, V::load(row + at));
+            return at < k_end ? __builtin_bit_cast(u4v, V::some(row + at, k_end - at)) : (u4v)(0u);
+        };
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            c[h] = get(q, k + h * (KS / 2) + group * E);
+            b[h] = get(p, k + h * (KS / 2) + group * E);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) acc = mfma<T>(c[h], b[h], acc);
+    };
+    u32 k = k_first + wave * KS;
+#pragma unroll 4
+    for (; k + KS <= k_end; k += FEW_WAVES * KS) step(k, Int<1>());
+    if (k < k_end) step(k, Int<0>());
+    sums[wave][lane] = acc;
+    __syncthreads();
+    const u32 m = in_group, n = n0 + group * 4;
+    if (wave != 0 || m >= a.rows || n >= a.cols) return;
+    const auto met = out.get(0, m, n, a.cols);
+#pragma unroll
+    for (int w = 1; w < FEW_WAVES; ++w) acc += sums[w][lane];
+    out.put(0, part, m, n, a.cols, acc, met);
+}
+
 // What memory holds for four columns of a row, as it lies there, so that several can be on their way: 16 bytes of floats or 8 of 16-bit values, by a type that is known
 // when the kernel runs.
 __device__ __forceinline__ u4v raw4(int type, const void* p, u64 at, u32 left) {

@@ -126,7 +126,8 @@ def big(t):
 
 
 # tokens, in, out, padding: whole large tiles, ragged ones on aligned rows, odd rows, sums in many parts, sums that end inside a chunk
-LARGE = [(4096, 128, 4096, 0), (3333, 200, 4600, 0), (4000, 77, 4099, 3), (4099, 65, 4000, 0), (700, 5000, 800, 0), (129, 9001, 130, 7), (2050, 100, 9000, 1), (260, 3000, 50257, 0)]
+LARGE = [(4096, 128, 4096, 0), (3333, 200, 4600, 0), (4000, 77, 4099, 3), (4099, 65, 4000, 0), (700, 5000, 800, 0), (129, 9001, 130, 7), (2050, 100, 9000, 1), (260, 3000, 50257, 0),
+         (1, 4096, 4096, 0), (1, 20000, 70, 0), (7, 9001, 50, 5), (16, 1000, 5003, 0), (17, 3001, 900, 0), (32, 512, 4097, 3), (33, 16384, 33, 0), (64, 2049, 1030, 1), (65, 2049, 1030, 1)]
 
 
 @pytest.mark.parametrize("n, inner, outer, pad", LARGE)
