@@ -176,6 +176,175 @@ struct UpdateOut {
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
 
+// ------------------------------------------------------------------------------------------
+// Small matrices, X of at most 64 R x 64 N: a block takes one through all of its steps, X and then A, then a + b A + c A A, in halves in LDS.  Eight waves, four by two, each 16 R x
+// 32 columns of A and 16 R x 32 N of X.  What bounds it is the way from one product to the next: reading, multiplying, a barrier, writing.
+// A row in LDS is 128 bytes for each 64 values, chunk c of 16 bytes of row r at c ^ (r & 7).
+// ------------------------------------------------------------------------------------------
+template <int WIDTH> __device__ __forceinline__ u32 small_at(u32 row, u32 col) { return row * (WIDTH * 2) + (((col >> 3) ^ (row & 7)) << 4) + (col & 7) * 2; }
+
+// 16 rows' (or, by k, columns') 32 k of a matrix in LDS.
+template <int WIDTH>
+__device__ __forceinline__ u4v small_rows(const uint8_t* m, u32 row0, u32 k0) {
+    const u32 lane = threadIdx.x & 63;
+    return *(const u4v*)(m + small_at<WIDTH>(row0 + (lane & 15), k0 + (lane >> 4) * 8));
+}
+template <int WIDTH>
+__device__ __forceinline__ u4v small_columns(const uint8_t* m, u32 col0, u32 k0) {
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s4* lds;
+    const u32 lane = threadIdx.x & 63, k = k0 + (lane >> 4) * 8 + ((lane & 15) >> 2), col = col0 + (lane & 3) * 4;
+    const u2v a = __builtin_bit_cast(u2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(m + small_at<WIDTH>(k, col)))), b = __builtin_bit_cast(u2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(m + small_at<WIDTH>(k + 4, col))));
+    return (u4v){a.x, a.y, b.x, b.y};
+}
+template <int WIDTH>
+__device__ __forceinline__ void small_put(uint8_t* m, u32 low, u32 row, u32 col, const float (&v)[4]) {
+    const Halves h = halves_of(v);
+    *(half4*)(m + small_at<WIDTH>(row, col)) = h.high;
+    *(half4*)(m + low + small_at<WIDTH>(row, col)) = h.low;
+}
+
+// high by high, high by low, low by high: each a round over the results, whose sums wait for each other.  TURNED: a result's rows and columns change places.
+template <int R, int C, bool TURNED = false>
+__device__ __forceinline__ void add_halves(f4 (&acc)[R][C], const u4v (&bh)[R], const u4v (&bl)[R], const u4v (&ch)[C], const u4v (&cl)[C]) {
+    const auto round = [&](const u4v (&b)[R], const u4v (&c)[C]) {
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+            for (int e = 0; e < R; ++e) acc[e][j] = TURNED ? mfma<F16>(b[e], c[j], acc[e][j]) : mfma<F16>(c[j], b[e], acc[e][j]);
+    };
+    round(bh, ch);
+    round(bl, ch);
+    round(bh, cl);
+}
+
+struct SmallSteps { float gram[STEPS_MOST], a[STEPS_MOST], b[STEPS_MOST], c[STEPS_MOST], next[STEPS_MOST]; u32 n; };
+
+template <class T, int R, int N>
+__global__ __launch_bounds__(512) void small_steps(const typename T::elem* g, u64 stride, u64 step, Shape s, float up, SmallSteps k, UpdateOut out) {
+    typedef Vec<T, 4> V;
+    constexpr u32 ROWS = 64 * R, COLS = 64 * N, X_LOW = ROWS * COLS * 2, A_LOW = ROWS * ROWS * 2;
+    __shared__ __attribute__((aligned(16))) uint8_t x[2 * X_LOW];
+    __shared__ __attribute__((aligned(16))) uint8_t m[2 * A_LOW];
+    __shared__ double norms[8];
+    const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, in_group = lane & 15;
+    const u64 matrix = out.matrix0 + blockIdx.x;
+    g += matrix * step;
+    const u32 g_rows = s.tall ? s.cols : s.rows, g_cols = s.tall ? s.rows : s.cols, G_COLS = s.tall ? ROWS : COLS;
+    constexpr int UNROLL = 2;
+    constexpr u32 EACH = ROWS * COLS / 2048;           // pieces of four values of a thread
+    typename V::raw r[EACH];
+    double sum = 0;
+#pragma unroll
+    for (u32 i = 0; i < EACH; ++i) {
+        const u32 u = threadIdx.x + i * 512, row = u / (G_COLS / 4), col = u % (G_COLS / 4) * 4;
+        r[i] = (typename V::raw)(0);
+        if (row < g_rows && col < g_cols) r[i] = col + 4 <= g_cols ? V::load(g + row * stride + col) : V::some(g + row * stride + col, g_cols - col);
+    }
+#pragma unroll
+    for (u32 i = 0; i < EACH; ++i) {
+        float v[4];
+        V::open(r[i], v);
+        for (int e = 0; e < 4; ++e) sum += (double)v[e] * (double)v[e];
+    }
+    for (int d = 32; d; d >>= 1) sum += __shfl_down(sum, d);
+    if (lane == 0) norms[wave] = sum;
+    __syncthreads();
+    sum = 0;
+    for (int i = 0; i < 8; ++i) sum += norms[i];
+    const double q = (sum == 0.0 ? 0.0 : sum <= DBL_MAX ? 1.0 / sqrt(sum) : NAN) * up;
+#pragma unroll
+    for (u32 i = 0; i < EACH; ++i) {
+        const u32 u = threadIdx.x + i * 512, row = u / (G_COLS / 4), col = u % (G_COLS / 4) * 4;
+        float v[4];
+        V::open(r[i], v);
+        for (int e = 0; e < 4; ++e) v[e] = row < g_rows && col + e < g_cols ? (float)((double)v[e] * q) : 0.0f;
+        if (!s.tall) small_put<COLS>(x, X_LOW, row, col, v);
+        else
+            for (int e = 0; e < 4; ++e) {
+                const _Float16 high = (_Float16)v[e];
+                *(_Float16*)(x + small_at<COLS>(col + e, row)) = high;
+                *(_Float16*)(x + X_LOW + small_at<COLS>(col + e, row)) = (_Float16)(v[e] - (float)high);
+            }
+    }
+    const u32 m0 = wave / 2 * 16 * R, an0 = wave % 2 * 32 * R, xn0 = wave % 2 * 32 * N;
+    for (u32 i = 0; i < k.n; ++i) {
+        __syncthreads();
+        // A = X X^T
+        f4 acc[R][2 * R] = {};
+        const auto square = [&](const uint8_t* of, u32 low, u32 width, auto get) {
+#pragma unroll UNROLL
+            for (u32 k0 = 0; k0 < width; k0 += 32) {
+                u4v bh[R], bl[R], ch[2 * R], cl[2 * R];
+#pragma unroll
+                for (int e = 0; e < R; ++e) { bh[e] = get(of, m0 + 16 * e, k0); bl[e] = get(of + low, m0 + 16 * e, k0); }
+#pragma unroll
+                for (int j = 0; j < 2 * R; ++j) { ch[j] = get(of, an0 + 16 * j, k0); cl[j] = get(of + low, an0 + 16 * j, k0); }
+                add_halves<R, 2 * R>(acc, bh, bl, ch, cl);
+            }
+        };
+        square(x, X_LOW, COLS, [](const uint8_t* of, u32 row, u32 k0) { return small_rows<COLS>(of, row, k0); });
+        Halves own[R][2 * R];                          // of A: a wave's part of A A is at the same places
+#pragma unroll
+        for (int e = 0; e < R; ++e)
+#pragma unroll
+            for (int j = 0; j < 2 * R; ++j) {
+                float v[4];
+                for (int t = 0; t < 4; ++t) v[t] = acc[e][j][t] * k.gram[i];
+                own[e][j] = halves_of(v);
+                const u32 row = m0 + 16 * e + in_group, col = an0 + 16 * j + group * 4;
+                *(half4*)(m + small_at<ROWS>(row, col)) = own[e][j].high;
+                *(half4*)(m + A_LOW + small_at<ROWS>(row, col)) = own[e][j].low;
+                acc[e][j] = (f4)(0.0f);
+            }
+        __syncthreads();
+        square(m, A_LOW, ROWS, [](const uint8_t* of, u32 row, u32 k0) { return small_rows<ROWS>(of, row, k0); });
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < R; ++e)
+#pragma unroll
+            for (int j = 0; j < 2 * R; ++j) {
+                const u32 row = m0 + 16 * e + in_group, col = an0 + 16 * j + group * 4;
+                float v[4];
+                for (int t = 0; t < 4; ++t) v[t] = k.b[i] * ((float)own[e][j].high[t] + (float)own[e][j].low[t]) + k.c[i] * acc[e][j][t] + (col + t == row && row < s.rows ? k.a[i] : 0.0f);
+                small_put<ROWS>(m, A_LOW, row, col, v);
+            }
+        __syncthreads();
+        // X = (a + b A + c A A) X; of a turned matrix the last one turned back
+        const bool last = i + 1 == k.n;
+        f4 next[R][2 * N] = {};
+#pragma unroll UNROLL
+        for (u32 k0 = 0; k0 < ROWS; k0 += 32) {
+            u4v bh[R], bl[R], ch[2 * N], cl[2 * N];
+#pragma unroll
+            for (int e = 0; e < R; ++e) { bh[e] = small_rows<ROWS>(m, m0 + 16 * e, k0); bl[e] = small_rows<ROWS>(m + A_LOW, m0 + 16 * e, k0); }
+#pragma unroll
+            for (int j = 0; j < 2 * N; ++j) { ch[j] = small_columns<COLS>(x, xn0 + 16 * j, k0); cl[j] = small_columns<COLS>(x + X_LOW, xn0 + 16 * j, k0); }
+            if (last && s.tall) add_halves<R, 2 * N, true>(next, bh, bl, ch, cl);
+            else add_halves<R, 2 * N>(next, bh, bl, ch, cl);
+        }
+        if (!last) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < R; ++e)
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j) {
+                    float v[4];
+                    for (int t = 0; t < 4; ++t) v[t] = next[e][j][t] * k.next[i];
+                    small_put<COLS>(x, X_LOW, m0 + 16 * e + in_group, xn0 + 16 * j + group * 4, v);
+                }
+            continue;
+        }
+#pragma unroll
+        for (int e = 0; e < R; ++e)
+#pragma unroll
+            for (int j = 0; j < 2 * N; ++j) {
+                const u32 row = s.tall ? xn0 + 16 * j + in_group : m0 + 16 * e + in_group, col = s.tall ? m0 + 16 * e + group * 4 : xn0 + 16 * j + group * 4;
+                if (row < g_rows && col < g_cols) out.put(blockIdx.x, 0, row, col, g_cols, next[e][j], out.get(blockIdx.x, row, col, g_cols));
+            }
+    }
+}
+
 // No step: X itself.
 __global__ __launch_bounds__(256) void update_plain(HalvesAt x, Shape s, UpdateOut out) {
     const u32 rows = s.tall ? s.cols : s.rows, cols = s.tall ? s.rows : s.cols;
@@ -289,7 +458,37 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
     const Shape s = {tall ? cols : rows, tall ? rows : cols, tall};
     const u32 n_parts = norm_blocks((u64)rows * cols);
     const auto each_matrix = [&](auto f) { for (u64 m = 0; m < count; m += 32768) f(m, (u32)(count - m < 32768 ? count - m : 32768)); };
-    double up = power_for(bounds[0]);
+    UpdateOut update = {out_type, scale, base_scale, d_base, base_stride, base_step, d_out, out_stride, out_step, 0};
+    // what step i multiplies its products' sums by: from the operands' powers of two to the result's
+    SmallSteps by = {};
+    by.n = steps;
+    for (u32 i = 0; i < steps; ++i) {
+        const double* k = h_coefficients ? h_coefficients + 3 * i : USUAL;
+        const double x_up = power_for(bounds[i]), gram_up = power_for(bounds[i] * bounds[i]), poly_up = power_for(poly_bound(k, bounds[i])), next_up = power_for(bounds[i + 1]);
+        by.gram[i] = (float)(gram_up / (x_up * x_up));
+        by.a[i] = (float)(poly_up * k[0]);
+        by.b[i] = (float)(poly_up / gram_up * k[1]);
+        by.c[i] = (float)(poly_up / (gram_up * gram_up) * k[2]);
+        by.next[i] = (float)(next_up / (poly_up * x_up));
+        update.scale = (float)(scale / (poly_up * x_up));
+    }
+    const float up = (float)power_for(bounds[0]);
+    if (steps == 0) update.scale = (float)(scale / up);
+    if (steps && at.cols <= 128) {
+        by_type(g_type, [&](auto tt) {
+            typedef decltype(tt) T;
+            const auto go = [&](auto kernel) {
+                for (u64 m = 0; m < count; m += 1u << 20) {
+                    update.matrix0 = m;
+                    launch(kernel, dim3((u32)(count - m < (1u << 20) ? count - m : 1u << 20)), 512, st, (const typename T::elem*)d_g, (u64)g_stride, (u64)g_step, s, up, by, update);
+                }
+            };
+            if (at.cols == 64) go(small_steps<T, 1, 1>);
+            else if (at.rows == 64) go(small_steps<T, 1, 2>);
+            else go(small_steps<T, 2, 2>);
+        });
+        return launched(call, launch);
+    }
     u32 across = 1;
     while (across < 256 && across * 4 < cols) across *= 2;
     each_matrix([&](u64 m, u32 n) {
@@ -298,7 +497,7 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
             typedef const typename T::elem* in;
             launch(norm_parts<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, rows, cols, across, m, parts);
             // (a grid has at most 2^16 blocks that way: 64 rows each are more than there are of the shorter side)
-            launch(scale_in<T>, dim3((u32)(at.cols / 64), (u32)(at.rows / 64), n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, (float)up, x);
+            launch(scale_in<T>, dim3((u32)(at.cols / 64), (u32)(at.rows / 64), n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, up, x);
         });
     });
     // R = P Q^T for all matrices, summed over all k of the halves
@@ -321,25 +520,17 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
         else if (area < 120ull * 256 * 256) go(Waves<2, 2, 4, 4, 2>());
         else go(Waves<2, 4, 8, 4, 2>());
     };
-    UpdateOut update = {out_type, scale, base_scale, d_base, base_stride, base_step, d_out, out_stride, out_step, 0};
-    if (steps == 0) {
+    if (steps == 0)
         each_matrix([&](u64 m, u32 n) {
             update.matrix0 = m;
-            update.scale = (float)(scale / up);
             launch(update_plain, dim3(norm_blocks(values), 1, n), 256, st, x, s, update);
         });
-        return launched(call, launch);
-    }
     for (u32 i = 0; i < steps; ++i) {
-        const double* k = h_coefficients ? h_coefficients + 3 * i : USUAL;
-        const double gram_up = power_for(bounds[i] * bounds[i]), poly_up = power_for(poly_bound(k, bounds[i])), next_up = power_for(bounds[i + 1]);
-        product(Int<0>(), Int<0>(), x, x, at.rows, at.rows, at.cols, GramOut{gram, (float)(gram_up / (up * up)), 0});
-        product(Int<0>(), Int<0>(), gram, gram, at.rows, at.rows, at.rows, PolyOut{gram, poly, (float)(poly_up * k[0]), (float)(poly_up / gram_up * k[1]), (float)(poly_up / (gram_up * gram_up) * k[2]), s.rows, 0});
-        update.scale = (float)(scale / (poly_up * up));
-        if (i + 1 < steps) product(Int<0>(), Int<1>(), poly, x, at.rows, at.cols, at.rows, GramOut{next, (float)(next_up / (poly_up * up)), 0});
+        product(Int<0>(), Int<0>(), x, x, at.rows, at.rows, at.cols, GramOut{gram, by.gram[i], 0});
+        product(Int<0>(), Int<0>(), gram, gram, at.rows, at.rows, at.rows, PolyOut{gram, poly, by.a[i], by.b[i], by.c[i], s.rows, 0});
+        if (i + 1 < steps) product(Int<0>(), Int<1>(), poly, x, at.rows, at.cols, at.rows, GramOut{next, by.next[i], 0});
         else if (tall) product(Int<1>(), Int<0>(), x, poly, s.cols, s.rows, at.rows, update);
         else product(Int<0>(), Int<1>(), poly, x, s.rows, s.cols, at.rows, update);
-        up = next_up;
         const HalvesAt t = x;
         x = next;
         next = t;
