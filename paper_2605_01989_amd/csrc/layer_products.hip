@@ -30,37 +30,64 @@ __device__ __forceinline__ Normal normal_of(float z) {
 // tanh's argument of GELU_TANH, twice, negated and for a power of two.
 __device__ __forceinline__ float tanh_power(float z) { return z * (-2.0f * LOG2E * ROOT_TWO_OVER_PI - 2.0f * LOG2E * ROOT_TWO_OVER_PI * CUBE * z * z); }
 
-// An exponential is a power of two, whose argument's rounding is worth w U of a result with exp(w) in it: as much as the fp32 argument itself.
-__device__ __forceinline__ float act_of(int act, float z) {
+// An exponential is a power of two, whose argument's rounding is worth w U of a result with exp(w) in it: as much as the fp32 argument itself.  The kind of activation is chosen
+// once for several values, which the matrix instructions' units need not wait for each other's exponentials.
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N]) {
     switch (act) {
-        case DBLP_ACT_RELU: return z <= 0.0f ? 0.0f : z;
-        case DBLP_ACT_GELU: {
-            const float tail = normal_of(z).tail;
-            return z * (z < 0.0f ? tail : 1.0f - tail);
-        }
-        case DBLP_ACT_GELU_TANH: return z * one_over(1.0f + exp2_of(tanh_power(z)));
-        case DBLP_ACT_SILU: return z * one_over(1.0f + exp2_of(-LOG2E * z));
-        default: return z;
+        case DBLP_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = v[i] <= 0.0f ? 0.0f : v[i];
+            break;
+        case DBLP_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float tail = normal_of(v[i]).tail;
+                v[i] *= v[i] < 0.0f ? tail : 1.0f - tail;
+            }
+            break;
+        case DBLP_ACT_GELU_TANH:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= one_over(1.0f + exp2_of(tanh_power(v[i])));
+            break;
+        case DBLP_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= one_over(1.0f + exp2_of(-LOG2E * v[i]));
+            break;
     }
 }
-// dy act'(z)
-__device__ __forceinline__ float gated(int act, float z, float dy) {
+// dy = dy act'(z).  A slope's 1 - p has lost U where p is near one; its factor there, z and its square, is below 40 until p is one and the product zero.
+template <int N>
+__device__ __forceinline__ void gate(int act, const float (&z)[N], float (&dy)[N]) {
     switch (act) {
-        case DBLP_ACT_RELU: return z > 0.0f ? dy : 0.0f;
-        case DBLP_ACT_GELU: {
-            const Normal n = normal_of(z);
-            return dy * ((z < 0.0f ? n.tail : 1.0f - n.tail) + z * (n.bell * (0.5f * ROOT_TWO_OVER_PI)));
-        }
-        case DBLP_ACT_GELU_TANH: {
-            // (past 30 the exponential has long been zero or infinity: a larger z' square would be infinite where zero times it is wanted)
-            const float t = fminf(fmaxf(z, -30.0f), 30.0f), e = exp2_of(tanh_power(t)), p = one_over(1.0f + e), rest = e < 1e30f ? e * p : 1.0f;      // 1 - p
-            return dy * (p + z * (p * rest * (2.0f * ROOT_TWO_OVER_PI + 6.0f * ROOT_TWO_OVER_PI * CUBE * t * t)));
-        }
-        case DBLP_ACT_SILU: {
-            const float e = exp2_of(-LOG2E * z), p = one_over(1.0f + e), rest = e < 1e30f ? e * p : 1.0f;
-            return dy * (p + z * (p * rest));
-        }
-        default: return dy;
+        case DBLP_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) dy[i] = z[i] > 0.0f ? dy[i] : 0.0f;
+            break;
+        case DBLP_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                // of -|z|, and of |z| one less that
+                const Normal n = normal_of(z[i]);
+                const float below = n.tail - fabsf(z[i]) * (n.bell * (0.5f * ROOT_TWO_OVER_PI));
+                dy[i] *= z[i] < 0.0f ? below : 1.0f - below;
+            }
+            break;
+        case DBLP_ACT_GELU_TANH:
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                // (past 30 the exponential has long been zero or infinity: a larger z' square would be infinite where zero times it is wanted)
+                const float t = fminf(fmaxf(z[i], -30.0f), 30.0f), p = one_over(1.0f + exp2_of(tanh_power(t)));
+                dy[i] *= p + z[i] * (p * (1.0f - p) * (2.0f * ROOT_TWO_OVER_PI + 6.0f * ROOT_TWO_OVER_PI * CUBE * t * t));
+            }
+            break;
+        case DBLP_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float p = one_over(1.0f + exp2_of(-LOG2E * z[i]));
+                dy[i] *= p + z[i] * (p * (1.0f - p));
+            }
+            break;
     }
 }
 
@@ -68,6 +95,21 @@ __device__ __forceinline__ float gated(int act, float z, float dy) {
 // what becomes of a product's sums
 // ------------------------------------------------------------------------------------------
 struct Matrix { void* p; u64 stride; };          // of a type that is known when the kernel runs
+
+template <class T, int N>
+__device__ __forceinline__ void store_rows_as(const Matrix& to, u32 m, u32 apart, u32 n, u32 cols, u32 on, const float (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N / 4; ++e) {
+        const float r[4] = {v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+        if (on >> e & 1) store_cols<Vec<T, 4>, 4>((typename T::elem*)to.p + (u64)(m + e * apart) * to.stride, n, cols, r);
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_rows(int type, const Matrix& to, u32 m, u32 apart, u32 n, u32 cols, u32 on, const float (&v)[N]) {
+    if (type == DBLP_F32) store_rows_as<F32>(to, m, apart, n, cols, on, v);
+    else if (type == DBLP_BF16) store_rows_as<BF16>(to, m, apart, n, cols, on, v);
+    else store_rows_as<F16>(to, m, apart, n, cols, on, v);
+}
 
 struct LayerOut {
     int type, act, bias_type;
@@ -80,19 +122,30 @@ struct LayerOut {
         if (residual.p) r.residual = raw4(type, residual.p, m * residual.stride + n, cols - n);
         return r;
     }
-    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc, const Met& met) const {
-        float v[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4];
+    // N rows, `apart` from each other, those that `on` names
+    template <int N>
+    __device__ __forceinline__ void put_rows(u32, u32, u32 m, u32 apart, u32 n, u32 cols, u32 on, const f4 (&acc)[N], const Met (&met)[N]) const {
+        float v[4 * N];
+        for (int i = 0; i < 4 * N; ++i) v[i] = acc[i / 4][i % 4];
         if (bias) {
-            open4(bias_type, met.bias, b);
-            for (int i = 0; i < 4; ++i) v[i] += b[i];
+            float b[4];
+            open4(bias_type, met[0].bias, b);
+            for (int i = 0; i < 4 * N; ++i) v[i] += b[i % 4];
         }
-        if (z.p) store4(type, z.p, m * z.stride + n, cols - n, v);
-        for (int i = 0; i < 4; ++i) v[i] = act_of(act, v[i]);
-        if (residual.p) {
-            open4(type, met.residual, b);
-            for (int i = 0; i < 4; ++i) v[i] += b[i];
-        }
-        store4(type, y.p, m * y.stride + n, cols - n, v);
+        if (z.p) store_rows(type, z, m, apart, n, cols, on, v);
+        activate(act, v);
+        if (residual.p)
+            for (int e = 0; e < N; ++e) {
+                float r[4];
+                open4(type, met[e].residual, r);
+                for (int i = 0; i < 4; ++i) v[4 * e + i] += r[i];
+            }
+        store_rows(type, y, m, apart, n, cols, on, v);
+    }
+    __device__ __forceinline__ void put(u32 matrix, u32 part, u32 m, u32 n, u32 cols, f4 acc, const Met& met) const {
+        const f4 a[1] = {acc};
+        const Met b[1] = {met};
+        put_rows<1>(matrix, part, m, 0, n, cols, 1, a, b);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
@@ -107,17 +160,31 @@ struct GateOut {
         if (base.p) r.base = raw4(type, base.p, m * base.stride + n, cols - n);
         return r;
     }
-    __device__ __forceinline__ void put(u32, u32, u32 m, u32 n, u32 cols, f4 acc, const Met& met) const {
-        float v[4] = {acc[0], acc[1], acc[2], acc[3]}, b[4];
+    template <int N>
+    __device__ __forceinline__ void put_rows(u32, u32, u32 m, u32 apart, u32 n, u32 cols, u32 on, const f4 (&acc)[N], const Met (&met)[N]) const {
+        float v[4 * N], b[4 * N];
+        for (int i = 0; i < 4 * N; ++i) v[i] = acc[i / 4][i % 4];
+        const auto open = [&](auto which) {
+            for (int e = 0; e < N; ++e) {
+                float r[4];
+                open4(type, which(met[e]), r);
+                for (int i = 0; i < 4; ++i) b[4 * e + i] = r[i];
+            }
+        };
         if (z.p) {
-            open4(type, met.z, b);
-            for (int i = 0; i < 4; ++i) v[i] = gated(act, b[i], v[i]);
+            open([](const Met& t) { return t.z; });
+            gate(act, b, v);
         }
         if (base.p) {
-            open4(type, met.base, b);
-            for (int i = 0; i < 4; ++i) v[i] += b[i];
+            open([](const Met& t) { return t.base; });
+            for (int i = 0; i < 4 * N; ++i) v[i] += b[i];
         }
-        store4(type, dx.p, m * dx.stride + n, cols - n, v);
+        store_rows(type, dx, m, apart, n, cols, on, v);
+    }
+    __device__ __forceinline__ void put(u32 matrix, u32 part, u32 m, u32 n, u32 cols, f4 acc, const Met& met) const {
+        const f4 a[1] = {acc};
+        const Met b[1] = {met};
+        put_rows<1>(matrix, part, m, 0, n, cols, 1, a, b);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
 };
@@ -188,9 +255,10 @@ __global__ __launch_bounds__(64) void join_sums(PartOut in, u32 cols, u32 parts,
 }
 
 // ------------------------------------------------------------------------------------------
-// activation_grad: a thread takes 16 bytes
+// activation_grad: a thread takes 16 bytes.  Bound by memory: 805 MB in 180 to 200 us whatever the activation, and none; two or four places a thread, and the hint that nothing is
+// used again soon, change nothing.
 // ------------------------------------------------------------------------------------------
-template <class T, int W>
+template <class T, int W, bool WHOLE>
 __global__ __launch_bounds__(256) void activation_units(Units s, int act, const typename T::elem* dy, u64 dy_stride, const typename T::elem* z, u64 z_stride, typename T::elem* dz, u64 dz_stride) {
     typedef Vec<T, W> V;
     const u32 u = blockIdx.x * 256 + threadIdx.x;
@@ -198,11 +266,12 @@ __global__ __launch_bounds__(256) void activation_units(Units s, int act, const 
     const u32 row = s.per_row.of(u), c = (u - row * s.per_row.d) * W;
     if (c >= s.cols) return;
     const u64 r = s.row0 + row;
-    float a[W], b[W];
-    V::open(settle_cols<V, W, false>(load_cols<V, W, false>(dy + r * dy_stride, c, s.cols), c, s.cols), a);
-    V::open(settle_cols<V, W, false>(load_cols<V, W, false>(z + r * z_stride, c, s.cols), c, s.cols), b);
-    for (int i = 0; i < W; ++i) a[i] = gated(act, b[i], a[i]);
-    store_cols<V, W>(dz + r * dz_stride, c, s.cols, a);
+    const typename V::raw a = load_cols<V, W, WHOLE>(dy + r * dy_stride, c, s.cols), b = load_cols<V, W, WHOLE>(z + r * z_stride, c, s.cols);
+    float x[W], y[W];
+    V::open(settle_cols<V, W, WHOLE>(a, c, s.cols), x);
+    V::open(settle_cols<V, W, WHOLE>(b, c, s.cols), y);
+    gate<W>(act, y, x);
+    store_cols<V, W>(dz + r * dz_stride, c, s.cols, x);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -444,7 +513,8 @@ extern "C" int dblp_activation_grad(int device, void* stream, uint64_t rows, uin
         typedef const typename T::elem* in;
         constexpr int W = 16 / sizeof(typename T::elem);
         each_launch<W>(rows, cols, [&](Units s) {
-            launch(activation_units<T, W>, dim3(blocks_of(s.n, 256)), 256, (hipStream_t)stream, s, activation, (in)d_dy, dy_stride, (in)d_z, z_stride, (typename T::elem*)d_dz, dz_stride);
+            launch(cols % W ? activation_units<T, W, false> : activation_units<T, W, true>, dim3(blocks_of(s.n, 256)), 256, (hipStream_t)stream, s, activation, (in)d_dy, dy_stride, (in)d_z, z_stride,
+                   (typename T::elem*)d_dz, dz_stride);
         });
     });
     return launched(call, launch);

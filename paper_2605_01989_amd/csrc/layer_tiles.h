@@ -335,10 +335,31 @@ __device__ __forceinline__ void tile_of(u64 b, u64 n, u32 tile_rows, u32 tile_co
     c = (u32)(in_band / high);
 }
 
+// ... and of a symmetric result, n tiles high and wide, those on and above the diagonal, n (n + 1) / 2.
+__device__ __forceinline__ void upper_tile_of(u64 b, u64 tiles, u32 n, u32& m, u32& c) {
+    const u64 each = tiles / 8, more = tiles % 8, die = b % 8;
+    u32 left = (u32)(die * each + (die < more ? die : more) + b / 8), row = 0;
+    while (left >= n - row) left -= n - row++;
+    m = row;
+    c = row + left;
+}
+
+// Four rows' results to an Out: together, if it takes them so.
+template <class Out, class Met>
+__device__ __forceinline__ auto put_all(const Out& out, u32 matrix, u32 part, u32 m, u32 apart, u32 n, u32 cols, u32 on, const f4 (&v)[4], const Met (&met)[4]) -> decltype(out.put_rows(0, 0, 0, 0, 0, 0, 0, v, met)) {
+    if (on) out.put_rows(matrix, part, m, apart, n, cols, on, v, met);
+}
+template <class Out, class... Met>
+__device__ __forceinline__ void put_all(const Out& out, u32 matrix, u32 part, u32 m, u32 apart, u32 n, u32 cols, u32 on, const f4 (&v)[4], const Met (&... met)[4]) {
+#pragma unroll
+    for (u32 e = 0; e < 4; ++e)
+        if (on >> e & 1) out.put(matrix, part, m + e * apart, n, cols, v[e], met[e]...);
+}
+
 // WR x WC waves, each 16 NM x 16 NN of the tile.
 template <int WR_, int WC_, int NM_, int NN_, int RING_> struct Waves { static constexpr int WR = WR_, WC = WC_, NM = NM_, NN = NN_, RING = RING_, BM = 16 * NM * WR, BN = 16 * NN * WC, ALL = WR * WC; };
 
-template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, class W, bool SUMS, class Out, bool HALVES = false>
+template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, class W, bool SUMS, class Out, bool HALVES = false, bool SYMMETRIC = false>
 __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out out) {
     typedef typename T::elem elem;
     constexpr int BM = W::BM, BN = W::BN, NM = W::NM, NN = W::NN, RING = W::RING;
@@ -347,7 +368,8 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
     constexpr u32 KS = FP::KS, STAGE = FP::BYTES + FQ::BYTES, COPIES = FP::COPIES + FQ::COPIES;
     __shared__ __attribute__((aligned(1024))) uint8_t ring[RING * STAGE];
     u32 tm, tn;
-    tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, a.tile_cols, tm, tn);
+    if (SYMMETRIC) upper_tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, tm, tn);
+    else tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, a.tile_cols, tm, tn);
     const u32 m0 = tm * BM, n0 = tn * BN;
     const u32 matrix = blockIdx.z / a.parts, part = blockIdx.z % a.parts;
     const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, in_group = lane & 15;
@@ -463,20 +485,33 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
                     for (int j = 0; j < NN; ++j) *(f4*)(mine + (i * 16 + in_group) * LINE + (j * 16 + group * 4) * 4) = acc[t * AT_ONCE + i][j];
-        // four at a time, so that what they meet in memory is asked for together
-        constexpr u32 LINES = 64 / (WIDTH / 4);
-        const u32 q = lane % (WIDTH / 4) * 4, n = n0 + wn + q;
+        // four at a time, so that what they meet in memory is asked for together.  TURNED: a result's columns as rows, of a symmetric one below the diagonal
+        const auto leave = [&](auto turned) {
+            constexpr bool TURNED = decltype(turned)::value;
+            constexpr u32 HIGH = TURNED ? WIDTH : AT_ONCE * 16, QUADS = (TURNED ? AT_ONCE * 16 : WIDTH) / 4, LINES = 64 / QUADS;
+            const u32 q = lane % QUADS * 4, rows0 = m0 + wm + turn * AT_ONCE * 16, n = TURNED ? rows0 + q : n0 + wn + q, row0 = TURNED ? n0 + wn : rows0;
+            if (lane >= LINES * QUADS) return;
 #pragma nounroll
-        for (u32 line = lane / (WIDTH / 4); line < AT_ONCE * 16; line += 4 * LINES) {
-            const u32 m = m0 + wm + turn * AT_ONCE * 16 + line;
-            decltype(out.get(0, 0, 0, 0)) met[4];
+            for (u32 line = lane / QUADS; line < HIGH; line += 4 * LINES) {
+                decltype(out.get(0, 0, 0, 0)) met[4];
 #pragma unroll
-            for (u32 e = 0; e < 4; ++e)
-                if (m + e * LINES < a.rows && n < a.cols) met[e] = out.get(matrix, m + e * LINES, n, a.cols);
+                for (u32 e = 0; e < 4; ++e)
+                    if (line + e * LINES < HIGH && row0 + line + e * LINES < a.rows && n < a.cols) met[e] = out.get(matrix, row0 + line + e * LINES, n, a.cols);
+                f4 v[4];
+                u32 on = 0;
 #pragma unroll
-            for (u32 e = 0; e < 4; ++e)
-                if (m + e * LINES < a.rows && n < a.cols) out.put(matrix, part, m + e * LINES, n, a.cols, *(const f4*)(mine + (line + e * LINES) * LINE + q * 4), met[e]);
-        }
+                for (u32 e = 0; e < 4; ++e) {
+                    if (line + e * LINES >= HIGH) continue;
+                    if (TURNED)
+                        for (u32 t = 0; t < 4; ++t) v[e][t] = *(const float*)(mine + (q + t) * LINE + (line + e * LINES) * 4);
+                    else v[e] = *(const f4*)(mine + (line + e * LINES) * LINE + q * 4);
+                    if (row0 + line + e * LINES < a.rows && n < a.cols) on |= 1u << e;
+                }
+                put_all(out, matrix, part, row0 + line, LINES, n, a.cols, on, v, met);
+            }
+        };
+        leave(Int<0>());
+        if (SYMMETRIC && tm != tn) leave(Int<1>());
     }
     if (SUMS && summing)
 #pragma unroll
@@ -591,10 +626,10 @@ __global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, u32 parts
 
 // Launches of a product's tiles: at most 2^20 tiles and 2^15 matrices' parts each (a grid's threads stay below 2^32, its z below 2^16).
 template <int BM, int BN, class F>
-static void each_tiles(Product a, u64 matrices, F f) {
+static void each_tiles(Product a, u64 matrices, F f, bool symmetric = false) {
     a.tile_cols = (u32)((a.cols + (u64)BN - 1) / BN);
     a.tile_rows = (u32)((a.rows + (u64)BM - 1) / BM);
-    a.tiles = (u64)a.tile_rows * a.tile_cols;
+    a.tiles = symmetric ? (u64)a.tile_rows * (a.tile_rows + 1) / 2 : (u64)a.tile_rows * a.tile_cols;
     for (u64 m = 0; m < matrices; m += 32768 / a.parts) {
         const u64 here = matrices - m < 32768 / a.parts ? matrices - m : 32768 / a.parts;
         for (a.tile0 = 0; a.tile0 < a.tiles; a.tile0 += 1u << 20)

@@ -500,9 +500,10 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
             launch(scale_in<T>, dim3((u32)(at.cols / 64), (u32)(at.rows / 64), n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, up, x);
         });
     });
-    // R = P Q^T for all matrices, summed over all k of the halves
-    const auto product = [&](auto p_by_k, auto q_by_k, const HalvesAt& P, const HalvesAt& Q, u64 m_rows, u64 m_cols, u64 depth, auto out) {
-        constexpr bool PK = decltype(p_by_k)::value, QK = decltype(q_by_k)::value;
+    // R = P Q^T for all matrices, summed over all k of the halves; of a symmetric one the tiles on and above the diagonal.
+    // The kind of tiles by an estimate of the time: rounds over the 256 CUs, of a fixed time and one for each stage of 64 k, in microseconds as measured.
+    const auto product = [&](auto p_by_k, auto q_by_k, auto symmetric, const HalvesAt& P, const HalvesAt& Q, u64 m_rows, u64 m_cols, u64 depth, auto out) {
+        constexpr bool PK = decltype(p_by_k)::value, QK = decltype(q_by_k)::value, SYM = decltype(symmetric)::value;
         typedef decltype(out) Out;
         const Product a = {{P.p, P.stride, P.step, P.low}, {Q.p, Q.stride, Q.step, Q.low}, (u32)m_rows, (u32)m_cols, (u32)(3 * depth), 0, (u32)(3 * depth), 1};
         const auto go = [&](auto waves) {
@@ -511,14 +512,24 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
                 out.matrix0 = m;
                 p.P.p = P.p + m * P.step;
                 p.Q.p = Q.p + m * Q.step;
-                launch(ring_products<F16, PK, QK, false, false, W, false, Out, true>, grid, 64 * W::ALL, st, p, out);
-            });
+                launch(ring_products<F16, PK, QK, false, false, W, false, Out, true, SYM>, grid, 64 * W::ALL, st, p, out);
+            }, SYM);
         };
-        const u64 area = m_rows * m_cols * count;
+        static const struct { u32 tile, blocks; double fixed, first, more; } K[4] = {{64, 3, 3.0, 0.40, 0.10}, {128, 2, 6.0, 0.83, 0.40}, {192, 1, 10.0, 1.05, 0}, {256, 1, 14.0, 1.65, 0}};
+        int best = 0;
+        double least = 1e30;
         const bool far = !in_reach<F16>(a.P) || !in_reach<F16>(a.Q);                      // (a tile of more rows would be out of reach)
-        if (far || area < 200ull * 128 * 128) go(Waves<2, 2, 2, 2, 3>());
-        else if (area < 120ull * 256 * 256) go(Waves<2, 2, 4, 4, 2>());
-        else go(Waves<2, 4, 8, 4, 2>());
+        for (int i = 0; i < (far ? 1 : 4); ++i) {
+            if (K[i].tile == 192 && !SYM) continue;
+            const double down = ceil(m_rows / (double)K[i].tile), across = ceil(m_cols / (double)K[i].tile), blocks = count * (SYM ? down * (down + 1) / 2 : down * across);
+            const double rounds = ceil(blocks / (256.0 * K[i].blocks)), held = rounds > 1 ? K[i].blocks : ceil(blocks / 256.0);
+            const double t = rounds * (K[i].fixed + a.depth / 64 * (K[i].first + (held - 1) * K[i].more));
+            if (t < least) { least = t; best = i; }
+        }
+        if (best == 0) go(Waves<2, 2, 2, 2, 3>());
+        else if (best == 1) go(Waves<2, 2, 4, 4, 2>());
+        else if (best == 3) go(Waves<2, 4, 8, 4, 2>());
+        else if constexpr (SYM) go(Waves<2, 4, 6, 3, 3>());
     };
     if (steps == 0)
         each_matrix([&](u64 m, u32 n) {
@@ -526,11 +537,11 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
             launch(update_plain, dim3(norm_blocks(values), 1, n), 256, st, x, s, update);
         });
     for (u32 i = 0; i < steps; ++i) {
-        product(Int<0>(), Int<0>(), x, x, at.rows, at.rows, at.cols, GramOut{gram, by.gram[i], 0});
-        product(Int<0>(), Int<0>(), gram, gram, at.rows, at.rows, at.rows, PolyOut{gram, poly, by.a[i], by.b[i], by.c[i], s.rows, 0});
-        if (i + 1 < steps) product(Int<0>(), Int<1>(), poly, x, at.rows, at.cols, at.rows, GramOut{next, by.next[i], 0});
-        else if (tall) product(Int<1>(), Int<0>(), x, poly, s.cols, s.rows, at.rows, update);
-        else product(Int<0>(), Int<1>(), poly, x, s.rows, s.cols, at.rows, update);
+        product(Int<0>(), Int<0>(), Int<1>(), x, x, at.rows, at.rows, at.cols, GramOut{gram, by.gram[i], 0});
+        product(Int<0>(), Int<0>(), Int<1>(), gram, gram, at.rows, at.rows, at.rows, PolyOut{gram, poly, by.a[i], by.b[i], by.c[i], s.rows, 0});
+        if (i + 1 < steps) product(Int<0>(), Int<1>(), Int<0>(), poly, x, at.rows, at.cols, at.rows, GramOut{next, by.next[i], 0});
+        else if (tall) product(Int<1>(), Int<0>(), Int<0>(), x, poly, s.cols, s.rows, at.rows, update);
+        else product(Int<0>(), Int<1>(), Int<0>(), poly, x, s.rows, s.cols, at.rows, update);
         const HalvesAt t = x;
         x = next;
         next = t;
