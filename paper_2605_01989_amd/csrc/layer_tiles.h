@@ -44,7 +44,7 @@ struct Operand { const void* p; u64 stride, step, low; };
 struct Product {
     Operand P, Q;
     u32 rows, cols, depth, tile_cols, part, parts;   // part: k of one part, a multiple of 128 bytes' (a stage's); tile_cols: tiles of a row of tiles
-    u32 tile_rows;
+    u32 tile_rows, odd_rows;                         // odd_rows: see PAIRS
     u64 tiles, tile0;                                // of the whole result; first one of this launch
 };
 
@@ -264,14 +264,15 @@ struct Feed {
         left -= by * sizeof(elem);
         k += KS;
     }
-    // The stage's copy number i of this wave, to LDS at `to`; k past the end as zeros.
-    __device__ __forceinline__ void copy(u32 i, u32 to) const {
+    // The stage's copy number i of this wave, to LDS at `to`; k past the end, and before `begin`, as zeros.
+    __device__ __forceinline__ void copy(u32 i, u32 to, u32 begin = 0) const {
         const u64 at = (u64)base;
         const u32 bytes = left < PAST_ALL - 4 ? ((u32)left + 3) & ~3u : PAST_ALL;        // (a chunk that goes past the operand's end brings zeros from there)
         const u32 rest = k < depth ? depth - k : 0;
         // (the same in all lanes: the compiler does not see it through the turns of halves)
         const rsrc_t from = {uniform((u32)at), uniform((u32)(at >> 32)), uniform(bytes), 0x00020000u};
-        copy_to_lds(from, kk + i * KD < rest ? offset[i] : PAST_ALL, to + (wave * N + i) * 1024);
+        const u32 k_here = kk + i * KD;
+        copy_to_lds(from, k_here < rest && (begin == 0 || k + k_here >= begin) ? offset[i] : PAST_ALL, to + (wave * N + i) * 1024);
     }
     // Through registers: asked for, and put down later.
     __device__ __forceinline__ void ask(u32 i) {
@@ -356,10 +357,13 @@ __device__ __forceinline__ void put_all(const Out& out, u32 matrix, u32 part, u3
         if (on >> e & 1) out.put(matrix, part, m + e * apart, n, cols, v[e], met[e]...);
 }
 
+// PAIRS: P has rows of 16-bit values an odd number of elements apart, so that no more than every other one begins at a multiple of four bytes, and Q lies by k.  The
+// others do so one element earlier.  Even and odd rows are two matrices (blockIdx.z), each with rows at multiples of four bytes that can be copied; of the shifted one k is one more
+// than the sum's, its first value, an element of another row, is set to zero, and Q's rows are taken one earlier.
 // WR x WC waves, each 16 NM x 16 NN of the tile.
 template <int WR_, int WC_, int NM_, int NN_, int RING_> struct Waves { static constexpr int WR = WR_, WC = WC_, NM = NM_, NN = NN_, RING = RING_, BM = 16 * NM * WR, BN = 16 * NN * WC, ALL = WR * WC; };
 
-template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, class W, bool SUMS, class Out, bool HALVES = false, bool SYMMETRIC = false>
+template <class T, bool P_BY_K, bool Q_BY_K, bool P_STAGED, bool Q_STAGED, class W, bool SUMS, class Out, bool HALVES = false, bool SYMMETRIC = false, bool PAIRS = false>
 __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out out) {
     typedef typename T::elem elem;
     constexpr int BM = W::BM, BN = W::BN, NM = W::NM, NN = W::NN, RING = W::RING;
@@ -372,14 +376,18 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
     else tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, a.tile_cols, tm, tn);
     const u32 m0 = tm * BM, n0 = tn * BN;
     const u32 matrix = blockIdx.z / a.parts, part = blockIdx.z % a.parts;
+    const u64 parity = PAIRS ? uniform(matrix) : 0;
+    const u32 shift = PAIRS ? ((u32)((uintptr_t)a.P.p >> 1) + (u32)(parity * a.P.stride)) & 1 : 0;
+    const u32 rows = PAIRS && parity ? a.odd_rows : a.rows, depth = a.depth + shift;
+    if (PAIRS && m0 >= rows) return;
     const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, in_group = lane & 15;
     const u32 wm = wave / W::WC * (16 * NM), wn = wave % W::WC * (16 * NN);
-    const u32 k_first = part * a.part, k_end = a.depth - k_first > a.part ? k_first + a.part : a.depth;
+    const u32 k_first = part * a.part, k_end = depth - k_first > a.part ? k_first + a.part : depth;
     const u32 stages = (k_end - k_first + KS - 1) / KS;
     const bool summing = SUMS && __builtin_amdgcn_readfirstlane(n0 == 0 && wn == 0);
     f4 acc[NM][NN] = {}, sum = {};
-    FP fp((const elem*)a.P.p + matrix * a.P.step, a.P.stride, m0, a.rows, k_first, k_end);
-    FQ fq((const elem*)a.Q.p + matrix * a.Q.step, a.Q.stride, n0, a.cols, k_first, k_end);
+    FP fp((const elem*)a.P.p + (PAIRS ? parity * a.P.stride - shift : matrix * a.P.step), PAIRS ? 2 * a.P.stride : a.P.stride, m0, rows, k_first, k_end);
+    FQ fq((const elem*)a.Q.p + (PAIRS ? 0 - shift * a.Q.stride : matrix * a.Q.step), a.Q.stride, n0, a.cols, k_first, k_end);
     if (HALVES) {
         fp.of_halves((const elem*)a.P.p + matrix * a.P.step, a.P.low, m0, k_first, a.depth);
         fq.of_halves((const elem*)a.Q.p + matrix * a.Q.step, a.Q.low, n0, k_first, a.depth);
@@ -389,7 +397,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
     const u32 ring_at = __builtin_amdgcn_readfirstlane(lds_address(ring));
     const auto copy = [&](u32 e, u32 slot) {
         if (e < FP::COPIES) fp.copy(e, ring_at + slot * STAGE);
-        else fq.copy(e - FP::COPIES, ring_at + slot * STAGE + FP::BYTES);
+        else fq.copy(e - FP::COPIES, ring_at + slot * STAGE + FP::BYTES, PAIRS ? shift : 0);
     };
     const auto ask = [&] {
         if (P_STAGED)
@@ -430,6 +438,10 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
         }
         ask();
         if (stages == 1) trim(0);
+        if (PAIRS && shift && k_first == 0) {
+            arrived_and_barrier<0>();
+            for (u32 row = threadIdx.x; row < BM; row += 64 * W::ALL) *(elem*)(ring + row * STAGE_BYTES + ((row & 7) << 4)) = (elem)0.0f;
+        }
         arrived_and_barrier<(RING - 1) * COPIES>();
 #pragma unroll
         for (int i = 0; i < NM; ++i) b[0][i] = rp.get(ring, 0, 0, i);
@@ -485,6 +497,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
                     for (int j = 0; j < NN; ++j) *(f4*)(mine + (i * 16 + in_group) * LINE + (j * 16 + group * 4) * 4) = acc[t * AT_ONCE + i][j];
+        const auto to_row = [&](u32 m) { return PAIRS ? 2 * m + (u32)parity : m; };
         // four at a time, so that what they meet in memory is asked for together.  TURNED: a result's columns as rows, of a symmetric one below the diagonal
         const auto leave = [&](auto turned) {
             constexpr bool TURNED = decltype(turned)::value;
@@ -496,7 +509,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 decltype(out.get(0, 0, 0, 0)) met[4];
 #pragma unroll
                 for (u32 e = 0; e < 4; ++e)
-                    if (line + e * LINES < HIGH && row0 + line + e * LINES < a.rows && n < a.cols) met[e] = out.get(matrix, row0 + line + e * LINES, n, a.cols);
+                    if (line + e * LINES < HIGH && row0 + line + e * LINES < rows && n < a.cols) met[e] = out.get(PAIRS ? 0 : matrix, to_row(row0 + line + e * LINES), n, a.cols);
                 f4 v[4];
                 u32 on = 0;
 #pragma unroll
@@ -505,9 +518,9 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                     if (TURNED)
                         for (u32 t = 0; t < 4; ++t) v[e][t] = *(const float*)(mine + (q + t) * LINE + (line + e * LINES) * 4);
                     else v[e] = *(const f4*)(mine + (line + e * LINES) * LINE + q * 4);
-                    if (row0 + line + e * LINES < a.rows && n < a.cols) on |= 1u << e;
+                    if (row0 + line + e * LINES < rows && n < a.cols) on |= 1u << e;
                 }
-                put_all(out, matrix, part, row0 + line, LINES, n, a.cols, on, v, met);
+                put_all(out, PAIRS ? 0 : matrix, part, to_row(row0 + line), PAIRS ? 2 * LINES : LINES, n, a.cols, on, v, met);
             }
         };
         leave(Int<0>());
@@ -642,4 +655,4 @@ template <class T> static bool copied(const Operand& o) {
     const u64 e = sizeof(typename T::elem);
     return !off(o.p, 4) && o.stride * e % 4 == 0 && o.step * e % 4 == 0;
 }
-template <class T> static bool in_reach(const Operand& o) { return o.stride < (1ull << 31) / 256 / sizeof(typename T::elem); }
+template <class T> static bool in_reach(const Operand& o) { return o.stride < (1ull << 31) / 512 / sizeof(typename T::elem); }        // (of 256 rows twice as far apart)
