@@ -298,21 +298,25 @@ extern "C" uint64_t dblp_linear_workspace(uint64_t n_tokens, uint32_t in, uint32
 enum Kind { TILES_64, TILES_128, TILES_256, KINDS };
 struct Way { Kind kind; u32 parts, part; };
 
-// Chosen by an estimate of the time: rounds of tiles over the 256 CUs, each a fixed time and one for each stage of 128 bytes of k.  Microseconds, as measured: a CU holds three, two or
-// one block of a kind, and a stage takes longer with more of them.
+// Chosen by an estimate of the time, in microseconds: rounds of tiles over the 256 CUs, each a fixed time and one for each stage of 128 bytes of k, which is longer with more blocks on a CU
+// (of the largest tiles, with more CUs at work); parts are written, read and added up at 5 TB/s.  As measured with each kind alone over 27 sizes; the choice is within 15 % of the best
+// kind and number of parts on them (8192 x 1024 x 4096 in tiles of 64, 128, 256: 118, 79, 68 us; 8192 x 768 x 2304: 18, 18, 26; its weight's gradient in 1, 4, 8 parts: 85, 44, 46).
 static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
-    static const struct { u32 tile, blocks; double fixed, stage[2]; } K[KINDS] = {{64, 3, 3.0, {0.45, 1.3}}, {128, 2, 6.0, {1.23, 3.4}}, {256, 1, 14.0, {1.65, 1e9}}};
+    static const struct { u32 tile, blocks; double fixed, stage[2][3]; } K[KINDS] = {
+        {64, 3, 3.5, {{0.28, 0.40, 0.50}, {0.65, 0.90, 1.10}}}, {128, 2, 5.0, {{0.64, 0.98, 0}, {2.2, 3.6, 0}}}, {256, 1, 10.0, {{1.15, 0, 0}, {0, 0, 0}}}};
     Way best = {TILES_64, 1, 0};
     double least = 1e30;
     const u64 ks = 128 / elem, stages = (depth + ks - 1) / ks, bytes = rows * round_up(cols, 4) * 4;
     for (int i = 0; i < KINDS; ++i) {
         if (i == TILES_256 && elem == 4) continue;
         const u64 tiles = ((rows + K[i].tile - 1) / K[i].tile) * ((cols + K[i].tile - 1) / K[i].tile);
-        for (u64 p = 1; p <= PARTS_MOST && (p == 1 || (p * bytes <= PARTS_BYTES && stages / p >= 4)); ++p) {
+        for (u64 p = 1; p <= PARTS_MOST && (p == 1 || (p * bytes <= PARTS_BYTES && stages / p >= 2)); ++p) {
             const u64 each = (stages + p - 1) / p;
             if (p > 1 && (stages + each - 1) / each != p) continue;
-            const double blocks = (double)tiles * p, rounds = ceil(blocks / (256.0 * K[i].blocks)), held = blocks < 256.0 * K[i].blocks ? ceil(blocks / 256.0) : K[i].blocks;
-            const double t = rounds * (K[i].fixed + each * K[i].stage[elem == 4] * (0.5 + 0.5 * held / K[i].blocks)) + (p > 1 ? 4.0 + p * bytes * 2 / 4e6 : 0.0);
+            const double blocks = (double)tiles * p, rounds = ceil(blocks / (256.0 * K[i].blocks));
+            const int held = blocks > 256.0 * K[i].blocks ? (int)K[i].blocks : blocks > 256.0 ? (int)ceil(blocks / 256.0) : 1;
+            const double stage = K[i].stage[elem == 4][held - 1] + (i == TILES_256 ? 0.4 * fmin(1.0, blocks / 256.0) : 0.0);
+            const double t = rounds * (K[i].fixed + each * stage) + (p > 1 ? 3.0 + p * bytes * 2 / 5e6 : 0.0);
             if (t < least) {
                 least = t;
                 best = {(Kind)i, (u32)p, (u32)(each * ks)};

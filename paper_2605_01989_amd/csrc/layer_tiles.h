@@ -619,7 +619,7 @@ struct PartOut {
     __device__ __forceinline__ void sums(u32, u32 part, u32 m, float s) const { if (row_sums) row_sums[(u64)part * rows + m] = s; }
 };
 
-// Adds the parts up, one after the other, and hands the results on: a thread takes four columns.
+// Adds the parts up, one after the other, eight of them on their way, and hands the results on: a thread takes four columns.
 template <class Out>
 __global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, u32 parts, Out out) {
     const u32 u = blockIdx.x * 256 + threadIdx.x;
@@ -627,13 +627,26 @@ __global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, u32 parts
     const u32 row = s.per_row.of(u), c = (u - row * s.per_row.d) * 4, m = (u32)s.row0 + row;
     if (in.row_sums && c == 0) {
         float sum = 0.0f;
-        for (u32 i = 0; i < parts; ++i) sum += in.row_sums[(u64)i * in.rows + m];
+        for (u32 i = 0; i < parts; i += 8) {
+            float v[8];
+#pragma unroll
+            for (u32 j = 0; j < 8; ++j) v[j] = i + j < parts ? in.row_sums[(u64)(i + j) * in.rows + m] : 0.0f;
+#pragma unroll
+            for (u32 j = 0; j < 8; ++j) sum += v[j];
+        }
         out.sums(0, 0, m, sum);
     }
     if (c >= s.cols) return;
     const auto met = out.get(0, m, c, s.cols);
+    const float* const p = in.p + m * in.stride + c;
     f4 sum = {};
-    for (u32 i = 0; i < parts; ++i) sum += *(const f4*)(in.p + i * in.step + m * in.stride + c);
+    for (u32 i = 0; i < parts; i += 8) {
+        f4 v[8];
+#pragma unroll
+        for (u32 j = 0; j < 8; ++j) v[j] = i + j < parts ? *(const f4*)(p + (i + j) * in.step) : (f4)(0.0f);
+#pragma unroll
+        for (u32 j = 0; j < 8; ++j) sum += v[j];
+    }
     out.put(0, 0, m, c, s.cols, sum, met);
 }
 

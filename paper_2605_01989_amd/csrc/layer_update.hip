@@ -515,7 +515,7 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
                 launch(ring_products<F16, PK, QK, false, false, W, false, Out, true, SYM>, grid, 64 * W::ALL, st, p, out);
             }, SYM);
         };
-        static const struct { u32 tile, blocks; double fixed, first, more; } K[4] = {{64, 3, 3.0, 0.40, 0.10}, {128, 2, 6.0, 0.83, 0.40}, {192, 1, 10.0, 1.05, 0}, {256, 1, 14.0, 1.65, 0}};
+        static const struct { u32 tile, blocks; double fixed, first, more; } K[4] = {{64, 3, 4.0, 0.30, 0.11}, {128, 2, 8.0, 0.76, 0.35}, {192, 1, 14.0, 1.08, 0}, {256, 1, 14.0, 1.60, 0}};
         int best = 0;
         double least = 1e30;
         const bool far = !in_reach<F16>(a.P) || !in_reach<F16>(a.Q);                      // (a tile of more rows would be out of reach)
