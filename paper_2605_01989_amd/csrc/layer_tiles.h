@@ -36,8 +36,8 @@ template <> __device__ __forceinline__ u4v ones<F16>() { return (u4v)(0x3C003C00
 template <> __device__ __forceinline__ u4v ones<F32>() { return (u4v)(0x3F800000u); }
 
 // One operand of a batch of products: element (row, k) at row * stride + k, or at k * stride + row where it lies by k.  An operand in halves is two such matrices of
-// fp16, `low` elements apart, whose sum it is: 22 significant bits.  A product of two of those is three of the halves', high by high, high by low and low by
-// high, one behind the other in one sum over 3 k; what is left out is below the halves' own rounding.
+// fp16, `low` elements apart, whose sum it is: 22 significant bits.  A product of two of those is three of the halves', low by high, high by low and high by high, one behind the
+// other in one sum over 3 k (the small ones first: they are rounded as what they are); what is left out is below the halves' own rounding.
 struct Operand { const void* p; u64 stride, step, low; };
 
 // What a launch computes: rows x cols results of sums over `depth` k, of which block z takes part z % parts of matrix z / parts.
@@ -223,7 +223,7 @@ struct Feed {
         left = ~0ull >> 1;
         place();
     }
-    __device__ __forceinline__ void place() { base = whole + (product == (HALVES == 1 ? 2 : 1) ? low : 0) + (BY_K ? (u64)k_in * stride : k_in); }
+    __device__ __forceinline__ void place() { base = whole + (product == (HALVES == 1 ? 0 : 1) ? low : 0) + (BY_K ? (u64)k_in * stride : k_in); }
 
     static __device__ __forceinline__ u32 turn(u32 k) {
         const u32 t = sizeof(elem) == 2 ? (k & 3) | (k >> 3 & 1) << 2 : k >> 2 & 3;

@@ -204,7 +204,7 @@ __device__ __forceinline__ void small_put(uint8_t* m, u32 low, u32 row, u32 col,
     *(half4*)(m + low + small_at<WIDTH>(row, col)) = h.low;
 }
 
-// high by high, high by low, low by high: each a round over the results, whose sums wait for each other.  TURNED: a result's rows and columns change places.
+// low by high, high by low, high by high: each a round over the results, whose sums wait for each other.  TURNED: a result's rows and columns change places.
 template <int R, int C, bool TURNED = false>
 __device__ __forceinline__ void add_halves(f4 (&acc)[R][C], const u4v (&bh)[R], const u4v (&bl)[R], const u4v (&ch)[C], const u4v (&cl)[C]) {
     const auto round = [&](const u4v (&b)[R], const u4v (&c)[C]) {
@@ -213,9 +213,9 @@ __device__ __forceinline__ void add_halves(f4 (&acc)[R][C], const u4v (&bh)[R], 
 #pragma unroll
             for (int e = 0; e < R; ++e) acc[e][j] = TURNED ? mfma<F16>(b[e], c[j], acc[e][j]) : mfma<F16>(c[j], b[e], acc[e][j]);
     };
-    round(bh, ch);
     round(bl, ch);
     round(bh, cl);
+    round(bh, ch);
 }
 
 struct SmallSteps { float gram[STEPS_MOST], a[STEPS_MOST], b[STEPS_MOST], c[STEPS_MOST], next[STEPS_MOST]; u32 n; };
