@@ -279,14 +279,6 @@ __global__ __launch_bounds__(256) void activation_units(Units s, int act, const 
 static bool bad_act(int act) { return act < DBLP_ACT_NONE || act > DBLP_ACT_SILU; }
 static bool bad_sizes(u64 tokens, u64 in, u64 out) { return tokens >= COUNT_LIMIT || in >= COUNT_LIMIT || out >= COUNT_LIMIT; }
 
-// Parts of a sum over k: at most this many, and as many as fit these bytes.
-#define PARTS_MOST 64
-#define PARTS_BYTES (128ull << 20)
-static u64 parts_bytes(u64 rows, u64 cols) {
-    const u64 one = rows * round_up(cols, 4) * 4;                                    // (below 2^64: both are below 2^31)
-    return one >= PARTS_BYTES / PARTS_MOST ? PARTS_BYTES : one * PARTS_MOST;
-}
-
 extern "C" uint64_t dblp_linear_workspace(uint64_t n_tokens, uint32_t in, uint32_t out) {
     if (bad_sizes(n_tokens, in, out)) return 0;
     u64 most = parts_bytes(n_tokens, out);
@@ -381,13 +373,14 @@ static void few(Launches& launch, hipStream_t stream, Product a, Out out, PartOu
     if (p > 1) {
         a.part = (u32)round_up((a.depth + p - 1) / p, TURN);
         a.parts = (a.depth + a.part - 1) / a.part;
+        parts.parts = a.parts;
     }
     for (a.tile0 = 0; a.tile0 < blocks; a.tile0 += 1u << 20) {
         const dim3 grid((u32)(blocks - a.tile0 < (1u << 20) ? blocks - a.tile0 : 1u << 20), 1, a.parts);
         if (a.parts == 1) launch(few_products<T, Out>, grid, 64 * FEW_WAVES, stream, a, out);
         else launch(few_products<T, PartOut>, grid, 64 * FEW_WAVES, stream, a, parts);
     }
-    if (a.parts > 1) each_launch<4>(a.rows, a.cols, [&](Units s) { launch(join_parts<Out>, dim3(blocks_of(s.n, 256)), 256, stream, parts, s, a.parts, out); });
+    if (a.parts > 1) each_launch<4>(a.rows, a.cols, [&](Units s) { launch(join_parts<Out>, dim3(blocks_of(s.n, 256)), 256, stream, parts, s, out); });
 }
 
 template <class T, bool P_BY_K, bool Q_BY_K, bool SUMS, class Out>
@@ -395,14 +388,14 @@ static void products(Launches& launch, hipStream_t stream, Product a, Out out, v
     if constexpr (!P_BY_K && !Q_BY_K) {
         if (few_rows(a.rows, a.cols)) {
             const u64 stride = round_up(a.cols, 4);
-            return few<T>(launch, stream, a, out, PartOut{(float*)workspace, stride, a.rows * stride, nullptr, a.rows});
+            return few<T>(launch, stream, a, out, PartOut{(float*)workspace, stride, a.rows * stride, nullptr, a.rows, 1});
         }
     }
     Way w = way_of(a.rows, a.cols, a.depth + (in_pairs<T, P_BY_K, Q_BY_K>(a) ? 1 : 0), sizeof(typename T::elem));
     if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0};
     a.parts = w.parts;
     a.part = w.parts > 1 ? w.part : (u32)round_up(a.depth ? a.depth : 1, 64);
-    PartOut parts = {(float*)workspace, round_up(a.cols, 4), 0, nullptr, a.rows};
+    PartOut parts = {(float*)workspace, round_up(a.cols, 4), 0, nullptr, a.rows, a.parts};
     parts.step = a.rows * parts.stride;
     bool row_sums = false;
     if constexpr (SUMS) {
@@ -428,7 +421,7 @@ static void products(Launches& launch, hipStream_t stream, Product a, Out out, v
     if (!row_sums) parts.row_sums = nullptr;
     if (w.parts == 1) return tiles<T, P_BY_K, Q_BY_K, SUMS>(launch, stream, a, w.kind, out);
     tiles<T, P_BY_K, Q_BY_K, SUMS>(launch, stream, a, w.kind, parts);
-    each_launch<4>(a.rows, a.cols, [&](Units s) { launch(join_parts<Out>, dim3(blocks_of(s.n, 256)), 256, stream, parts, s, w.parts, out); });
+    each_launch<4>(a.rows, a.cols, [&](Units s) { launch(join_parts<Out>, dim3(blocks_of(s.n, 256)), 256, stream, parts, s, out); });
 }
 
 extern "C" int dblp_linear(int device, void* stream, uint64_t n_tokens, uint32_t in, uint32_t out, const void* d_x, uint64_t x_stride,

@@ -608,20 +608,21 @@ __device__ __forceinline__ void store4(int type, void* p, u64 at, u32 left, cons
 }
 struct None {};
 
-// Parts of a sum over k, each a matrix of floats of its own, to be joined.
+// Parts of a sum over k, each a matrix of floats of its own, to be joined; those of one matrix of a batch behind each other.
 struct PartOut {
     float* p;
     u64 stride, step;            // of rows, a multiple of four; of parts
     float* row_sums;
-    u32 rows;
+    u32 rows, parts;
     __device__ __forceinline__ None get(u32, u32, u32, u32) const { return None(); }
-    __device__ __forceinline__ void put(u32, u32 part, u32 m, u32 n, u32, f4 acc, None) const { *(f4*)(p + part * step + m * stride + n) = acc; }
+    __device__ __forceinline__ void put(u32 matrix, u32 part, u32 m, u32 n, u32, f4 acc, None) const { *(f4*)(p + ((u64)matrix * parts + part) * step + m * stride + n) = acc; }
     __device__ __forceinline__ void sums(u32, u32 part, u32 m, float s) const { if (row_sums) row_sums[(u64)part * rows + m] = s; }
 };
 
 // Adds the parts up, one after the other, eight of them on their way, and hands the results on: a thread takes four columns.
 template <class Out>
-__global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, u32 parts, Out out) {
+__global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, Out out) {
+    const u32 parts = in.parts, matrix = blockIdx.z;
     const u32 u = blockIdx.x * 256 + threadIdx.x;
     if (u >= s.n) return;
     const u32 row = s.per_row.of(u), c = (u - row * s.per_row.d) * 4, m = (u32)s.row0 + row;
@@ -637,8 +638,8 @@ __global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, u32 parts
         out.sums(0, 0, m, sum);
     }
     if (c >= s.cols) return;
-    const auto met = out.get(0, m, c, s.cols);
-    const float* const p = in.p + m * in.stride + c;
+    const auto met = out.get(matrix, m, c, s.cols);
+    const float* const p = in.p + (u64)matrix * parts * in.step + m * in.stride + c;
     f4 sum = {};
     for (u32 i = 0; i < parts; i += 8) {
         f4 v[8];
@@ -647,7 +648,15 @@ __global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, u32 parts
 #pragma unroll
         for (u32 j = 0; j < 8; ++j) sum += v[j];
     }
-    out.put(0, 0, m, c, s.cols, sum, met);
+    out.put(matrix, 0, m, c, s.cols, sum, met);
+}
+
+// At most this many parts, and as many as fit these bytes.
+#define PARTS_MOST 64
+#define PARTS_BYTES (128ull << 20)
+static u64 parts_bytes(u64 rows, u64 cols) {
+    const u64 one = rows * round_up(cols, 4) * 4;                                    // (below 2^64: both are below 2^31)
+    return one >= PARTS_BYTES / PARTS_MOST ? PARTS_BYTES : one * PARTS_MOST;
 }
 
 // Launches of a product's tiles: at most 2^20 tiles and 2^15 matrices' parts each (a grid's threads stay below 2^32, its z below 2^16).

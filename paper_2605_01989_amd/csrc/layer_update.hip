@@ -365,7 +365,10 @@ __global__ __launch_bounds__(256) void update_plain(HalvesAt x, Shape s, UpdateO
 // C-ABI
 // ------------------------------------------------------------------------------------------
 // Where the matrices lie in the workspace, each as high and low halves of padded rows and columns, and the partial norms.
-struct Space { u64 rows, cols, parts, x[2], gram, poly, bytes; };
+static constexpr bool is_parts(const PartOut&) { return true; }
+template <class Out> static constexpr bool is_parts(const Out&) { return false; }
+
+struct Space { u64 rows, cols, norms, x[2], gram, poly, parts, bytes; };
 
 static Space space_of(u64 count, u64 rows, u64 cols) {
     Space s = {};
@@ -373,10 +376,11 @@ static Space space_of(u64 count, u64 rows, u64 cols) {
     const auto take = [&](u64 bytes) { const u64 here = at; at += round_up(bytes, 256); return here; };
     s.rows = round_up(rows < cols ? rows : cols, 64);
     s.cols = round_up(rows < cols ? cols : rows, 64);
-    s.parts = take(count * norm_blocks(rows * cols) * 8);
+    s.norms = take(count * norm_blocks(rows * cols) * 8);
     for (int i = 0; i < 2; ++i) s.x[i] = take(count * s.rows * s.cols * 4);
     s.gram = take(count * s.rows * s.rows * 4);
     s.poly = take(count * s.rows * s.rows * 4);
+    s.parts = take(parts_bytes(count * s.rows, s.rows));
     s.bytes = at + 256;
     return s;
 }
@@ -449,7 +453,7 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
     const hipStream_t st = (hipStream_t)stream;
     const Space at = space_of(count, rows, cols);
     uint8_t* const ws = (uint8_t*)d_workspace;
-    double* const parts = (double*)(ws + at.parts);
+    double* const norms = (double*)(ws + at.norms);
     const u64 values = at.rows * at.cols, square = at.rows * at.rows;
     const auto halves = [&](u64 place, u64 cols) { return HalvesAt{(_Float16*)(ws + place), cols, 2 * at.rows * cols, at.rows * cols}; };
     HalvesAt x = halves(at.x[0], at.cols), next = halves(at.x[1], at.cols);
@@ -495,41 +499,65 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
         by_type(g_type, [&](auto tt) {
             typedef decltype(tt) T;
             typedef const typename T::elem* in;
-            launch(norm_parts<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, rows, cols, across, m, parts);
+            launch(norm_parts<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, rows, cols, across, m, norms);
             // (a grid has at most 2^16 blocks that way: 64 rows each are more than there are of the shorter side)
-            launch(scale_in<T>, dim3((u32)(at.cols / 64), (u32)(at.rows / 64), n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)parts, n_parts, up, x);
+            launch(scale_in<T>, dim3((u32)(at.cols / 64), (u32)(at.rows / 64), n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)norms, n_parts, up, x);
         });
     });
-    // R = P Q^T for all matrices, summed over all k of the halves; of a symmetric one the tiles on and above the diagonal.
-    // The kind of tiles by an estimate of the time: rounds over the 256 CUs, of a fixed time and one for each stage of 64 k, in microseconds as measured.
+    // R = P Q^T for all matrices, summed over all k of the halves; of a symmetric one the tiles on and above the diagonal, in parts where that is a few of them.
+    // The kind of tiles and the number of parts by an estimate of the time: rounds over the 256 CUs, of a fixed time and one for each stage of 64 k, in microseconds as measured; parts
+    // are written, read and added up at 5 TB/s.
     const auto product = [&](auto p_by_k, auto q_by_k, auto symmetric, const HalvesAt& P, const HalvesAt& Q, u64 m_rows, u64 m_cols, u64 depth, auto out) {
         constexpr bool PK = decltype(p_by_k)::value, QK = decltype(q_by_k)::value, SYM = decltype(symmetric)::value;
-        typedef decltype(out) Out;
-        const Product a = {{P.p, P.stride, P.step, P.low}, {Q.p, Q.stride, Q.step, Q.low}, (u32)m_rows, (u32)m_cols, (u32)(3 * depth), 0, (u32)(3 * depth), 1};
-        const auto go = [&](auto waves) {
-            typedef decltype(waves) W;
-            each_tiles<W::BM, W::BN>(a, count, [&](Product p, dim3 grid, u64 m) {
-                out.matrix0 = m;
-                p.P.p = P.p + m * P.step;
-                p.Q.p = Q.p + m * Q.step;
-                launch(ring_products<F16, PK, QK, false, false, W, false, Out, true, SYM>, grid, 64 * W::ALL, st, p, out);
-            }, SYM);
-        };
         static const struct { u32 tile, blocks; double fixed, first, more; } K[4] = {{64, 3, 4.0, 0.30, 0.11}, {128, 2, 8.0, 0.76, 0.35}, {192, 1, 14.0, 1.08, 0}, {256, 1, 14.0, 1.60, 0}};
+        Product a = {{P.p, P.stride, P.step, P.low}, {Q.p, Q.stride, Q.step, Q.low}, (u32)m_rows, (u32)m_cols, (u32)(3 * depth), 0, (u32)(3 * depth), 1};
+        const bool far = !in_reach<F16>(a.P) || !in_reach<F16>(a.Q);                      // (a tile of more rows would be out of reach)
+        const u64 stages = a.depth / 64, bytes = count * m_rows * m_cols * 4;
         int best = 0;
         double least = 1e30;
-        const bool far = !in_reach<F16>(a.P) || !in_reach<F16>(a.Q);                      // (a tile of more rows would be out of reach)
         for (int i = 0; i < (far ? 1 : 4); ++i) {
             if (K[i].tile == 192 && !SYM) continue;
-            const double down = ceil(m_rows / (double)K[i].tile), across = ceil(m_cols / (double)K[i].tile), blocks = count * (SYM ? down * (down + 1) / 2 : down * across);
-            const double rounds = ceil(blocks / (256.0 * K[i].blocks)), held = rounds > 1 ? K[i].blocks : ceil(blocks / 256.0);
-            const double t = rounds * (K[i].fixed + a.depth / 64 * (K[i].first + (held - 1) * K[i].more));
-            if (t < least) { least = t; best = i; }
+            const double down = ceil(m_rows / (double)K[i].tile), across = ceil(m_cols / (double)K[i].tile), tiles = count * (SYM ? down * (down + 1) / 2 : down * across);
+            for (u64 p = 1; p <= (SYM ? PARTS_MOST : 1) && (p == 1 || (p * bytes <= PARTS_BYTES && stages / p >= 4)); ++p) {
+                const u64 each = (stages + p - 1) / p;
+                if ((stages + each - 1) / each != p) continue;
+                const double blocks = tiles * p, rounds = ceil(blocks / (256.0 * K[i].blocks)), held = rounds > 1 ? K[i].blocks : ceil(blocks / 256.0);
+                const double t = rounds * (K[i].fixed + each * (K[i].first + (held - 1) * K[i].more)) + (p > 1 ? 4.0 + p * bytes * 2 / 5e6 : 0.0);
+                if (t < least) {
+                    least = t;
+                    best = i;
+                    a.parts = (u32)p;
+                    a.part = (u32)(each * 64);
+                }
+            }
         }
+        const PartOut parts = {(float*)(ws + at.parts), m_cols, m_rows * m_cols, nullptr, (u32)m_rows, a.parts};
+        const auto tiles_of = [&](auto waves, auto to) {
+            typedef decltype(waves) W;
+            each_tiles<W::BM, W::BN>(a, count, [&](Product p, dim3 grid, u64 m) {
+                if constexpr (is_parts(to)) to.p = parts.p + m * a.parts * parts.step;
+                else to.matrix0 = m;
+                p.P.p = P.p + m * P.step;
+                p.Q.p = Q.p + m * Q.step;
+                launch(ring_products<F16, PK, QK, false, false, W, false, decltype(to), true, SYM>, grid, 64 * W::ALL, st, p, to);
+            }, SYM);
+        };
+        const auto go = [&](auto waves) {
+            if constexpr (SYM) if (a.parts > 1) return tiles_of(waves, parts);
+            tiles_of(waves, out);
+        };
         if (best == 0) go(Waves<2, 2, 2, 2, 3>());
         else if (best == 1) go(Waves<2, 2, 4, 4, 2>());
         else if (best == 3) go(Waves<2, 4, 8, 4, 2>());
         else if constexpr (SYM) go(Waves<2, 4, 6, 3, 3>());
+        if constexpr (SYM)
+            if (a.parts > 1)
+                each_matrix([&](u64 m, u32 n) {
+                    PartOut in = parts;
+                    in.p += m * a.parts * parts.step;
+                    out.matrix0 = m;
+                    each_launch<4>(m_rows, (u32)m_cols, [&](Units s) { launch(join_parts<decltype(out)>, dim3(blocks_of(s.n, 256), 1, n), 256, st, in, s, out); });
+                });
     };
     if (steps == 0)
         each_matrix([&](u64 m, u32 n) {

@@ -306,7 +306,7 @@ def test_gradients_of_two_layers(act):
             assert abs(slope - want) <= curve + (2 * 2 * (wide + dim + 8) * U * mag) / step
 
 
-ORTHOGONAL = [(1, 1, 1), (1, 1, 5), (1, 7, 1), (2, 3, 4), (1, 16, 16), (3, 17, 40), (2, 40, 17), (1, 64, 64), (1, 128, 128), (2, 100, 128), (1, 130, 65), (1, 65, 300), (2, 129, 257), (1, 300, 200)]
+ORTHOGONAL = [(1, 1, 1), (1, 1, 5), (1, 7, 1), (2, 3, 4), (1, 16, 16), (3, 17, 40), (2, 40, 17), (1, 64, 64), (1, 128, 128), (2, 100, 128), (1, 130, 65), (1, 65, 300), (2, 129, 257), (1, 300, 200), (3, 64, 6016), (2, 4100, 70), (1, 10, 20001), (1, 600, 513)]
 
 
 @pytest.mark.parametrize("t", TYPES)
@@ -347,6 +347,20 @@ def test_orthogonalize_makes_singular_values_alike():
         s = torch.linalg.svdvals(d(got))
         assert 0.67 < float(s.min()) and float(s.max()) < 1.22
         assert float((d(u).T @ d(got) @ d(v) - torch.eye(r, dtype=torch.float64)).abs().max()) < 0.34
+
+
+def test_orthogonalize_of_many_matrices():
+    """More of them than a grid's third dimension holds, small ones of one launch and others."""
+    import paper_2605_01989_amd as dblp
+    g = gen(13)
+    for count, rows, cols in ((70000, 3, 4), (33000, 2, 129)):
+        x = torch.randn(count, rows, cols, generator=g, device="cuda")
+        out = torch.empty_like(x)
+        dblp.orthogonalize(x, out, space(dblp.orthogonalize_workspace(count, rows, cols)))
+        for i in (0, 1, 32767, 32768, count - 1):
+            want, e = ref.orthogonal(d(x[i]), 5)
+            assert float((d(out[i]) - want).norm()) <= e + 4 * U * float(want.norm()), (count, i)
+        assert bool(torch.isfinite(out).all())
 
 
 def test_orthogonalize_of_zeros_and_what_is_not_finite():
