@@ -10,7 +10,8 @@ again, and every worker applies the mean that the receiver formed.
 The right answer to a token is its successor, the reward one for it and zero otherwise, so the mean reward says whether all of it works:
 it begins at one over the vocabulary and ends near one.
 
-Matrix products, sampling and the update are torch's; everything else is a kernel of the library.  Prints one JSON object.  GPU required.
+Sampling is torch's, and so are, unless --layers is given, the matrix products and the update; everything else is a kernel of the library.  With --layers the products are
+the library's too, and the square matrix is updated by its mean gradient made orthogonal.  Prints one JSON object.  GPU required.
 """
 from __future__ import annotations
 
@@ -49,19 +50,38 @@ class Policy:
 
 
 class Worker:
-    """One worker's buffers, and its step.  Activations and logits are of type `dtype`."""
+    """One worker's buffers, and its step.  Activations and logits are of type `dtype`; layers: the library's products and not torch's."""
 
-    def __init__(self, policy, batch, seq, rank, p_drop, dtype=torch.bfloat16):
+    def __init__(self, policy, batch, seq, rank, p_drop, dtype=torch.bfloat16, layers=False):
         vocab, dim = policy.shapes[0]
         t, f = batch * seq, dict(device="cuda")
+        self.layers = layers
         self.policy, self.rank, self.p_drop, self.batch, self.seq, self.dtype = policy, rank, p_drop, batch, seq, dtype
         self.gen = torch.Generator(device="cuda").manual_seed(1000 + rank)
         self.pos = torch.arange(seq, **f).repeat(batch)
         self.h, self.y, self.dz = (torch.empty(t, dim, dtype=dtype, **f) for _ in range(3))
         self.stats, self.old, self.ref = torch.empty(5, **f), torch.empty(t, **f), torch.empty(t, **f)
         self.grad = torch.empty(policy.n, **f)
-        self.ws = torch.empty(max(dblp.embed_grad_workspace(t, vocab, dim), dblp.embed_grad_workspace(t, seq, dim), dblp.logits_workspace(t, vocab)),
-                              dtype=torch.uint8, **f)
+        self.ws = torch.empty(max(dblp.embed_grad_workspace(t, vocab, dim), dblp.embed_grad_workspace(t, seq, dim), dblp.logits_workspace(t, vocab),
+                                  dblp.linear_workspace(t, dim, vocab), dblp.linear_workspace(t, dim, dim)), dtype=torch.uint8, **f)
+
+    def product(self, x, weight):
+        """x weight^T, the weight in the activations' type."""
+        if not self.layers:
+            return x @ weight.T
+        out = torch.empty(x.shape[0], weight.shape[0], dtype=x.dtype, device=x.device)
+        dblp.linear(x, weight, out, self.ws)
+        return out
+
+    def product_grad(self, dy, x, weight, grad, base=None):
+        """The gradient of x, on top of `base`; that of the weight in `grad`."""
+        if not self.layers:
+            grad.copy_(dy.T @ x)
+            return dy @ weight if base is None else torch.addmm(base, dy, weight)
+        dx = torch.empty_like(x)
+        dblp.linear_grad_weight(dy, x, grad, self.ws)
+        dblp.linear_grad_input(dy, weight, dx, self.ws, base=base)
+        return dx
 
     def masks(self, step):
         """Of the sum of embeddings and of the residual branch; the seed is the worker's, a step draws two."""
@@ -74,8 +94,8 @@ class Worker:
         table, positions, mix = params
         first, second = self.masks(step)
         dblp.embed(self.tokens, table, self.h, positions=self.pos, pos_table=positions, drop=first)
-        dblp.dropout(self.h @ mix.to(self.dtype).T, self.y, second, residual=self.h)
-        return self.y @ table.to(self.dtype).T
+        dblp.dropout(self.product(self.h, mix.to(self.dtype)), self.y, second, residual=self.h)
+        return self.product(self.y, table.to(self.dtype))
 
     def sample(self, start):
         """New prompts, answers to them, and both policies' scores."""
@@ -103,11 +123,9 @@ class Worker:
         x = self.logits((p.table, p.positions, p.mix), step)
         dblp.policy_loss(x, self.targets, self.advantages, self.weights, self.stats, self.ws, old_logp=self.old, ref_logp=self.ref,
                          dlogits=x, clip=CLIP, kl_coef=KL)
-        g_table.copy_(x.T @ self.y)                                                      # the table as the output head
-        dy = x @ p.table.to(self.dtype)
+        dy = self.product_grad(x, self.y, p.table.to(self.dtype), g_table)               # the table as the output head
         dblp.dropout(dy, self.dz, second)
-        g_mix.copy_(self.dz.T @ self.h)
-        dh = torch.addmm(dy, self.dz, p.mix.to(self.dtype))
+        dh = self.product_grad(self.dz, self.h, p.mix.to(self.dtype), g_mix, base=dy)
         dblp.embed_grad(self.tokens, dh, g_table, self.ws, drop=first, base=g_table)     # and as the embedding, on top
         dblp.embed_grad(self.pos, dh, g_positions, self.ws, drop=first)
         return self.grad
@@ -161,10 +179,33 @@ class Receiver:
         return again, agg.phase_signal()[0]
 
 
-def train(workers=4, iterations=40, steps=3, vocab=64, seq=32, dim=128, batch=64, p_drop=0.1, loss=0.1, bound_ppm=20_000, rate=4.0, max_norm=0.25):
+class Update:
+    """The step that a mean gradient is made into: its direction, clipped, or, of the square matrix and with `layers`, the nearly orthogonal matrix of a momentum of it."""
+
+    def __init__(self, policy, rate, max_norm, layers, matrix_rate=0.02, momentum=0.8):
+        self.policy, self.rate, self.max_norm, self.layers, self.matrix_rate, self.momentum = policy, rate, max_norm, layers, matrix_rate, momentum
+        if layers:
+            self.mean_mix = torch.zeros_like(policy.mix)
+            self.ws = torch.empty(dblp.orthogonalize_workspace(1, *policy.mix.shape), dtype=torch.uint8, device="cuda")
+
+    def __call__(self, mean, norm):
+        p = self.policy
+        step = -self.rate * min(1.0, self.max_norm / max(norm, 1e-30))
+        if not self.layers:
+            p.flat.add_(mean, alpha=step)
+            return
+        table, positions, mix = p.views(mean)
+        p.table.add_(table, alpha=step)
+        p.positions.add_(positions, alpha=step)
+        self.mean_mix.mul_(self.momentum).add_(mix)
+        dblp.orthogonalize(self.mean_mix, p.mix, self.ws, scale=-self.matrix_rate, base=p.mix)
+
+
+def train(workers=4, iterations=40, steps=3, vocab=64, seq=32, dim=128, batch=64, p_drop=0.1, loss=0.1, bound_ppm=20_000, rate=4.0, max_norm=0.25, layers=False):
     policy = Policy(vocab, seq, dim, seed=1)
     start = [v.clone() for v in (policy.table, policy.positions, policy.mix)]
-    group = [Worker(policy, batch, seq, rank, p_drop) for rank in range(workers)]
+    group = [Worker(policy, batch, seq, rank, p_drop, layers=layers) for rank in range(workers)]
+    update = Update(policy, rate, max_norm, layers)
     receiver = Receiver(policy, workers, loss, bound_ppm)
     out = dict(workers=workers, parameters=policy.n, packets_of_a_round=workers * receiver.agg.n_pkts, reward=[], kl=[], clipped=[], sent_again=0, rounds=0)
     for it in range(iterations):
@@ -175,7 +216,7 @@ def train(workers=4, iterations=40, steps=3, vocab=64, seq=32, dim=128, batch=64
             again, norm = receiver.round(number + 1, grads)
             out["sent_again"] += again
             out["rounds"] += 1
-            policy.flat.add_(receiver.mean, alpha=-rate * min(1.0, max_norm / max(norm, 1e-30)))
+            update(receiver.mean, norm)
         stats = torch.stack([w.stats for w in group]).mean(0).tolist()
         out["kl"].append(round(stats[2], 4))
         out["clipped"].append(round(stats[3] / max(stats[4], 1.0), 4))
@@ -188,9 +229,10 @@ def main():
     ap.add_argument("--iterations", type=int, default=40)
     ap.add_argument("--loss", type=float, default=0.1)
     ap.add_argument("--bound-ppm", type=int, default=20_000)
+    ap.add_argument("--layers", action="store_true", help="the library's matrix products, and the square matrix' update made orthogonal")
     args = ap.parse_args()
     assert torch.cuda.is_available(), "needs a GPU"
-    print(json.dumps(train(workers=args.workers, iterations=args.iterations, loss=args.loss, bound_ppm=args.bound_ppm)))
+    print(json.dumps(train(workers=args.workers, iterations=args.iterations, loss=args.loss, bound_ppm=args.bound_ppm, layers=args.layers)))
 
 
 if __name__ == "__main__":
