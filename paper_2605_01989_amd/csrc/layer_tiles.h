@@ -532,13 +532,6 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
             if (group == i * 16 / NM / 4 && m0 + wm + i * 16 + in_group < a.rows) out.sums(matrix, part, m0 + wm + i * 16 + in_group, sum[i * 16 / NM % 4]);
 }
 
-// Columns [n, n + 4) of a row, as floats.
-template <class T>
-__device__ __forceinline__ void get4(const typename T::elem* row, u32 n, u32 cols, float (&v)[4]) {
-    typedef Vec<T, 4> V;
-    V::open(n + 4 <= cols ? V::load(row + n) : V::some(row + n, cols - n), v);
-}
-
 // ------------------------------------------------------------------------------------------
 // At most 16 rows (tokens that are decoded): the weights are read once, from memory straight into the matrix instructions' registers.  A block makes 16 columns of all rows; its
 // waves share k, 128 bytes of it at a time, and add their sums up in LDS.  Bound by the reading of Q; P comes from the caches.

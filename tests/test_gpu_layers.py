@@ -36,7 +36,8 @@ def act_slack(y, w, p):
 
 # tokens, in, out, padding of the rows, shift: none of one, one of each, odd ones, whole tiles and one more, many k
 SHAPES = [(0, 5, 7, 0, 0), (3, 0, 5, 0, 0), (4, 6, 0, 0, 0), (1, 1, 1, 0, 0), (1, 64, 128, 0, 0), (1, 333, 70, 0, 0), (2, 7, 3, 0, 1), (5, 8, 64, 8, 0), (16, 256, 48, 0, 0),
-          (17, 40, 129, 3, 2), (33, 130, 65, 0, 0), (64, 64, 64, 0, 0), (100, 333, 61, 1, 1), (129, 200, 257, 0, 0), (300, 1000, 40, 0, 0), (257, 65, 260, 7, 3)]
+          (17, 40, 129, 3, 2), (33, 130, 65, 0, 0), (64, 64, 64, 0, 0), (100, 333, 61, 1, 1), (129, 200, 257, 0, 0), (300, 1000, 40, 0, 0), (257, 65, 260, 7, 3),
+          (100, 66, 130, 2, 2), (70, 70, 68, 0, 2), (90, 129, 67, 4, 1), (20, 190, 30, 2, 6)]
 
 
 @pytest.mark.parametrize("out", ["same", "f32"])
@@ -494,6 +495,49 @@ def test_offsets_past_32_bits():
     dblp.linear_grad_input(dy, w, dx, ws)
     dblp.linear_grad_input(fdy, w, fdx, ws)
     assert torch.equal(dx, fdx)
+
+
+def test_rows_far_apart_within_a_tiles_reach():
+    """Rows as far apart as a tile's offsets reach, where the wide kernels still take them, and one element farther, where they do not."""
+    import paper_2605_01989_amd as dblp
+    n, inner, outer = 600, 72, 80
+    g = gen(21)
+    buf = torch.empty(n * ((1 << 21) + 2), dtype=torch.bfloat16, device="cuda")
+    for t, far in ((torch.bfloat16, (1 << 21) - 2), (torch.bfloat16, (1 << 21) - 1), (torch.bfloat16, 1 << 21), (torch.float32, (1 << 20) - 1), (torch.float32, 1 << 20)):
+        x, w, dy = (torch.randn(*s, generator=g, device="cuda").to(t) for s in ((n, inner), (outer, inner), (n, outer)))
+        ws = space(dblp.linear_workspace(n, inner, outer))
+        apart = lambda m: buf.view(t).as_strided(m.shape, (far, 1)).copy_(m)  # noqa: E731
+        y, fy = torch.empty(n, outer, dtype=t, device="cuda"), torch.empty(n, outer, dtype=t, device="cuda")
+        dblp.linear(x, w, y, ws)
+        dblp.linear(apart(x), w, fy, ws)
+        close(fy, d(x) @ d(w).T, 2 * (inner + 4) * U * (d(x).abs() @ d(w).abs().T), t)
+        assert torch.equal(y, fy)
+        dx, fdx = torch.empty(n, inner, dtype=t, device="cuda"), torch.empty(n, inner, dtype=t, device="cuda")
+        dblp.linear_grad_input(dy, w, dx, ws)
+        dblp.linear_grad_input(apart(dy), w, fdx, ws)
+        for got in (dx, fdx):
+            close(got, d(dy) @ d(w), 2 * (outer + 4) * U * (d(dy).abs() @ d(w).abs()), t)
+        dw, fdw = torch.empty(outer, inner, device="cuda"), torch.empty(outer, inner, device="cuda")
+        dblp.linear_grad_weight(dy, x, dw, ws)
+        dblp.linear_grad_weight(apart(dy), x, fdw, ws)
+        for got in (dw, fdw):
+            close(got, d(dy).T @ d(x), 2 * (n + 4) * U * (d(dy).abs().T @ d(x).abs()), torch.float32)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+def test_values_below_the_normal_numbers_count(t):
+    """16-bit operands below their type's normal numbers are multiplied as what they are."""
+    import paper_2605_01989_amd as dblp
+    t = TYPES[t]
+    tiny = torch.finfo(t).tiny
+    g = gen(22)
+    for n, inner, outer in ((3, 64, 32), (80, 96, 70), (70, 65, 33)):
+        x = (torch.randint(-60, 60, (n, inner), generator=g, device="cuda") / 64 * tiny).to(t)
+        w = (torch.randn(outer, inner, generator=g, device="cuda") * 2.0 ** (120 if t == torch.bfloat16 else 10)).to(t)
+        y = torch.empty(n, outer, device="cuda")
+        dblp.linear(x, w, y, space(dblp.linear_workspace(n, inner, outer)))
+        assert bool((x != 0).any()) and float(x.float().abs().max()) < tiny
+        close(y, d(x) @ d(w).T, 2 * (inner + 4) * U * (d(x).abs() @ d(w).abs().T), torch.float32)
 
 
 def test_rows_that_are_one_row():
