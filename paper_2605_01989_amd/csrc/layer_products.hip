@@ -295,7 +295,7 @@ struct Way { Kind kind; u32 parts, part; };
 // kind and number of parts on them (8192 x 1024 x 4096 in tiles of 64, 128, 256: 118, 79, 68 us; 8192 x 768 x 2304: 18, 18, 26; its weight's gradient in 1, 4, 8 parts: 85, 44, 46).
 static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
     static const struct { u32 tile, blocks; double fixed, stage[2][3]; } K[KINDS] = {
-        {64, 3, 3.5, {{0.28, 0.40, 0.50}, {0.65, 0.90, 1.10}}}, {128, 2, 5.0, {{0.64, 0.98, 0}, {2.2, 3.6, 0}}}, {256, 1, 10.0, {{1.15, 0, 0}, {0, 0, 0}}}};
+        {64, 3, 3.5, {{0.28, 0.40, 0.50}, {0.65, 0.90, 1.10}}}, {128, 2, 5.0, {{0.64, 0.98, 0}, {1.85, 2.65, 0}}}, {256, 1, 10.0, {{1.15, 0, 0}, {0, 0, 0}}}};
     Way best = {TILES_64, 1, 0};
     double least = 1e30;
     const u64 ks = 128 / elem, stages = (depth + ks - 1) / ks, bytes = rows * round_up(cols, 4) * 4;

@@ -35,6 +35,41 @@ template <> __device__ __forceinline__ u4v ones<BF16>() { return (u4v)(0x3F803F8
 template <> __device__ __forceinline__ u4v ones<F16>() { return (u4v)(0x3C003C00u); }
 template <> __device__ __forceinline__ u4v ones<F32>() { return (u4v)(0x3F800000u); }
 
+// Floats as sums of three bf16 values: the upper half of the bits, rounded, that of what is left, and the rest, which has eight bits at most.  A product of two such sums is taken as the
+// six of its nine products that are above 2^-24 of it, each exact, on units of sixteen times the rate: what is left out is no more than the rounding of a product to fp32.  Of values that
+// are not finite, or whose upper half is rounded to infinity, it is NaN.  (The bits' arithmetic runs at the full rate, conversions do not.)
+struct Thirds { u4v high, middle, low; };
+__device__ __forceinline__ u32 upper_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }       // of b, of a
+__device__ __forceinline__ Thirds thirds_of(u4v a, u4v b) {
+    const u32 x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    u32 h[8], m[8], l[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        h[i] = (x[i] + 0x8000u) & 0xFFFF0000u;
+        const float r = __builtin_bit_cast(float, x[i]) - __builtin_bit_cast(float, h[i]);
+        m[i] = __builtin_bit_cast(u32, r) & 0xFFFF0000u;
+        l[i] = __builtin_bit_cast(u32, r - __builtin_bit_cast(float, m[i]));
+    }
+    const auto pack = [](const u32 (&v)[8]) { return (u4v){upper_halves(v[0], v[1]), upper_halves(v[2], v[3]), upper_halves(v[4], v[5]), upper_halves(v[6], v[7])}; };
+    return {pack(h), pack(m), pack(l)};
+}
+// For several b, whose sums then need not wait for each other.
+template <int N>
+__device__ __forceinline__ void mfma_thirds(const Thirds& a, const Thirds (&b)[N], f4* const (&c)[N]) {
+    const auto round = [&](u4v x, auto y) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) *c[i] = mfma<BF16>(x, y(b[i]), *c[i]);
+    };
+    const auto high = [](const Thirds& t) { return t.high; };
+    const auto middle = [](const Thirds& t) { return t.middle; };
+    round(a.low, high);
+    round(a.high, [](const Thirds& t) { return t.low; });
+    round(a.middle, middle);
+    round(a.middle, high);
+    round(a.high, middle);
+    round(a.high, high);
+}
+
 // One operand of a batch of products: element (row, k) at row * stride + k, or at k * stride + row where it lies by k.  An operand in halves is two such matrices of
 // fp16, `low` elements apart, whose sum it is: 22 significant bits.  A product of two of those is three of the halves', low by high, high by low and high by high, one behind the
 // other in one sum over 3 k (the small ones first: they are rounded as what they are); what is left out is below the halves' own rounding.
@@ -425,63 +460,147 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
         fp.trim(ring + slot * STAGE, end);
         fq.trim(ring + slot * STAGE + FP::BYTES, end);
     };
-    u4v b[2][NM], c[NN];
-    if (stages) {
-        for (u32 i = 0; i < RING; ++i) {
+    // Floats in thirds: a stage is one step of 32 k, of which a lane holds chunks `group` and 4 + group.  Bound by the making of the thirds, 6.5 instructions a value and wave.  A tile with a
+    // result that is not finite is made again of floats.  4096 x 4096 x 4096: 685 us (200 TFLOP/s), of floats 1050 and by the library 915.
+    constexpr bool THIRDS = sizeof(elem) == 4 && NM * NN == 16;
+    if constexpr (THIRDS) {
+        const auto all = [&](auto plain) {
+            constexpr bool PLAIN = decltype(plain)::value;
+            FP p = fp;
+            FQ q = fq;
+            const auto copy_all = [&](u32 to) {
 #pragma unroll
-            for (u32 e = 0; e < COPIES; ++e) copy(e, i);
-            next_copied();
-        }
-        for (u32 i = 0; i < 2; ++i) {
-            ask();
-            put(i);
-        }
-        ask();
-        if (stages == 1) trim(0);
-        if (PAIRS && shift && k_first == 0) {
+                for (u32 e = 0; e < FP::COPIES; ++e) p.copy(e, ring_at + to * STAGE);
+#pragma unroll
+                for (u32 e = 0; e < FQ::COPIES; ++e) q.copy(e, ring_at + to * STAGE + FP::BYTES);
+                p.next();
+                q.next();
+            };
+            for (u32 i = 0; i < RING; ++i) copy_all(i);
+            u32 slot = 0;
+            for (u32 s = 0; s < stages; ++s) {
+                if (s + 1 == stages) trim(slot);
+                arrived_and_barrier<(RING - 1) * COPIES>();
+                const u32 at = slot * STAGE;
+                u4v b[NM][2];
+                Thirds t[NM];
+#pragma unroll
+                for (int i = 0; i < NM; ++i) {
+                    b[i][0] = rp.get(ring, at, 0, i);
+                    b[i][1] = rp.get(ring, at, 1, i);
+                    if (!PLAIN) t[i] = thirds_of(b[i][0], b[i][1]);
+                }
+                u4v c[NN][2];
+#pragma unroll
+                for (int j = 0; j < NN; ++j) {
+                    c[j][0] = rq.get(ring, at + FP::BYTES, 0, j);
+                    c[j][1] = rq.get(ring, at + FP::BYTES, 1, j);
+                }
+                Thirds u = {};
+                if (!PLAIN) u = thirds_of(c[0][0], c[0][1]);
+#pragma unroll
+                for (int j = 0; j < NN; ++j) {
+                    if (PLAIN) {
+#pragma unroll
+                        for (int i = 0; i < NM; ++i) acc[i][j] = mfma<F32>(c[j][1], b[i][1], mfma<F32>(c[j][0], b[i][0], acc[i][j]));
+                    } else {
+                        // the next thirds are made while these are multiplied
+                        Thirds next = {};
+                        if (j + 1 < NN) next = thirds_of(c[j + 1 < NN ? j + 1 : j][0], c[j + 1 < NN ? j + 1 : j][1]);
+                        f4* const to[4] = {&acc[0][j], &acc[1][j], &acc[2][j], &acc[3][j]};
+                        mfma_thirds<4>(u, t, to);
+                        u = next;
+                    }
+                }
+                if (SUMS && summing) {
+                    asm volatile("");
+#pragma unroll
+                    for (int i = 0; i < NM; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) sum = mfma<F32>(in_group * NM / 16 == i ? ones<F32>() : (u4v)(0u), b[i][h], sum);
+                }
+                arrived_and_barrier<(RING - 1) * COPIES>();
+                copy_all(slot);
+                slot = slot + 1 == RING ? 0 : slot + 1;
+            }
+        };
+        if (stages) {
+            all(Int<0>());
+            bool finite = true;
+#pragma unroll
+            for (int i = 0; i < NM; ++i)
+#pragma unroll
+                for (int j = 0; j < NN; ++j)
+                    for (int e = 0; e < 4; ++e) finite &= fabsf(acc[i][j][e]) <= FLT_MAX;
             arrived_and_barrier<0>();
-            for (u32 row = threadIdx.x; row < BM; row += 64 * W::ALL) *(elem*)(ring + row * STAGE_BYTES + ((row & 7) << 4)) = (elem)0.0f;
+            if (__syncthreads_or(!finite)) {
+#pragma unroll
+                for (int i = 0; i < NM; ++i)
+#pragma unroll
+                    for (int j = 0; j < NN; ++j) acc[i][j] = (f4)(0.0f);
+                sum = (f4)(0.0f);
+                all(Int<1>());
+            }
         }
-        arrived_and_barrier<(RING - 1) * COPIES>();
+    } else {
+        u4v b[2][NM], c[NN];
+        if (stages) {
+            for (u32 i = 0; i < RING; ++i) {
 #pragma unroll
-        for (int i = 0; i < NM; ++i) b[0][i] = rp.get(ring, 0, 0, i);
+                for (u32 e = 0; e < COPIES; ++e) copy(e, i);
+                next_copied();
+            }
+            for (u32 i = 0; i < 2; ++i) {
+                ask();
+                put(i);
+            }
+            ask();
+            if (stages == 1) trim(0);
+            if (PAIRS && shift && k_first == 0) {
+                arrived_and_barrier<0>();
+                for (u32 row = threadIdx.x; row < BM; row += 64 * W::ALL) *(elem*)(ring + row * STAGE_BYTES + ((row & 7) << 4)) = (elem)0.0f;
+            }
+            arrived_and_barrier<(RING - 1) * COPIES>();
 #pragma unroll
-        for (int j = 0; j < NN; ++j) c[j] = rq.get(ring, FP::BYTES, 0, j);
-    }
-    // Multiplies one half's fragments; between rows of matrix instructions, which take longer, the next half's are read and, COPYING, a stage is copied.
-    const auto half = [&](auto copying, const u4v (&b)[NM], u4v (&b1)[NM], u32 slot1, u32 half1, u32 to) {
-        constexpr int EACH = (COPIES + NN - 1) / NN;
+            for (int i = 0; i < NM; ++i) b[0][i] = rp.get(ring, 0, 0, i);
 #pragma unroll
-        for (int j = 0; j < NN; ++j) {
-#pragma unroll
-            for (int i = j * NM / NN; i < (j + 1) * NM / NN; ++i) b1[i] = rp.get(ring, slot1 * STAGE, half1, i);
-            if (decltype(copying)::value)
-#pragma unroll
-                for (u32 e = j * EACH; e < (j + 1) * EACH && e < COPIES; ++e) copy(e, to);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < NM; ++i) acc[i][j] = mfma<T>(c[j], b[i], acc[i][j]);
-            __builtin_amdgcn_sched_barrier(0);
-            c[j] = rq.get(ring, slot1 * STAGE + FP::BYTES, half1, j);
+            for (int j = 0; j < NN; ++j) c[j] = rq.get(ring, FP::BYTES, 0, j);
         }
-        // sums over k: products with ones, those of fragment i in rows 16 / NM i and up of one result
-        if (SUMS && summing) {
-            asm volatile("");                      // (or the compiler computes them everywhere and chooses)
+        // Multiplies one half's fragments; between rows of matrix instructions, which take longer, the next half's are read and, COPYING, a stage is copied.
+        const auto half = [&](auto copying, const u4v (&b)[NM], u4v (&b1)[NM], u32 slot1, u32 half1, u32 to) {
+            constexpr int EACH = (COPIES + NN - 1) / NN;
 #pragma unroll
-            for (int i = 0; i < NM; ++i) sum = mfma<T>(in_group * NM / 16 == i ? ones<T>() : (u4v)(0u), b[i], sum);
+            for (int j = 0; j < NN; ++j) {
+#pragma unroll
+                for (int i = j * NM / NN; i < (j + 1) * NM / NN; ++i) b1[i] = rp.get(ring, slot1 * STAGE, half1, i);
+                if (decltype(copying)::value)
+#pragma unroll
+                    for (u32 e = j * EACH; e < (j + 1) * EACH && e < COPIES; ++e) copy(e, to);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NM; ++i) acc[i][j] = mfma<T>(c[j], b[i], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+                c[j] = rq.get(ring, slot1 * STAGE + FP::BYTES, half1, j);
+            }
+            // sums over k: products with ones, those of fragment i in rows 16 / NM i and up of one result
+            if (SUMS && summing) {
+                asm volatile("");                      // (or the compiler computes them everywhere and chooses)
+#pragma unroll
+                for (int i = 0; i < NM; ++i) sum = mfma<T>(in_group * NM / 16 == i ? ones<T>() : (u4v)(0u), b[i], sum);
+            }
+        };
+        u32 slot = 0;
+        for (u32 s = 0; s < stages; ++s) {
+            const u32 then = slot + 1 == RING ? 0 : slot + 1;
+            half(Int<0>(), b[0], b[1], slot, 1, 0);
+            if (s + 2 == stages) trim(then);
+            arrived_and_barrier<(RING - 2) * COPIES>();
+            put((s + 2) % RING);
+            ask();
+            half(Int<1>(), b[1], b[0], then, 0, slot);
+            next_copied();
+            slot = then;
         }
-    };
-    u32 slot = 0;
-    for (u32 s = 0; s < stages; ++s) {
-        const u32 then = slot + 1 == RING ? 0 : slot + 1;
-        half(Int<0>(), b[0], b[1], slot, 1, 0);
-        if (s + 2 == stages) trim(then);
-        arrived_and_barrier<(RING - 2) * COPIES>();
-        put((s + 2) % RING);
-        ask();
-        half(Int<1>(), b[1], b[0], then, 0, slot);
-        next_copied();
-        slot = then;
     }
     // the result's tile through LDS, some of a wave's rows at a time: rows leave whole, and what is done with them stands here once
     arrived_and_barrier<0>();

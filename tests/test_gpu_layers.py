@@ -573,3 +573,28 @@ def test_norms_are_of_the_whole_matrix():
         for i in range(3):
             want = torch.tensor(math.pi).item() * d(x[i]) / d(x[i]).norm()
             close(out[i], want, (2.0 ** -22 + 4 * U) * want.abs() + 2.0 ** -30, torch.float32)
+
+
+def test_floats_of_every_size_and_what_is_not_finite_in_large_tiles():
+    """Fp32 products of many tiles: values from far below to near the largest number, and infinities, whose tiles are made in another way."""
+    import paper_2605_01989_amd as dblp
+    g = gen(31)
+    n, inner, outer = 1500, 400, 2200
+    x, w = torch.randn(n, inner, generator=g, device="cuda"), torch.randn(outer, inner, generator=g, device="cuda")
+    x *= 2.0 ** torch.randint(-60, 60, (n, 1), generator=g, device="cuda")
+    w *= 2.0 ** torch.randint(-40, 40, (outer, 1), generator=g, device="cuda")
+    x[5] = torch.finfo(torch.float32).max
+    x[5, 1:] = 0.0
+    ws = space(dblp.linear_workspace(n, inner, outer))
+    y, clean = torch.empty(n, outer, device="cuda"), torch.empty(n, outer, device="cuda")
+    dblp.linear(x, w, y, ws)
+    want, mag = x.double() @ w.double().T, x.double().abs() @ w.double().abs().T
+    assert bool((((y.double() - want).abs() <= 2 * (inner + 4) * U * mag + 2.0 ** -125) | (want.abs() * (1 + U) > torch.finfo(torch.float32).max) & torch.isinf(y)).all())
+    clean.copy_(y)
+    x[700, 3], w[900, 7], x[1400, 0] = float("inf"), -float("inf"), float("nan")
+    dblp.linear(x, w, y, ws)
+    want = x.double() @ w.double().T
+    hit = ~torch.isfinite(want)
+    assert torch.equal(torch.isnan(y), torch.isnan(want)) and torch.equal(y[hit & ~torch.isnan(want)].double(), want[hit & ~torch.isnan(want)])
+    # (a row or column that keeps its values keeps its results, to the bits where its tile was not made again)
+    assert bool((((y.double() - want).abs() <= 2 * (inner + 4) * U * mag + 2.0 ** -125) | hit | (want.abs() * (1 + U) > torch.finfo(torch.float32).max)).all())
