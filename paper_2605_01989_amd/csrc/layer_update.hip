@@ -220,77 +220,88 @@ __device__ __forceinline__ void add_halves(f4 (&acc)[R][C], const u4v (&bh)[R], 
 
 struct SmallSteps { float gram[STEPS_MOST], a[STEPS_MOST], b[STEPS_MOST], c[STEPS_MOST], next[STEPS_MOST]; u32 n; };
 
-template <class T, int R, int N>
-__global__ __launch_bounds__(512) void small_steps(const typename T::elem* g, u64 stride, u64 step, Shape s, float up, SmallSteps k, UpdateOut out) {
-    typedef Vec<T, 4> V;
-    constexpr u32 ROWS = 64 * R, COLS = 64 * N, X_LOW = ROWS * COLS * 2, A_LOW = ROWS * ROWS * 2;
-    __shared__ __attribute__((aligned(16))) uint8_t x[2 * X_LOW];
-    __shared__ __attribute__((aligned(16))) uint8_t m[2 * A_LOW];
-    __shared__ double norms[8];
-    const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, in_group = lane & 15;
-    const u64 matrix = out.matrix0 + blockIdx.x;
-    g += matrix * step;
-    const u32 g_rows = s.tall ? s.cols : s.rows, g_cols = s.tall ? s.rows : s.cols, G_COLS = s.tall ? ROWS : COLS;
-    constexpr int UNROLL = 2;
-    constexpr u32 EACH = ROWS * COLS / 2048;           // pieces of four values of a thread
-    typename V::raw r[EACH];
-    double sum = 0;
-#pragma unroll
-    for (u32 i = 0; i < EACH; ++i) {
-        const u32 u = threadIdx.x + i * 512, row = u / (G_COLS / 4), col = u % (G_COLS / 4) * 4;
-        r[i] = (typename V::raw)(0);
-        if (row < g_rows && col < g_cols) r[i] = col + 4 <= g_cols ? V::load(g + row * stride + col) : V::some(g + row * stride + col, g_cols - col);
+template <int R, int N>
+struct Small {
+    static constexpr u32 ROWS = 64 * R, COLS = 64 * N, X_LOW = ROWS * COLS * 2, A_LOW = ROWS * ROWS * 2, EACH = ROWS * COLS / 2048;       // EACH: fours of X of a thread
+    u32 group, in_group, m0, an0, xn0;
+    __device__ __forceinline__ Small() {
+        const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        group = lane >> 4;
+        in_group = lane & 15;
+        m0 = wave / 2 * 16 * R;
+        an0 = wave % 2 * 32 * R;
+        xn0 = wave % 2 * 32 * N;
     }
+    // Values of G on their way to X's columns col0 and up.
+    template <class T> struct Values {
+        typedef Vec<T, 4> V;
+        typename V::raw r[EACH];
+        u32 rows, cols, across, row0, col0;
+        bool tall;
+        __device__ __forceinline__ Values(const typename T::elem* g, u64 stride, const Shape& s, u32 first) : tall(s.tall) {
+            rows = tall ? s.cols : s.rows;
+            cols = tall ? s.rows : s.cols;
+            across = (tall ? ROWS : COLS) / 4;
+            row0 = tall ? first : 0;
+            col0 = tall ? 0 : first;
 #pragma unroll
-    for (u32 i = 0; i < EACH; ++i) {
-        float v[4];
-        V::open(r[i], v);
-        for (int e = 0; e < 4; ++e) sum += (double)v[e] * (double)v[e];
-    }
-    for (int d = 32; d; d >>= 1) sum += __shfl_down(sum, d);
-    if (lane == 0) norms[wave] = sum;
-    __syncthreads();
-    sum = 0;
-    for (int i = 0; i < 8; ++i) sum += norms[i];
-    const double q = (sum == 0.0 ? 0.0 : sum <= DBL_MAX ? 1.0 / sqrt(sum) : NAN) * up;
-#pragma unroll
-    for (u32 i = 0; i < EACH; ++i) {
-        const u32 u = threadIdx.x + i * 512, row = u / (G_COLS / 4), col = u % (G_COLS / 4) * 4;
-        float v[4];
-        V::open(r[i], v);
-        for (int e = 0; e < 4; ++e) v[e] = row < g_rows && col + e < g_cols ? (float)((double)v[e] * q) : 0.0f;
-        if (!s.tall) small_put<COLS>(x, X_LOW, row, col, v);
-        else
-            for (int e = 0; e < 4; ++e) {
-                const _Float16 high = (_Float16)v[e];
-                *(_Float16*)(x + small_at<COLS>(col + e, row)) = high;
-                *(_Float16*)(x + X_LOW + small_at<COLS>(col + e, row)) = (_Float16)(v[e] - (float)high);
+            for (u32 i = 0; i < EACH; ++i) {
+                r[i] = (typename V::raw)(0);
+                const u32 row = row0 + at(i) / across, col = col0 + at(i) % across * 4;
+                if (row < rows && col < cols) r[i] = col + 4 <= cols ? V::load(g + row * stride + col) : V::some(g + row * stride + col, cols - col);
             }
-    }
-    const u32 m0 = wave / 2 * 16 * R, an0 = wave % 2 * 32 * R, xn0 = wave % 2 * 32 * N;
-    for (u32 i = 0; i < k.n; ++i) {
-        __syncthreads();
-        // A = X X^T
-        f4 acc[R][2 * R] = {};
-        const auto square = [&](const uint8_t* of, u32 low, u32 width, auto get) {
-#pragma unroll UNROLL
-            for (u32 k0 = 0; k0 < width; k0 += 32) {
-                u4v bh[R], bl[R], ch[2 * R], cl[2 * R];
+        }
+        static __device__ __forceinline__ u32 at(u32 i) { return threadIdx.x + i * 512; }
+        __device__ __forceinline__ double squares() const {
+            double sum = 0;
 #pragma unroll
-                for (int e = 0; e < R; ++e) { bh[e] = get(of, m0 + 16 * e, k0); bl[e] = get(of + low, m0 + 16 * e, k0); }
-#pragma unroll
-                for (int j = 0; j < 2 * R; ++j) { ch[j] = get(of, an0 + 16 * j, k0); cl[j] = get(of + low, an0 + 16 * j, k0); }
-                add_halves<R, 2 * R>(acc, bh, bl, ch, cl);
+            for (u32 i = 0; i < EACH; ++i) {
+                float v[4];
+                V::open(r[i], v);
+                for (int e = 0; e < 4; ++e) sum += (double)v[e] * (double)v[e];
             }
-        };
-        square(x, X_LOW, COLS, [](const uint8_t* of, u32 row, u32 k0) { return small_rows<COLS>(of, row, k0); });
-        Halves own[R][2 * R];                          // of A: a wave's part of A A is at the same places
+            return sum;
+        }
+        // (zeros behind the matrix stay zeros where the norm is NaN)
+        __device__ __forceinline__ void put(uint8_t* x, double q) const {
+#pragma unroll
+            for (u32 i = 0; i < EACH; ++i) {
+                const u32 row = at(i) / across, col = at(i) % across * 4;
+                float v[4];
+                V::open(r[i], v);
+                for (int e = 0; e < 4; ++e) v[e] = row0 + row < rows && col0 + col + e < cols ? (float)((double)v[e] * q) : 0.0f;
+                if (!tall) small_put<COLS>(x, X_LOW, row, col, v);
+                else
+                    for (int e = 0; e < 4; ++e) {
+                        const _Float16 high = (_Float16)v[e];
+                        *(_Float16*)(x + small_at<COLS>(col + e, row)) = high;
+                        *(_Float16*)(x + X_LOW + small_at<COLS>(col + e, row)) = (_Float16)(v[e] - (float)high);
+                    }
+            }
+        }
+    };
+    // acc += M M^T of a matrix of WIDTH columns
+    template <int WIDTH>
+    __device__ __forceinline__ void square(f4 (&acc)[R][2 * R], const uint8_t* of, u32 low) const {
+#pragma unroll 2
+        for (u32 k0 = 0; k0 < WIDTH; k0 += 32) {
+            u4v bh[R], bl[R], ch[2 * R], cl[2 * R];
+#pragma unroll
+            for (int e = 0; e < R; ++e) { bh[e] = small_rows<WIDTH>(of, m0 + 16 * e, k0); bl[e] = small_rows<WIDTH>(of + low, m0 + 16 * e, k0); }
+#pragma unroll
+            for (int j = 0; j < 2 * R; ++j) { ch[j] = small_rows<WIDTH>(of, an0 + 16 * j, k0); cl[j] = small_rows<WIDTH>(of + low, an0 + 16 * j, k0); }
+            add_halves<R, 2 * R>(acc, bh, bl, ch, cl);
+        }
+    }
+    // From A's sums a + b A + c A A to m, A by the way there too; a wave's part of A A is at the same places as its part of A.
+    __device__ __forceinline__ void poly(f4 (&acc)[R][2 * R], uint8_t* m, u32 rows, float gram, float a, float b, float c) const {
+        Halves own[R][2 * R];
 #pragma unroll
         for (int e = 0; e < R; ++e)
 #pragma unroll
             for (int j = 0; j < 2 * R; ++j) {
                 float v[4];
-                for (int t = 0; t < 4; ++t) v[t] = acc[e][j][t] * k.gram[i];
+                for (int t = 0; t < 4; ++t) v[t] = acc[e][j][t] * gram;
                 own[e][j] = halves_of(v);
                 const u32 row = m0 + 16 * e + in_group, col = an0 + 16 * j + group * 4;
                 *(half4*)(m + small_at<ROWS>(row, col)) = own[e][j].high;
@@ -298,7 +309,7 @@ __global__ __launch_bounds__(512) void small_steps(const typename T::elem* g, u6
                 acc[e][j] = (f4)(0.0f);
             }
         __syncthreads();
-        square(m, A_LOW, ROWS, [](const uint8_t* of, u32 row, u32 k0) { return small_rows<ROWS>(of, row, k0); });
+        square<ROWS>(acc, m, A_LOW);
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < R; ++e)
@@ -306,43 +317,177 @@ __global__ __launch_bounds__(512) void small_steps(const typename T::elem* g, u6
             for (int j = 0; j < 2 * R; ++j) {
                 const u32 row = m0 + 16 * e + in_group, col = an0 + 16 * j + group * 4;
                 float v[4];
-                for (int t = 0; t < 4; ++t) v[t] = k.b[i] * ((float)own[e][j].high[t] + (float)own[e][j].low[t]) + k.c[i] * acc[e][j][t] + (col + t == row && row < s.rows ? k.a[i] : 0.0f);
+                for (int t = 0; t < 4; ++t) v[t] = b * ((float)own[e][j].high[t] + (float)own[e][j].low[t]) + c * acc[e][j][t] + (col + t == row && row < rows ? a : 0.0f);
                 small_put<ROWS>(m, A_LOW, row, col, v);
             }
         __syncthreads();
-        // X = (a + b A + c A A) X; of a turned matrix the last one turned back
-        const bool last = i + 1 == k.n;
-        f4 next[R][2 * N] = {};
-#pragma unroll UNROLL
+    }
+    // next = m x; turned: a result's rows and columns change places
+    __device__ __forceinline__ void apply(f4 (&next)[R][2 * N], const uint8_t* m, const uint8_t* x, bool turned) const {
+#pragma unroll 2
         for (u32 k0 = 0; k0 < ROWS; k0 += 32) {
             u4v bh[R], bl[R], ch[2 * N], cl[2 * N];
 #pragma unroll
             for (int e = 0; e < R; ++e) { bh[e] = small_rows<ROWS>(m, m0 + 16 * e, k0); bl[e] = small_rows<ROWS>(m + A_LOW, m0 + 16 * e, k0); }
 #pragma unroll
             for (int j = 0; j < 2 * N; ++j) { ch[j] = small_columns<COLS>(x, xn0 + 16 * j, k0); cl[j] = small_columns<COLS>(x + X_LOW, xn0 + 16 * j, k0); }
-            if (last && s.tall) add_halves<R, 2 * N, true>(next, bh, bl, ch, cl);
+            if (turned) add_halves<R, 2 * N, true>(next, bh, bl, ch, cl);
             else add_halves<R, 2 * N>(next, bh, bl, ch, cl);
         }
-        if (!last) {
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < R; ++e)
-#pragma unroll
-                for (int j = 0; j < 2 * N; ++j) {
-                    float v[4];
-                    for (int t = 0; t < 4; ++t) v[t] = next[e][j][t] * k.next[i];
-                    small_put<COLS>(x, X_LOW, m0 + 16 * e + in_group, xn0 + 16 * j + group * 4, v);
-                }
-            continue;
-        }
+    }
+    __device__ __forceinline__ void keep(const f4 (&next)[R][2 * N], float by, uint8_t* x) const {
 #pragma unroll
         for (int e = 0; e < R; ++e)
 #pragma unroll
             for (int j = 0; j < 2 * N; ++j) {
-                const u32 row = s.tall ? xn0 + 16 * j + in_group : m0 + 16 * e + in_group, col = s.tall ? m0 + 16 * e + group * 4 : xn0 + 16 * j + group * 4;
-                if (row < g_rows && col < g_cols) out.put(blockIdx.x, 0, row, col, g_cols, next[e][j], out.get(blockIdx.x, row, col, g_cols));
+                float v[4];
+                for (int t = 0; t < 4; ++t) v[t] = next[e][j][t] * by;
+                small_put<COLS>(x, X_LOW, m0 + 16 * e + in_group, xn0 + 16 * j + group * 4, v);
             }
     }
+    __device__ __forceinline__ void leave(const f4 (&next)[R][2 * N], const UpdateOut& out, u32 matrix, const Shape& s, u32 first) const {
+        const u32 rows = s.tall ? s.cols : s.rows, cols = s.tall ? s.rows : s.cols;
+#pragma unroll
+        for (int e = 0; e < R; ++e)
+#pragma unroll
+            for (int j = 0; j < 2 * N; ++j) {
+                const u32 row = s.tall ? first + xn0 + 16 * j + in_group : m0 + 16 * e + in_group, col = s.tall ? m0 + 16 * e + group * 4 : first + xn0 + 16 * j + group * 4;
+                if (row < rows && col < cols) out.put(matrix, 0, row, col, cols, next[e][j], out.get(matrix, row, col, cols));
+            }
+    }
+};
+
+template <class T, int R, int N>
+__global__ __launch_bounds__(512) void small_steps(const typename T::elem* g, u64 stride, u64 step, Shape s, float up, SmallSteps k, UpdateOut out) {
+    typedef Small<R, N> S;
+    __shared__ __attribute__((aligned(16))) uint8_t x[2 * S::X_LOW];
+    __shared__ __attribute__((aligned(16))) uint8_t m[2 * S::A_LOW];
+    __shared__ double norms[8];
+    const S small;
+    const typename S::template Values<T> values(g + (out.matrix0 + blockIdx.x) * step, stride, s, 0);
+    double sum = values.squares();
+    for (int d = 32; d; d >>= 1) sum += __shfl_down(sum, d);
+    if ((threadIdx.x & 63) == 0) norms[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = 0;
+    for (int i = 0; i < 8; ++i) sum += norms[i];
+    values.put(x, (sum == 0.0 ? 0.0 : sum <= DBL_MAX ? 1.0 / sqrt(sum) : NAN) * up);
+    for (u32 i = 0; i < k.n; ++i) {
+        __syncthreads();
+        f4 acc[R][2 * R] = {};
+        small.template square<S::COLS>(acc, x, S::X_LOW);
+        small.poly(acc, m, s.rows, k.gram[i], k.a[i], k.b[i], k.c[i]);
+        const bool last = i + 1 == k.n;
+        f4 next[R][2 * N] = {};
+        small.apply(next, m, x, last && s.tall);
+        if (last) {
+            small.leave(next, out, blockIdx.x, s, 0);
+        } else {
+            __syncthreads();
+            small.keep(next, k.next[i], x);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Long ones of at most 128 rows: the same by many blocks, each with some pieces of 128 columns of X.  A step is two launches: blocks multiply their pieces and add up their part of the
+// next A from them, as they lie in LDS, and one block a matrix joins the parts and makes a + b A + c A A.  What bounds it is the launches, 5 to 7 us each with a block's few products
+// in a row: 40 x 64 x 1536 in 104 us, 152 as products of tiles that go through memory; X's reads and writes where the matrices are many (300 x 64 x 3000 1040 us, 2.3 TB/s).
+// ------------------------------------------------------------------------------------------
+// 16 bytes a thread between LDS and a piece of a matrix in halves.
+template <int ROWS, int WIDTH, bool OUT>
+__device__ __forceinline__ void piece(const HalvesAt& of, u64 matrix, u32 col0, uint8_t* lds) {
+    constexpr u32 LOW = ROWS * WIDTH * 2;
+#pragma unroll
+    for (u32 i = 0; i < ROWS * WIDTH / 8 / 512; ++i) {
+        const u32 u = threadIdx.x + i * 512, row = u / (WIDTH / 8), col = u % (WIDTH / 8) * 8;
+        u4v* const high = (u4v*)(of.p + matrix * of.step + row * of.stride + col0 + col);
+        u4v* const low = (u4v*)((_Float16*)high + of.low);
+        u4v* const a = (u4v*)(lds + small_at<WIDTH>(row, col));
+        u4v* const b = (u4v*)(lds + LOW + small_at<WIDTH>(row, col));
+        if (OUT) { *high = *a; *low = *b; }
+        else { *a = *high; *b = *low; }
+    }
+}
+
+// (a thread's values of A's part lie where the same thread of the block that joins them reads 16 bytes beside its neighbours')
+template <int R>
+__device__ __forceinline__ void thin_part(const f4 (&acc)[R][2 * R], float* part) {
+#pragma unroll
+    for (int e = 0; e < R; ++e)
+#pragma unroll
+        for (int j = 0; j < 2 * R; ++j) ((f4*)part)[(e * 2 * R + j) * 512 + threadIdx.x] = acc[e][j];
+}
+
+template <class T, int R>
+__global__ __launch_bounds__(512) void thin_first(const typename T::elem* g, u64 stride, u64 step, Shape s, u64 matrix0, const double* norms, u32 n_norms, float up, HalvesAt to, float* parts) {
+    typedef Small<R, 2> S;
+    __shared__ __attribute__((aligned(16))) uint8_t x[2 * S::X_LOW];
+    const S small;
+    const u64 matrix = matrix0 + blockIdx.z;
+    const double q = one_over_norm(norms + matrix * n_norms, n_norms) * up;
+    f4 acc[R][2 * R] = {};
+    for (u32 col0 = blockIdx.x * 128; col0 < to.stride; col0 += gridDim.x * 128) {
+        const typename S::template Values<T> values(g + matrix * step, stride, s, col0);
+        __syncthreads();
+        values.put(x, q);
+        __syncthreads();
+        piece<S::ROWS, S::COLS, true>(to, matrix, col0, x);
+        small.template square<S::COLS>(acc, x, S::X_LOW);
+    }
+    thin_part<R>(acc, parts + (matrix * gridDim.x + blockIdx.x) * (S::ROWS * S::ROWS));
+}
+
+template <int R>
+__global__ __launch_bounds__(512) void thin_poly(const float* parts, u32 n_parts, u32 rows, float gram, float a, float b, float c, u64 matrix0, HalvesAt poly) {
+    typedef Small<R, 2> S;
+    __shared__ __attribute__((aligned(16))) uint8_t m[2 * S::A_LOW];
+    const S small;
+    const u64 matrix = matrix0 + blockIdx.x;
+    parts += matrix * n_parts * (S::ROWS * S::ROWS);
+    f4 acc[R][2 * R] = {};
+    for (u32 i = 0; i < n_parts; i += 4)
+#pragma unroll
+        for (int e = 0; e < R; ++e)
+#pragma unroll
+            for (int j = 0; j < 2 * R; ++j) {
+                const f4* const at = (const f4*)(parts + (u64)i * (S::ROWS * S::ROWS)) + (e * 2 * R + j) * 512 + threadIdx.x;
+                f4 v[4];
+#pragma unroll
+                for (u32 t = 0; t < 4; ++t) v[t] = i + t < n_parts ? at[t * (S::ROWS * S::ROWS / 4)] : (f4)(0.0f);
+#pragma unroll
+                for (u32 t = 0; t < 4; ++t) acc[e][j] += v[t];
+            }
+    small.poly(acc, m, rows, gram, a, b, c);
+    piece<S::ROWS, S::ROWS, true>(poly, matrix, 0, m);
+}
+
+template <int R>
+__global__ __launch_bounds__(512) void thin_apply(HalvesAt poly, HalvesAt xs, Shape s, float by, bool last, UpdateOut out, float* parts) {
+    typedef Small<R, 2> S;
+    __shared__ __attribute__((aligned(16))) uint8_t x[2 * S::X_LOW];
+    __shared__ __attribute__((aligned(16))) uint8_t m[2 * S::A_LOW];
+    const S small;
+    const u64 matrix = out.matrix0 + blockIdx.z;
+    piece<S::ROWS, S::ROWS, false>(poly, matrix, 0, m);
+    f4 acc[R][2 * R] = {};
+    for (u32 col0 = blockIdx.x * 128; col0 < xs.stride; col0 += gridDim.x * 128) {
+        __syncthreads();
+        piece<S::ROWS, S::COLS, false>(xs, matrix, col0, x);
+        __syncthreads();
+        f4 next[R][4] = {};
+        small.apply(next, m, x, last && s.tall);
+        if (last) {
+            small.leave(next, out, blockIdx.z, s, col0);
+            continue;
+        }
+        __syncthreads();
+        small.keep(next, by, x);
+        __syncthreads();
+        piece<S::ROWS, S::COLS, true>(xs, matrix, col0, x);
+        small.template square<S::COLS>(acc, x, S::X_LOW);
+    }
+    if (!last) thin_part<R>(acc, parts + (matrix * gridDim.x + blockIdx.x) * (S::ROWS * S::ROWS));
 }
 
 // No step: X itself.
@@ -375,7 +520,7 @@ static Space space_of(u64 count, u64 rows, u64 cols) {
     u64 at = 0;
     const auto take = [&](u64 bytes) { const u64 here = at; at += round_up(bytes, 256); return here; };
     s.rows = round_up(rows < cols ? rows : cols, 64);
-    s.cols = round_up(rows < cols ? cols : rows, 64);
+    s.cols = round_up(rows < cols ? cols : rows, s.rows <= 128 ? 128 : 64);        // (long ones of few rows go by pieces of 128)
     s.norms = take(count * norm_blocks(rows * cols) * 8);
     for (int i = 0; i < 2; ++i) s.x[i] = take(count * s.rows * s.cols * 4);
     s.gram = take(count * s.rows * s.rows * 4);
@@ -493,6 +638,16 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
         });
         return launched(call, launch);
     }
+    // Long ones of at most 128 rows by thin_first and what follows it, where they are many or not too long (the first of two times, in us): one block a matrix joins A's parts, and few
+    // blocks hold a single long one up.  Of 64 rows as many blocks as two fit a CU, 12 x 64 x 1671 72 and 124, 1 x 64 x 5297 84 and 112, 1 x 64 x 1000000 3129 and 2683; of 128 one a CU
+    // and 16 parts, 128 x 128 x 2048 509 and 918, 16 x 128 x 4096 226 and 279, 1 x 128 x 512 95 and 106, 1 x 128 x 5297 212 and 140.  A's parts lie where the others' do, a single one where A would.
+    const bool few_rows = at.rows == 64;
+    const u32 pieces = (u32)(at.cols / 128);
+    u32 blocks = (u32)((few_rows ? 512 : 256) / count);
+    if (blocks > (few_rows ? PARTS_MOST : 16)) blocks = few_rows ? PARTS_MOST : 16;
+    if (blocks > pieces) blocks = pieces;
+    if (blocks < 1) blocks = 1;
+    const bool thin = steps && at.rows <= 128 && (blocks * count >= 256 || pieces <= (few_rows ? 256 : 4));
     u32 across = 1;
     while (across < 256 && across * 4 < cols) across *= 2;
     each_matrix([&](u64 m, u32 n) {
@@ -500,10 +655,32 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
             typedef decltype(tt) T;
             typedef const typename T::elem* in;
             launch(norm_parts<T>, dim3(n_parts, 1, n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, rows, cols, across, m, norms);
+            if (thin) return;
             // (a grid has at most 2^16 blocks that way: 64 rows each are more than there are of the shorter side)
             launch(scale_in<T>, dim3((u32)(at.cols / 64), (u32)(at.rows / 64), n), 256, st, (in)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)norms, n_parts, up, x);
         });
     });
+    if (thin) {
+        float* const a_parts = (float*)(ws + (blocks == 1 ? at.gram : at.parts));
+        const auto go = [&](auto r) {
+            constexpr int R = decltype(r)::value;
+            each_matrix([&](u64 m, u32 n) {
+                by_type(g_type, [&](auto tt) {
+                    typedef decltype(tt) T;
+                    launch(thin_first<T, R>, dim3(blocks, 1, n), 512, st, (const typename T::elem*)d_g, (u64)g_stride, (u64)g_step, s, m, (const double*)norms, n_parts, up, x, a_parts);
+                });
+                UpdateOut out = update;
+                out.matrix0 = m;
+                for (u32 i = 0; i < steps; ++i) {
+                    launch(thin_poly<R>, dim3(n), 512, st, (const float*)a_parts, blocks, s.rows, by.gram[i], by.a[i], by.b[i], by.c[i], m, poly);
+                    launch(thin_apply<R>, dim3(blocks, 1, n), 512, st, poly, x, s, by.next[i], i + 1 == steps, out, a_parts);
+                }
+            });
+        };
+        if (few_rows) go(Int<1>());
+        else go(Int<2>());
+        return launched(call, launch);
+    }
     // R = P Q^T for all matrices, summed over all k of the halves; of a symmetric one the tiles on and above the diagonal, in parts where that is a few of them.
     // The kind of tiles and the number of parts by an estimate of the time: rounds over the 256 CUs, of a fixed time and one for each stage of 64 k, in microseconds as measured; parts
     // are written, read and added up at 5 TB/s.

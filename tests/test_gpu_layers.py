@@ -383,6 +383,37 @@ def test_orthogonalize_of_zeros_and_what_is_not_finite():
             assert float((d(out[i]) - want - 2.0 * d(base[i])).norm()) <= e + 4 * U * float(2 * base[i].norm() + want.norm())
 
 
+@pytest.mark.parametrize("count,rows,cols", [(1, 90, 511), (4, 300, 128), (270, 9, 300), (270, 400, 100), (90, 65, 700), (1, 64, 8200), (40, 1100, 33)])
+def test_orthogonalize_of_long_ones(count, rows, cols):
+    """Blocks of one piece and of some, of odd sizes and padded rows, with matrices of zeros and others that are not finite beside them, in place and not."""
+    import paper_2605_01989_amd as dblp
+    g = gen(rows)
+    x = torch.randn(count, rows, cols, generator=g, device="cuda")
+    bad = count > 2
+    if bad:
+        x[0] = 0.0
+        x[1, rows - 1, cols - 1] = float("nan")
+    ws = space(dblp.orthogonalize_workspace(count, rows, cols))
+    for t in TYPES.values():
+        buf = torch.full((count, rows, cols + 3), -77.0, dtype=t, device="cuda")
+        stack, base = buf[:, :, :cols], torch.randn(count, rows, cols, generator=g, device="cuda")
+        stack.copy_(x)
+        start = stack.clone()
+        got = torch.empty(count, rows, cols, device="cuda")
+        dblp.orthogonalize(stack, got, ws, scale=-0.5, base=base, base_scale=0.75, steps=3)
+        if bad:
+            assert torch.equal(got[0], 0.75 * base[0]) and bool(torch.isnan(got[1]).all())
+        for i in {0, 2 * bad, count // 2, count - 1} - {0, 1} if bad else range(count):
+            o, e = ref.orthogonal(d(start[i]), 3)
+            want = -0.5 * o + 0.75 * d(base[i])
+            assert float((d(got[i]) - want).norm()) <= 0.5 * e + 4 * U * float(want.norm() + o.norm()), i
+        apart = torch.empty(count, rows, cols, dtype=t, device="cuda")
+        dblp.orthogonalize(stack, apart, ws, scale=0.3, base=start, steps=2)
+        dblp.orthogonalize(stack, stack, ws, scale=0.3, base=stack, steps=2)
+        assert torch.equal(torch.nan_to_num(stack, nan=5.0), torch.nan_to_num(apart, nan=5.0))
+        assert bool((buf[:, :, cols:] == -77.0).all())
+
+
 def test_orthogonalize_in_place_and_with_other_coefficients():
     import paper_2605_01989_amd as dblp
     g = gen(3)
