@@ -20,12 +20,15 @@ static u32 norm_blocks(u64 values) {
     return (u32)(n < 1 ? 1 : n < NORM_MOST ? n : NORM_MOST);
 }
 
+template <int WAVES>
 __device__ __forceinline__ double block_sum(double v) {
-    __shared__ double sh[4];
+    __shared__ double sh[WAVES];
     for (int d = 32; d; d >>= 1) v += __shfl_down(v, d);
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();
-    return sh[0] + sh[1] + sh[2] + sh[3];
+    v = 0;
+    for (int i = 0; i < WAVES; ++i) v += sh[i];
+    return v;
 }
 
 // Sums of squares, in fp64, where neither a square nor a sum of them leaves the range.  `across` threads, a power of two, take a row, four values each at a time; a
@@ -53,13 +56,14 @@ __global__ __launch_bounds__(256) void norm_parts(const typename T::elem* g, u64
                 for (int e = 0; e < 4; ++e) sum += (double)v[e] * (double)v[e];
             }
         }
-    sum = block_sum(sum);
+    sum = block_sum<4>(sum);
     if (threadIdx.x == 0) parts[matrix * gridDim.x + blockIdx.x] = sum;
 }
 
-// One over the norm; 0 of a matrix of zeros, NaN where a value is not finite.
+// One over the norm; 0 of a matrix of zeros, NaN where a value is not finite.  (n is 256 at most.)
+template <int WAVES>
 __device__ __forceinline__ double one_over_norm(const double* parts, u32 n) {
-    const double sum = block_sum(threadIdx.x < n ? parts[threadIdx.x] : 0.0);
+    const double sum = block_sum<WAVES>(threadIdx.x < n ? parts[threadIdx.x] : 0.0);
     return sum == 0.0 ? 0.0 : sum <= DBL_MAX ? 1.0 / sqrt(sum) : NAN;
 }
 
@@ -106,7 +110,7 @@ __global__ __launch_bounds__(256) void scale_in(const typename T::elem* g, u64 s
         const typename T::elem* const at = g + (u64)(g_row + 16 * i) * stride + g_col;
         if (g_row + 16 * i < g_rows && g_col < g_cols) r[i] = g_col + 4 <= g_cols ? V::load(at) : V::some(at, g_cols - g_col);
     }
-    const double q = one_over_norm(parts + matrix * n_parts, n_parts) * up;
+    const double q = one_over_norm<4>(parts + matrix * n_parts, n_parts) * up;
 #pragma unroll
     for (u32 i = 0; i < 4; ++i) {
         float v[4];
@@ -362,15 +366,9 @@ __global__ __launch_bounds__(512) void small_steps(const typename T::elem* g, u6
     typedef Small<R, N> S;
     __shared__ __attribute__((aligned(16))) uint8_t x[2 * S::X_LOW];
     __shared__ __attribute__((aligned(16))) uint8_t m[2 * S::A_LOW];
-    __shared__ double norms[8];
     const S small;
     const typename S::template Values<T> values(g + (out.matrix0 + blockIdx.x) * step, stride, s, 0);
-    double sum = values.squares();
-    for (int d = 32; d; d >>= 1) sum += __shfl_down(sum, d);
-    if ((threadIdx.x & 63) == 0) norms[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    sum = 0;
-    for (int i = 0; i < 8; ++i) sum += norms[i];
+    const double sum = block_sum<8>(values.squares());
     values.put(x, (sum == 0.0 ? 0.0 : sum <= DBL_MAX ? 1.0 / sqrt(sum) : NAN) * up);
     for (u32 i = 0; i < k.n; ++i) {
         __syncthreads();
@@ -425,7 +423,7 @@ __global__ __launch_bounds__(512) void thin_first(const typename T::elem* g, u64
     __shared__ __attribute__((aligned(16))) uint8_t x[2 * S::X_LOW];
     const S small;
     const u64 matrix = matrix0 + blockIdx.z;
-    const double q = one_over_norm(norms + matrix * n_norms, n_norms) * up;
+    const double q = one_over_norm<8>(norms + matrix * n_norms, n_norms) * up;
     f4 acc[R][2 * R] = {};
     for (u32 col0 = blockIdx.x * 128; col0 < to.stride; col0 += gridDim.x * 128) {
         const typename S::template Values<T> values(g + matrix * step, stride, s, col0);
