@@ -360,21 +360,30 @@ struct Reader {
     }
 };
 
-// Block number b's tile.  Blocks go to the eight dies in turn; each die gets tiles that lie together, rows of tiles in bands of eight, so that its L2 holds
+// This block's number among the launch's tiles of all z.  Blocks go to the eight dies in turn; each die gets tiles, and matrices or parts of k, that lie together, so that its L2 holds
 // what its blocks read at the same time.
-__device__ __forceinline__ void tile_of(u64 b, u64 n, u32 tile_rows, u32 tile_cols, u32& m, u32& c) {
-    const u64 each = n / 8, more = n % 8, die = b % 8;
-    const u64 id = die * each + (die < more ? die : more) + b / 8;
-    const u64 band = id / (8ull * tile_cols), in_band = id % (8ull * tile_cols);
-    const u32 first = (u32)band * 8, high = tile_rows - first < 8 ? tile_rows - first : 8;
-    m = first + (u32)(in_band % high);
-    c = (u32)(in_band / high);
+__device__ __forceinline__ u32 block_by_die() {
+    const u32 n = gridDim.x * gridDim.z, b = blockIdx.z * gridDim.x + blockIdx.x, each = n / 8, more = n % 8, die = b % 8;        // (below 2^31: each_tiles)
+    return die * each + (die < more ? die : more) + b / 8;
+}
+// Tiles go in bands of eight rows of tiles, down and then across.
+__device__ __forceinline__ void tile_of(u64 id, u32 tile_rows, u32 tile_cols, u32& m, u32& c) {
+    u32 band, in_band;
+    if (id >> 32 || tile_cols >> 28) {
+        band = (u32)(id / (8ull * tile_cols));
+        in_band = (u32)(id % (8ull * tile_cols));
+    } else {
+        band = (u32)id / (8 * tile_cols);
+        in_band = (u32)id % (8 * tile_cols);
+    }
+    const u32 first = band * 8, high = tile_rows - first < 8 ? tile_rows - first : 8;
+    m = first + in_band % high;
+    c = in_band / high;
 }
 
 // ... and of a symmetric result, n tiles high and wide, those on and above the diagonal, n (n + 1) / 2.
-__device__ __forceinline__ void upper_tile_of(u64 b, u64 tiles, u32 n, u32& m, u32& c) {
-    const u64 each = tiles / 8, more = tiles % 8, die = b % 8;
-    u32 left = (u32)(die * each + (die < more ? die : more) + b / 8), row = 0;
+__device__ __forceinline__ void upper_tile_of(u64 id, u32 n, u32& m, u32& c) {
+    u32 left = (u32)id, row = 0;
     while (left >= n - row) left -= n - row++;
     m = row;
     c = row + left;
@@ -393,7 +402,7 @@ __device__ __forceinline__ void put_all(const Out& out, u32 matrix, u32 part, u3
 }
 
 // PAIRS: P has rows of 16-bit values an odd number of elements apart, so that no more than every other one begins at a multiple of four bytes, and Q lies by k.  The
-// others do so one element earlier.  Even and odd rows are two matrices (blockIdx.z), each with rows at multiples of four bytes that can be copied; of the shifted one k is one more
+// others do so one element earlier.  Even and odd rows are two matrices , each with rows at multiples of four bytes that can be copied; of the shifted one k is one more
 // than the sum's, its first value, an element of another row, is set to zero, and Q's rows are taken one earlier.
 // WR x WC waves, each 16 NM x 16 NN of the tile.
 template <int WR_, int WC_, int NM_, int NN_, int RING_> struct Waves { static constexpr int WR = WR_, WC = WC_, NM = NM_, NN = NN_, RING = RING_, BM = 16 * NM * WR, BN = 16 * NN * WC, ALL = WR * WC; };
@@ -407,10 +416,12 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
     constexpr u32 KS = FP::KS, STAGE = FP::BYTES + FQ::BYTES, COPIES = FP::COPIES + FQ::COPIES;
     __shared__ __attribute__((aligned(1024))) uint8_t ring[RING * STAGE];
     u32 tm, tn;
-    if (SYMMETRIC) upper_tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, tm, tn);
-    else tile_of(a.tile0 + blockIdx.x, a.tiles, a.tile_rows, a.tile_cols, tm, tn);
+    const u32 id = block_by_die();
+    const u32 z = gridDim.z > 1 ? id / gridDim.x : 0, tile = gridDim.z > 1 ? id % gridDim.x : id;
+    if (SYMMETRIC) upper_tile_of(a.tile0 + tile, a.tile_rows, tm, tn);
+    else tile_of(a.tile0 + tile, a.tile_rows, a.tile_cols, tm, tn);
     const u32 m0 = tm * BM, n0 = tn * BN;
-    const u32 matrix = blockIdx.z / a.parts, part = blockIdx.z % a.parts;
+    const u32 matrix = a.parts > 1 ? z / a.parts : z, part = a.parts > 1 ? z % a.parts : 0;
     const u64 parity = PAIRS ? uniform(matrix) : 0;
     const u32 shift = PAIRS ? ((u32)((uintptr_t)a.P.p >> 1) + (u32)(parity * a.P.stride)) & 1 : 0;
     const u32 rows = PAIRS && parity ? a.odd_rows : a.rows, depth = a.depth + shift;
@@ -771,7 +782,7 @@ static u64 parts_bytes(u64 rows, u64 cols) {
     return one >= PARTS_BYTES / PARTS_MOST ? PARTS_BYTES : one * PARTS_MOST;
 }
 
-// Launches of a product's tiles: at most 2^20 tiles and 2^15 matrices' parts each (a grid's threads stay below 2^32, its z below 2^16).
+// Launches of a product's tiles: at most 2^20 tiles, or 2^16 of 2^15 matrices' parts (a grid's threads along x stay below 2^32, its z below 2^16, its blocks below 2^32).
 template <int BM, int BN, class F>
 static void each_tiles(Product a, u64 matrices, F f, bool symmetric = false) {
     a.tile_cols = (u32)((a.cols + (u64)BN - 1) / BN);
@@ -779,8 +790,8 @@ static void each_tiles(Product a, u64 matrices, F f, bool symmetric = false) {
     a.tiles = symmetric ? (u64)a.tile_rows * (a.tile_rows + 1) / 2 : (u64)a.tile_rows * a.tile_cols;
     for (u64 m = 0; m < matrices; m += 32768 / a.parts) {
         const u64 here = matrices - m < 32768 / a.parts ? matrices - m : 32768 / a.parts;
-        for (a.tile0 = 0; a.tile0 < a.tiles; a.tile0 += 1u << 20)
-            f(a, dim3((u32)(a.tiles - a.tile0 < (1u << 20) ? a.tiles - a.tile0 : 1u << 20), 1, (u32)here * a.parts), m);
+        const u32 z = (u32)here * a.parts, most = z > 1 ? 1u << 16 : 1u << 20;
+        for (a.tile0 = 0; a.tile0 < a.tiles; a.tile0 += most) f(a, dim3((u32)(a.tiles - a.tile0 < most ? a.tiles - a.tile0 : most), 1, z), m);
     }
 }
 
