@@ -136,7 +136,8 @@ struct Staged {
 __device__ __forceinline__ u4v chunk_of(const uint8_t* tile, u32 row, u32 chunk) { return *(const u4v*)(tile + row * 128 + (chunk ^ (row & 7)) * 16); }
 
 // Four waves, two by two, each a quarter of a BM x BN tile: operands of any place and stride.  SUMS: of the first column of tiles, also P's own sums over k.  `out` gets the
-// results, four columns of a row at a time, and what its `get` has found in memory for them; `sums` gets a row's sum.
+// results, four columns of a row at a time, and what its `get` has found in memory for them; `sums` gets a row's sum.  For operands whose rows are so far apart that a tile's
+// offsets pass 31 bits.  Bound by the loads' way through registers: 2048 x 2048 x 2048 of bf16, rows 2^21 elements apart, 39 us (444 TFLOP/s), 31 by ring_products on near ones.
 template <class T, bool P_BY_K, bool Q_BY_K, int BM, int BN, bool SUMS, class Out>
 __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out) {
     typedef typename T::elem elem;
@@ -208,6 +209,9 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out
 //   by k     a row is one k of BT rows, in granules of 16 rows; granule g of k lies at g ^ turn(k), so that the rows of k that one transposing read of four k
 //            takes lie in different banks.  16-bit values are transposed on the way out (ds_read_b64_tr_b16: of 16 lanes with
 //            four values each, lane i gets value i % 4 of lanes i / 4, i / 4 + 4, ...), floats are read one by one.
+// Bound by the matrix instructions and by LDS' reads beside them (the instructions at work 65 % of the time in the largest products), small products by the rounds of tiles.  The largest
+// tile, 256 x 256 of eight waves with 128 x 64 results each, reads 96 KiB of LDS for 32 k, four of 128 x 128 128 KiB; four waves' results do not fit the registers.  8192 x 8192 x 8192 of
+// bf16: 806 us (1.36 PFLOP/s) by rows and rows, 797 by rows and k, 817 by k and k into floats; 4096 x 4096 x 4096 110, 114, 115; the library's 751 to 912 and 94 to 120.
 // ------------------------------------------------------------------------------------------
 #define STAGE_BYTES 128
 
@@ -402,7 +406,7 @@ __device__ __forceinline__ void put_all(const Out& out, u32 matrix, u32 part, u3
 }
 
 // PAIRS: P has rows of 16-bit values an odd number of elements apart, so that no more than every other one begins at a multiple of four bytes, and Q lies by k.  The
-// others do so one element earlier.  Even and odd rows are two matrices , each with rows at multiples of four bytes that can be copied; of the shifted one k is one more
+// others do so one element earlier.  Even and odd rows are two matrices, each with rows at multiples of four bytes that can be copied; of the shifted one k is one more
 // than the sum's, its first value, an element of another row, is set to zero, and Q's rows are taken one earlier.
 // WR x WC waves, each 16 NM x 16 NN of the tile.
 template <int WR_, int WC_, int NM_, int NN_, int RING_> struct Waves { static constexpr int WR = WR_, WC = WC_, NM = NM_, NN = NN_, RING = RING_, BM = 16 * NM * WR, BN = 16 * NN * WC, ALL = WR * WC; };
@@ -664,7 +668,8 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
 
 // ------------------------------------------------------------------------------------------
 // At most 16 rows (tokens that are decoded): the weights are read once, from memory straight into the matrix instructions' registers.  A block makes 16 columns of all rows; its
-// waves share k, 128 bytes of it at a time, and add their sums up in LDS.  Bound by the reading of Q; P comes from the caches.
+// waves share k, 128 bytes of it at a time, and add their sums up in LDS.  Bound by the reading of Q; P comes from the caches.  Of bf16 weights that are not in the caches 16384 x 4096 for
+// one row 27 us (4.9 TB/s), for four 29; 4096 x 1024 for one 4.6, where the launch counts, 7.3 from call to call.
 // ------------------------------------------------------------------------------------------
 #define FEW_WAVES 16
 template <class T, class Out>
@@ -742,7 +747,7 @@ struct PartOut {
     __device__ __forceinline__ void sums(u32, u32 part, u32 m, float s) const { if (row_sums) row_sums[(u64)part * rows + m] = s; }
 };
 
-// Adds the parts up, one after the other, eight of them on their way, and hands the results on: a thread takes four columns.
+// Adds the parts up, one after the other, eight of them on their way, and hands the results on: a thread takes four columns.  Bound by memory: 138 MB to 13 in 25 us (6 TB/s).
 template <class Out>
 __global__ __launch_bounds__(256) void join_parts(PartOut in, Units s, Out out) {
     const u32 parts = in.parts, matrix = blockIdx.z;
