@@ -358,9 +358,9 @@ static void tiles(Launches& launch, hipStream_t stream, Product a, Kind kind, Ou
     else if constexpr (sizeof(typename T::elem) == 2) by_place(Waves<2, 4, 8, 4, 2>());
 }
 
-// Few rows, where a block reads little more of P than of Q, or there are few blocks: with 16 rows of 4096 values and 16384 columns P's reading takes over (34 us, by tiles 25; with
-// 4 rows 25).  In parts that make 512 blocks, of at least two turns of a block's waves each.
-static bool few_rows(u64 rows, u64 cols) { return rows <= 4 || (rows <= 16 && cols <= 8192); }
+// Few rows, where a block reads little more of P than of Q, or there are few blocks: with 16 rows of 4096 16-bit values and 16384 columns P's reading takes over (40 us, by tiles 30; with
+// 4 rows 30 and 30; of floats 84 and 84, with 8 rows 72 and 83).  In parts that make 512 blocks, of at least two turns of a block's waves each.
+static bool few_rows(u64 rows, u64 cols, u32 elem) { return rows <= 4 || (rows <= 16 && (cols <= 8192 || elem == 4)); }
 template <class T, class Out>
 static void few(Launches& launch, hipStream_t stream, Product a, Out out, PartOut parts) {
     constexpr u32 TURN = FEW_WAVES * 128 / sizeof(typename T::elem);
@@ -387,7 +387,7 @@ static void few(Launches& launch, hipStream_t stream, Product a, Out out, PartOu
 template <class T, bool P_BY_K, bool Q_BY_K, bool SUMS, class Out>
 static void products(Launches& launch, hipStream_t stream, Product a, Out out, void* workspace) {
     if constexpr (!P_BY_K && !Q_BY_K) {
-        if (few_rows(a.rows, a.cols)) {
+        if (few_rows(a.rows, a.cols, sizeof(typename T::elem))) {
             const u64 stride = round_up(a.cols, 4);
             return few<T>(launch, stream, a, out, PartOut{(float*)workspace, stride, a.rows * stride, nullptr, a.rows, 1});
         }
