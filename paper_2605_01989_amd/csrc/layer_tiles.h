@@ -435,7 +435,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
     const u32 k_first = part * a.part, k_end = depth - k_first > a.part ? k_first + a.part : depth;
     const u32 stages = (k_end - k_first + KS - 1) / KS;
     const bool summing = SUMS && __builtin_amdgcn_readfirstlane(n0 == 0 && wn == 0);
-    f4 acc[NM][NN] = {}, sum = {};
+    f4 acc[NM][NN] = {}, sum[SUMS ? NM : 1] = {};
     FP fp((const elem*)a.P.p + (PAIRS ? parity * a.P.stride - shift : matrix * a.P.step), PAIRS ? 2 * a.P.stride : a.P.stride, m0, rows, k_first, k_end);
     FQ fq((const elem*)a.Q.p + (PAIRS ? 0 - shift * a.Q.stride : matrix * a.Q.step), a.Q.stride, n0, a.cols, k_first, k_end);
     if (HALVES) {
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
 #pragma unroll
                     for (int i = 0; i < NM; ++i)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) sum = mfma<F32>(in_group * NM / 16 == i ? ones<F32>() : (u4v)(0u), b[i][h], sum);
+                        for (int h = 0; h < 2; ++h) sum[i] = mfma<F32>(ones<F32>(), b[i][h], sum[i]);
                 }
                 arrived_and_barrier<(RING - 1) * COPIES>();
                 copy_all(slot);
@@ -546,14 +546,14 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
             for (int i = 0; i < NM; ++i)
 #pragma unroll
                 for (int j = 0; j < NN; ++j)
-                    for (int e = 0; e < 4; ++e) finite &= fabsf(acc[i][j][e]) <= FLT_MAX;
+                    for (int e = 0; e < 4; ++e) finite &= fabsf(acc[i][j][e]) <= FLT_MAX || m0 + wm + 16 * i + in_group >= rows || n0 + wn + 16 * j + group * 4 + e >= a.cols;
             arrived_and_barrier<0>();
             if (__syncthreads_or(!finite)) {
 #pragma unroll
                 for (int i = 0; i < NM; ++i)
 #pragma unroll
                     for (int j = 0; j < NN; ++j) acc[i][j] = (f4)(0.0f);
-                sum = (f4)(0.0f);
+                for (f4& of : sum) of = (f4)(0.0f);
                 all(Int<1>());
             }
         }
@@ -597,11 +597,11 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 __builtin_amdgcn_sched_barrier(0);
                 c[j] = rq.get(ring, slot1 * STAGE + FP::BYTES, half1, j);
             }
-            // sums over k: products with ones, those of fragment i in rows 16 / NM i and up of one result
+            // sums over k: products with ones, each fragment's by itself (what one row holds must not meet another's, be it times zero)
             if (SUMS && summing) {
                 asm volatile("");                      // (or the compiler computes them everywhere and chooses)
 #pragma unroll
-                for (int i = 0; i < NM; ++i) sum = mfma<T>(in_group * NM / 16 == i ? ones<T>() : (u4v)(0u), b[i], sum);
+                for (int i = 0; i < NM; ++i) sum[i] = mfma<T>(ones<T>(), b[i], sum[i]);
             }
         };
         u32 slot = 0;
@@ -663,7 +663,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
     if (SUMS && summing)
 #pragma unroll
         for (int i = 0; i < NM; ++i)
-            if (group == i * 16 / NM / 4 && m0 + wm + i * 16 + in_group < a.rows) out.sums(matrix, part, m0 + wm + i * 16 + in_group, sum[i * 16 / NM % 4]);
+            if (group == 0 && m0 + wm + i * 16 + in_group < a.rows) out.sums(matrix, part, m0 + wm + i * 16 + in_group, sum[i][0]);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -235,6 +235,38 @@ def test_infinities_stay_in_their_row():
             assert torch.equal(y[~hit], clean[~hit]) and not torch.isfinite(y[hit]).any()
 
 
+@pytest.mark.parametrize("n,inner,outer", [(40, 30, 61), (300, 70, 200), (9000, 100, 130), (1000, 2000, 1001), (700, 1900, 2100), (2500, 4000, 4003)])
+def test_what_is_not_finite_stays_in_its_sum(n, inner, outer):
+    """A bias' gradient is of its own column: not of its neighbours', and not of what lies behind a row's end."""
+    import paper_2605_01989_amd as dblp
+    for t in TYPES.values():
+        g = gen(outer)
+        buf = torch.full((n, outer + 13), float("nan"), dtype=t, device="cuda")
+        dy, x = buf[:, :outer], torch.randn(n, inner, generator=g, device="cuda").to(t)
+        dy.copy_(torch.randn(n, outer, generator=g, device="cuda"))
+        clean = torch.zeros(n, outer + 13, dtype=t, device="cuda")[:, :outer]
+        clean.copy_(dy)
+        ws = space(dblp.linear_workspace(n, inner, outer))
+        dw, want = torch.empty(outer, inner, device="cuda"), torch.empty(outer, inner, device="cuda")
+        db, sums = torch.empty(outer, device="cuda"), torch.empty(outer, device="cuda")
+        dblp.linear_grad_weight(clean, x, want, ws, bias_grad=sums)
+        dblp.linear_grad_weight(dy, x, dw, ws, bias_grad=db)
+        assert torch.equal(db, sums) and torch.equal(dw, want)
+        off = (d(db) - d(dy).sum(0)).abs()
+        assert bool((off <= 2 * (n + 4) * U * d(dy).abs().sum(0)).all())
+        dy[n // 2, 17], dy[n - 1, outer - 2] = float("inf"), float("nan")
+        dblp.linear_grad_weight(dy, x, dw, ws, bias_grad=db)
+        rest = torch.ones(outer, dtype=torch.bool, device="cuda")
+        rest[17] = rest[outer - 2] = False
+        assert torch.equal(db[rest], sums[rest]) and float(db[17]) == math.inf and math.isnan(float(db[outer - 2]))
+        if t != torch.float32:
+            assert torch.equal(dw[rest], want[rest])
+        else:                                      # a large tile of floats that holds such a value is made by other instructions: as near, not the same bits
+            keep = rest.cpu()
+            mine, other = d(dy).T[keep], d(x)
+            assert bool(((d(dw)[keep] - mine @ other).abs() <= 2 * (n + 4) * U * (mine.abs() @ other.abs())).all())
+
+
 def test_in_place():
     import paper_2605_01989_amd as dblp
     g = gen(5)
@@ -381,6 +413,49 @@ def test_orthogonalize_of_zeros_and_what_is_not_finite():
         for i in (0, 4):
             want, e = ref.orthogonal(d(x[i]), steps)
             assert float((d(out[i]) - want - 2.0 * d(base[i])).norm()) <= e + 4 * U * float(2 * base[i].norm() + want.norm())
+
+
+@pytest.mark.parametrize("n,inner,outer", [(1100, 1301, 1203), (2200, 333, 1601), (4099, 65, 2051), (90, 4001, 903)])
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
+def test_odd_rows_give_what_even_ones_give(t, n, inner, outer):
+    """Values at odd addresses and strides, NaN all around them and in the workspace, bit for bit as from rows at multiples of 16 bytes (the input's
+    gradient, whose sum begins one k earlier in odd rows, where dy's are even)."""
+    import paper_2605_01989_amd as dblp
+    g = gen(n)
+
+    def both(rows, cols):
+        values = torch.randn(rows, cols, generator=g, device="cuda").to(t)
+        got = []
+        for stride, shift in ((cols + cols % 2 + 1, 1), ((cols + 7) // 8 * 8, 0)):
+            buf = torch.full((rows * stride + 8 + shift,), float("nan"), dtype=t, device="cuda")
+            got.append(buf[shift:shift + rows * stride].view(rows, stride)[:, :cols])
+            got[-1].copy_(values)
+        return got
+
+    x, w, dy = both(n, inner), both(outer, inner), both(n, outer)
+    bias = torch.randn(outer, generator=g, device="cuda")
+    ws = torch.full((dblp.linear_workspace(n, inner, outer),), 255, dtype=torch.uint8, device="cuda")
+    got = []
+    for k in (0, 1):
+        y, dx, dw, db = (torch.full(size, -77.0, device="cuda") for size in ((n, outer), (n, inner), (outer, inner), (outer,)))
+        dblp.linear(x[k], w[k], y, ws, bias=bias, activation="relu")
+        dblp.linear_grad_input(dy[1], w[k], dx, ws)
+        dblp.linear_grad_weight(dy[k], x[k], dw, ws, bias_grad=db)
+        again = torch.empty_like(dw)
+        ws.fill_(7 * k)
+        dblp.linear_grad_weight(dy[k], x[1 - k], again, ws)
+        got.append((y, dx, dw, db))
+        assert torch.equal(again, dw)
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    for k in (0, 1):
+        dx = torch.empty(n, inner, device="cuda")
+        dblp.linear_grad_input(dy[0], w[k], dx, ws)
+        off = (d(dx) - d(dy[1]) @ d(w[1])).abs()
+        assert bool((off <= 2 * (outer + 4) * U * (d(dy[1]).abs() @ d(w[1]).abs())).all())
+    want = (d(dy[1]).T @ d(x[1]))
+    off = (d(got[0][2]) - want).abs()
+    assert bool((off <= 2 * (n + 4) * U * (d(dy[1]).abs().T @ d(x[1]).abs())).all())
 
 
 @pytest.mark.parametrize("count,rows,cols", [(1, 90, 511), (4, 300, 128), (270, 9, 300), (270, 400, 100), (90, 65, 700), (1, 64, 8200), (40, 1100, 33)])
