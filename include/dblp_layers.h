@@ -68,7 +68,8 @@ int dblp_linear_grad_weight(int device, void* stream, uint64_t n_tokens, uint32_
                             uint64_t dy_stride, const void* d_x, uint64_t x_stride, int type, const float* d_base,
                             uint64_t base_stride, float* d_dw, uint64_t dw_stride, const float* d_bias_base, float* d_dbias,
                             void* d_workspace, uint64_t workspace_bytes);
-/* Bytes of the workspace of these three; 0 if an argument is out of range. */
+/* Bytes of the workspace of these three; 0 if an argument is out of range.  Up to 1 GB of it is for operands of 16-bit values whose rows do not begin
+ * at multiples of four bytes, which are laid out anew there. */
 uint64_t dblp_linear_workspace(uint64_t n_tokens, uint32_t in, uint32_t out);
 
 /* dz = dy act'(z), for a layer whose activation is not followed by a product; dy, z and dz of one type.  In place: dz may

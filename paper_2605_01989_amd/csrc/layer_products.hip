@@ -280,16 +280,27 @@ __global__ __launch_bounds__(256) void activation_units(Units s, int act, const 
 static bool bad_act(int act) { return act < DBLP_ACT_NONE || act > DBLP_ACT_SILU; }
 static bool bad_sizes(u64 tokens, u64 in, u64 out) { return tokens >= COUNT_LIMIT || in >= COUNT_LIMIT || out >= COUNT_LIMIT; }
 
-extern "C" uint64_t dblp_linear_workspace(uint64_t n_tokens, uint32_t in, uint32_t out) {
-    if (bad_sizes(n_tokens, in, out)) return 0;
+// A workspace: parts of a product and of a bias' gradient, then room for two operands with rows at multiples of 16 bytes, up to so many bytes.
+#define ALIGNED_BYTES (1ull << 30)
+static u64 aligned_stride(u64 cols) { return round_up(cols, 8); }
+static u64 aligned_bytes(u64 lines, u64 cols) {
+    const u64 stride = aligned_stride(cols);                                         // (lines stride 2 <= 2^63)
+    return lines * stride * 2 < ALIGNED_BYTES ? round_up(lines * stride * 2, 256) : ALIGNED_BYTES;
+}
+static u64 aligned_at(u64 n_tokens, u64 in, u64 out) {
     u64 most = parts_bytes(n_tokens, out);
     for (const u64 other : {parts_bytes(n_tokens, in), parts_bytes(out, in)}) if (other > most) most = other;
-    return 256 + most + round_up((u64)PARTS_MOST * out * 4, 256);
+    return 256 + round_up(most, 256) + round_up((u64)PARTS_MOST * out * 4, 256);
+}
+extern "C" uint64_t dblp_linear_workspace(uint64_t n_tokens, uint32_t in, uint32_t out) {
+    if (bad_sizes(n_tokens, in, out)) return 0;
+    const u64 w = aligned_bytes(out, in), dy = aligned_bytes(n_tokens, out), two = aligned_bytes(n_tokens, in) + (w > dy ? w : dy);
+    return aligned_at(n_tokens, in, out) + (two < ALIGNED_BYTES ? two : ALIGNED_BYTES);
 }
 
 // A way to make a product: tiles of one kind, the sum over k in `parts` parts.
 enum Kind { TILES_64, TILES_128, TILES_256, KINDS };
-struct Way { Kind kind; u32 parts, part; };
+struct Way { Kind kind; u32 parts, part; double us; };
 
 // Chosen by an estimate of the time, in microseconds: rounds of tiles over the 256 CUs, each a fixed time and one for each stage of 128 bytes of k, which is longer with more blocks on a CU
 // (of the largest tiles, with more CUs at work); parts are written, read and added up at 5 TB/s.  As measured with each kind alone over 27 sizes; the choice is within 15 % of the best
@@ -297,8 +308,8 @@ struct Way { Kind kind; u32 parts, part; };
 static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
     static const struct { u32 tile, blocks; double fixed, stage[2][3]; } K[KINDS] = {
         {64, 3, 3.5, {{0.28, 0.40, 0.50}, {0.65, 0.90, 1.10}}}, {128, 2, 5.0, {{0.64, 0.98, 0}, {1.85, 2.65, 0}}}, {256, 1, 10.0, {{1.15, 0, 0}, {0, 0, 0}}}};
-    Way best = {TILES_64, 1, 0};
-    double least = 1e30;
+    Way best = {TILES_64, 1, 0, 0};
+    double& least = best.us = 1e30;
     const u64 ks = 128 / elem, stages = (depth + ks - 1) / ks, bytes = rows * round_up(cols, 4) * 4;
     for (int i = 0; i < KINDS; ++i) {
         if (i == TILES_256 && elem == 4) continue;
@@ -311,8 +322,7 @@ static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
             const double stage = K[i].stage[elem == 4][held - 1] + (i == TILES_256 ? 0.4 * fmin(1.0, blocks / 256.0) : 0.0);
             const double t = rounds * (K[i].fixed + each * stage) + (p > 1 ? 3.0 + p * bytes * 2 / 5e6 : 0.0);
             if (t < least) {
-                least = t;
-                best = {(Kind)i, (u32)p, (u32)(each * ks)};
+                best = {(Kind)i, (u32)p, (u32)(each * ks), t};
             }
         }
     }
@@ -384,16 +394,53 @@ static void few(Launches& launch, hipStream_t stream, Product a, Out out, PartOu
     if (a.parts > 1) each_launch<4>(a.rows, a.cols, [&](Units s) { launch(join_parts<Out>, dim3(blocks_of(s.n, 256)), 256, stream, parts, s, out); });
 }
 
+// Rows of 16-bit values at multiples of 16 bytes: a thread writes eight, those past a row's end anything.  Bound by memory.
+__global__ __launch_bounds__(256) void align_units(Units s, const __bf16* from, u64 from_stride, __bf16* to, u64 to_stride) {
+    typedef Vec<BF16, 8> V;                                                          // (either type's: bits)
+    const u32 u = blockIdx.x * 256 + threadIdx.x;
+    if (u >= s.n) return;
+    const u32 row = s.per_row.of(u), c = (u - row * s.per_row.d) * 8;
+    const u64 r = s.row0 + row;
+    if (c < s.cols) V::store(to + r * to_stride + c, settle_cols<V, 8, false>(load_cols<V, 8, false>(from + r * from_stride, c, s.cols), c, s.cols));
+}
+
+// Operands that cannot be copied to LDS as they lie go there through registers, or are laid out anew in the workspace where that takes less time: the way through registers adds 0.3
+// to 1.4 times the product's time where both lie by rows, about 2 times where one and 1 to 4 times where both lie by k, and laying them out reads and writes them once.  P by rows with Q by k
+// stays: its even and odd rows are two matrices.  Through registers and laid out, in us: 8192 x 4097 x 4097 751 and 353, its input's gradient 878 and 326, its weight's 802 and 394;
+// 1695 x 3893 x 1167 66 (and by the rule so, 52 of operands at multiples of 16 bytes), 85 and 40, 160 and 47; 20000 x 129 x 129's weight's 19 and 24, which the rule has wrong.
+template <class T, bool P_BY_K, bool Q_BY_K>
+static void align(Launches& launch, hipStream_t stream, Product& a, void* aligned) {
+    constexpr double ADDED = P_BY_K ? 2.0 : Q_BY_K ? 1.2 : 0.5;
+    struct { Operand* of; u64 lines, cols; } odd[2];
+    u32 n = 0;
+    if (!copied<T>(a.P) && (P_BY_K || !Q_BY_K)) odd[n++] = {&a.P, P_BY_K ? a.depth : a.rows, P_BY_K ? a.rows : a.depth};
+    if (!copied<T>(a.Q)) odd[n++] = {&a.Q, Q_BY_K ? a.depth : a.cols, Q_BY_K ? a.cols : a.depth};
+    if (n == 0 || a.rows == 0 || a.cols == 0 || a.depth == 0) return;
+    u64 bytes = 0;
+    for (u32 i = 0; i < n; ++i) bytes += aligned_bytes(odd[i].lines, odd[i].cols);
+    if (bytes >= ALIGNED_BYTES || way_of(a.rows, a.cols, a.depth, sizeof(typename T::elem)).us * ADDED < 3.0 * n + bytes * 2 / 5e6) return;
+    uint8_t* to = (uint8_t*)aligned;
+    for (u32 i = 0; i < n; ++i) {
+        const u64 stride = aligned_stride(odd[i].cols), from_stride = odd[i].of->stride;
+        const __bf16* const from = (const __bf16*)odd[i].of->p;
+        each_launch<8>(odd[i].lines, (u32)odd[i].cols, [&](Units s) { launch(align_units, dim3(blocks_of(s.n, 256)), 256, stream, s, from, from_stride, (__bf16*)to, stride); });
+        odd[i].of->p = to;
+        odd[i].of->stride = stride;
+        to += aligned_bytes(odd[i].lines, odd[i].cols);
+    }
+}
+
 template <class T, bool P_BY_K, bool Q_BY_K, bool SUMS, class Out>
-static void products(Launches& launch, hipStream_t stream, Product a, Out out, void* workspace) {
+static void products(Launches& launch, hipStream_t stream, Product a, Out out, void* workspace, void* aligned) {
     if constexpr (!P_BY_K && !Q_BY_K) {
         if (few_rows(a.rows, a.cols, sizeof(typename T::elem))) {
             const u64 stride = round_up(a.cols, 4);
             return few<T>(launch, stream, a, out, PartOut{(float*)workspace, stride, a.rows * stride, nullptr, a.rows, 1});
         }
     }
+    if constexpr (sizeof(typename T::elem) == 2) align<T, P_BY_K, Q_BY_K>(launch, stream, a, aligned);
     Way w = way_of(a.rows, a.cols, a.depth + (in_pairs<T, P_BY_K, Q_BY_K>(a) ? 1 : 0), sizeof(typename T::elem));
-    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0};
+    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0, 0};
     a.parts = w.parts;
     a.part = w.parts > 1 ? w.part : (u32)round_up(a.depth ? a.depth : 1, 64);
     PartOut parts = {(float*)workspace, round_up(a.cols, 4), 0, nullptr, a.rows, a.parts};
@@ -447,7 +494,7 @@ extern "C" int dblp_linear(int device, void* stream, uint64_t n_tokens, uint32_t
     Launches launch;
     const LayerOut o = {out_type, activation, bias_type, d_bias, {(void*)d_residual, residual_stride}, {d_y, y_stride}, {d_z, z_stride}};
     by_type(type, [&](auto tt) {
-        products<decltype(tt), false, false, false>(launch, (hipStream_t)stream, Product{{d_x, x_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, out, in}, o, d_workspace);
+        products<decltype(tt), false, false, false>(launch, (hipStream_t)stream, Product{{d_x, x_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, out, in}, o, d_workspace, (uint8_t*)d_workspace + aligned_at(n_tokens, in, out));
     });
     return launched(call, launch);
 }
@@ -474,7 +521,7 @@ extern "C" int dblp_linear_grad_input(int device, void* stream, uint64_t n_token
     Launches launch;
     const GateOut o = {out_type, activation, {(void*)d_z, z_stride}, {(void*)d_base, base_stride}, {d_dx, dx_stride}};
     by_type(type, [&](auto tt) {
-        products<decltype(tt), false, true, false>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, in, out}, o, d_workspace);
+        products<decltype(tt), false, true, false>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_w, w_stride, 0}, (u32)n_tokens, in, out}, o, d_workspace, (uint8_t*)d_workspace + aligned_at(n_tokens, in, out));
     });
     return launched(call, launch);
 }
@@ -500,7 +547,7 @@ extern "C" int dblp_linear_grad_weight(int device, void* stream, uint64_t n_toke
     Launches launch;
     const WeightOut o = {d_base, base_stride, d_dw, dw_stride, d_bias_base, d_dbias};
     by_type(type, [&](auto tt) {
-        products<decltype(tt), true, true, true>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_x, x_stride, 0}, out, in, (u32)n_tokens}, o, d_workspace);
+        products<decltype(tt), true, true, true>(launch, (hipStream_t)stream, Product{{d_dy, dy_stride, 0}, {d_x, x_stride, 0}, out, in, (u32)n_tokens}, o, d_workspace, (uint8_t*)d_workspace + aligned_at(n_tokens, in, out));
     });
     return launched(call, launch);
 }
