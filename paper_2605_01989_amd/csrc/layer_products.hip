@@ -300,7 +300,7 @@ extern "C" uint64_t dblp_linear_workspace(uint64_t n_tokens, uint32_t in, uint32
 
 // A way to make a product: tiles of one kind, the sum over k in `parts` parts.
 enum Kind { TILES_64, TILES_128, TILES_256, KINDS };
-struct Way { Kind kind; u32 parts, part; double us; };
+struct Way { Kind kind; u32 parts, part; double us, stages_us; };     // (stages_us: of it, without what each round and the parts' sum take)
 
 // Chosen by an estimate of the time, in microseconds: rounds of tiles over the 256 CUs, each a fixed time and one for each stage of 128 bytes of k, which is longer with more blocks on a CU
 // (of the largest tiles, with more CUs at work); parts are written, read and added up at 5 TB/s.  As measured with each kind alone over 27 sizes; the choice is within 15 % of the best
@@ -308,7 +308,7 @@ struct Way { Kind kind; u32 parts, part; double us; };
 static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
     static const struct { u32 tile, blocks; double fixed, stage[2][3]; } K[KINDS] = {
         {64, 3, 3.5, {{0.28, 0.40, 0.50}, {0.65, 0.90, 1.10}}}, {128, 2, 5.0, {{0.64, 0.98, 0}, {1.85, 2.65, 0}}}, {256, 1, 10.0, {{1.15, 0, 0}, {0, 0, 0}}}};
-    Way best = {TILES_64, 1, 0, 0};
+    Way best = {TILES_64, 1, 0, 0, 0};
     double& least = best.us = 1e30;
     const u64 ks = 128 / elem, stages = (depth + ks - 1) / ks, bytes = rows * round_up(cols, 4) * 4;
     for (int i = 0; i < KINDS; ++i) {
@@ -322,7 +322,7 @@ static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
             const double stage = K[i].stage[elem == 4][held - 1] + (i == TILES_256 ? 0.4 * fmin(1.0, blocks / 256.0) : 0.0);
             const double t = rounds * (K[i].fixed + each * stage) + (p > 1 ? 3.0 + p * bytes * 2 / 5e6 : 0.0);
             if (t < least) {
-                best = {(Kind)i, (u32)p, (u32)(each * ks), t};
+                best = {(Kind)i, (u32)p, (u32)(each * ks), t, rounds * each * stage};
             }
         }
     }
@@ -404,21 +404,21 @@ __global__ __launch_bounds__(256) void align_units(Units s, const __bf16* from, 
     if (c < s.cols) V::store(to + r * to_stride + c, settle_cols<V, 8, false>(load_cols<V, 8, false>(from + r * from_stride, c, s.cols), c, s.cols));
 }
 
-// Operands that cannot be copied to LDS as they lie go there through registers, or are laid out anew in the workspace where that takes less time: the way through registers adds 0.3
-// to 1.4 times the product's time where both lie by rows, about 2 times where one and 1 to 4 times where both lie by k, and laying them out reads and writes them once.  P by rows with Q by k
-// stays: its even and odd rows are two matrices.  Through registers and laid out, in us: 8192 x 4097 x 4097 751 and 353, its input's gradient 878 and 326, its weight's 802 and 394;
-// 1695 x 3893 x 1167 66 (and by the rule so, 52 of operands at multiples of 16 bytes), 85 and 40, 160 and 47; 20000 x 129 x 129's weight's 19 and 24, which the rule has wrong.
+// Operands that cannot be copied to LDS as they lie go there through registers, or are laid out anew in the workspace where that takes less time: the way through registers adds 0.5
+// to 1.4 times the stages' time where both lie by rows, 1.8 to 4 times where one and 1.2 to 5 times where both lie by k (and are odd), and laying out is a launch and reads and writes them.
+// P by rows with Q by k stays: its even and odd rows are two matrices.  Through registers and laid out, in us: 8192 x 4097 x 4097 751 and 353, its input's gradient 878 and 326, its
+// weight's 802 and 394; the gradients of 1695 x 3893 x 1167 85 and 40, 160 and 47; of 20000 x 129 x 129 the weight's 19 and 24, by the rule 19.
 template <class T, bool P_BY_K, bool Q_BY_K>
 static void align(Launches& launch, hipStream_t stream, Product& a, void* aligned) {
-    constexpr double ADDED = P_BY_K ? 2.0 : Q_BY_K ? 1.2 : 0.5;
     struct { Operand* of; u64 lines, cols; } odd[2];
     u32 n = 0;
     if (!copied<T>(a.P) && (P_BY_K || !Q_BY_K)) odd[n++] = {&a.P, P_BY_K ? a.depth : a.rows, P_BY_K ? a.rows : a.depth};
     if (!copied<T>(a.Q)) odd[n++] = {&a.Q, Q_BY_K ? a.depth : a.cols, Q_BY_K ? a.cols : a.depth};
     if (n == 0 || a.rows == 0 || a.cols == 0 || a.depth == 0) return;
+    const double added = P_BY_K ? (n == 2 ? 3.0 : 1.0) : Q_BY_K ? 1.9 : 0.7;
     u64 bytes = 0;
     for (u32 i = 0; i < n; ++i) bytes += aligned_bytes(odd[i].lines, odd[i].cols);
-    if (bytes >= ALIGNED_BYTES || way_of(a.rows, a.cols, a.depth, sizeof(typename T::elem)).us * ADDED < 3.0 * n + bytes * 2 / 5e6) return;
+    if (bytes >= ALIGNED_BYTES || way_of(a.rows, a.cols, a.depth, sizeof(typename T::elem)).stages_us * added < 2.7 * n + bytes * 2 / 5e6) return;
     uint8_t* to = (uint8_t*)aligned;
     for (u32 i = 0; i < n; ++i) {
         const u64 stride = aligned_stride(odd[i].cols), from_stride = odd[i].of->stride;
@@ -440,7 +440,7 @@ static void products(Launches& launch, hipStream_t stream, Product a, Out out, v
     }
     if constexpr (sizeof(typename T::elem) == 2) align<T, P_BY_K, Q_BY_K>(launch, stream, a, aligned);
     Way w = way_of(a.rows, a.cols, a.depth + (in_pairs<T, P_BY_K, Q_BY_K>(a) ? 1 : 0), sizeof(typename T::elem));
-    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0, 0};
+    if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0, 0, 0};
     a.parts = w.parts;
     a.part = w.parts > 1 ? w.part : (u32)round_up(a.depth ? a.depth : 1, 64);
     PartOut parts = {(float*)workspace, round_up(a.cols, 4), 0, nullptr, a.rows, a.parts};
