@@ -577,6 +577,60 @@ def test_recorded_calls_give_what_eager_ones_give():
         assert all(torch.equal(a, b) for a, b in zip(eager[i], (y, z, dx, dw, db, params)))
 
 
+def test_recorded_calls_of_odd_rows():
+    """Two graphs with one workspace, in which each lays its operands out, replayed in turn on new values, with eager calls between them."""
+    import paper_2605_01989_amd as dblp
+    n, inner, outer = 1300, 1301, 1203
+    g = gen(31)
+    x, w, dy = (torch.randn(*s, generator=g, device="cuda").to(torch.float16) for s in ((n, inner), (outer, inner), (n, outer)))
+    ws = space(max(dblp.linear_workspace(n, inner, outer), dblp.orthogonalize_workspace(9, 100, inner)))
+    y, dx, dw, db = (torch.empty(*s, device="cuda") for s in ((n, outer), (n, inner), (outer, inner), (outer,)))
+    rows = torch.empty(9, 100, inner, device="cuda")
+
+    def forward():
+        dblp.linear(x, w, y, ws, activation="gelu")
+        dblp.linear_grad_input(dy, w, dx, ws)
+
+    def back():
+        dblp.linear_grad_weight(dy, x, dw, ws, bias_grad=db)
+        dblp.orthogonalize(dw[:900].view(9, 100, inner), rows, ws, steps=2)
+    graphs = []
+    torch.cuda.synchronize()
+    for f in (forward, back):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            f()
+        graphs.append(graph)
+    for i in range(3):
+        x.copy_(torch.randn(n, inner, generator=gen(i), device="cuda"))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        replayed = [v.clone() for v in (y, dx, dw, db, rows)]
+        for v in (y, dx, dw, db, rows):
+            v.fill_(-77.0)
+        forward(), back()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (y, dx, dw, db, rows)))
+
+
+def test_odd_rows_far_apart():
+    import paper_2605_01989_amd as dblp
+    n, inner, outer, far = 600, 701, 301, (1 << 22) + 1
+    g = gen(8)
+    t = torch.bfloat16
+    x, w, dy = (torch.randn(*s, generator=g, device="cuda").to(t) for s in ((n, inner), (outer, inner), (n, outer)))
+    buf = torch.empty(n * far, dtype=t, device="cuda")
+    ws = space(dblp.linear_workspace(n, inner, outer))
+    y, dw, dx = (torch.empty(*s, device="cuda") for s in ((n, outer), (outer, inner), (n, inner)))
+    fx = buf.as_strided((n, inner), (far, 1)).copy_(x)
+    fdy = buf[4096:].as_strided((n, outer), (far, 1)).copy_(dy)
+    dblp.linear(fx, w, y, ws)
+    dblp.linear_grad_weight(fdy, fx, dw, ws)
+    dblp.linear_grad_input(fdy, w, dx, ws)
+    for got, a, b in ((y, d(x), d(w).T), (dw, d(dy).T, d(x)), (dx, d(dy), d(w))):
+        assert bool(((d(got) - a @ b).abs() <= 2 * (a.shape[1] + 4) * U * (a.abs() @ b.abs())).all())
+
+
 def test_offsets_past_32_bits():
     """Rows far enough apart that a row's place passes 2^32 elements."""
     import paper_2605_01989_amd as dblp
