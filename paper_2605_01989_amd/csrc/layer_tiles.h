@@ -220,9 +220,10 @@ __device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_rea
 #define PAST_ALL 0x80000000u                     // an offset that no buffer here reaches: a copy of it writes zeros
 
 // 64 lanes' 16 bytes at `offset` of a buffer to 1024 bytes of LDS at `to`.  No register is written, so nothing can be overwritten by it, and the compiler waits
-// for it nowhere: by a builtin it would before each read of LDS.  m0 is nobody's else in these kernels.
+// for it nowhere: by a builtin it would before each read of LDS.  Nor does it look into these lines for the wait states that a copy needs behind a write of m0, one, and
+// behind a vector instruction's write of a register of `from`, five, of which the write of m0 is one.
 __device__ __forceinline__ void copy_to_lds(rsrc_t from, u32 offset, u32 to) {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "m0");
 }
 template <int N> __device__ __forceinline__ void arrived_and_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
