@@ -439,10 +439,11 @@ static void products(Launches& launch, hipStream_t stream, Product a, Out out, v
         }
     }
     if constexpr (sizeof(typename T::elem) == 2) align<T, P_BY_K, Q_BY_K>(launch, stream, a, aligned);
-    Way w = way_of(a.rows, a.cols, a.depth + (in_pairs<T, P_BY_K, Q_BY_K>(a) ? 1 : 0), sizeof(typename T::elem));
+    const u32 depth = a.depth + (in_pairs<T, P_BY_K, Q_BY_K>(a) ? 1 : 0);             // (of the longer of two sums: what a part or all parts have to cover)
+    Way w = way_of(a.rows, a.cols, depth, sizeof(typename T::elem));
     if (!in_reach<T>(a.P) || !in_reach<T>(a.Q)) w = {TILES_64, 1, 0, 0, 0};
     a.parts = w.parts;
-    a.part = w.parts > 1 ? w.part : (u32)round_up(a.depth ? a.depth : 1, 64);
+    a.part = w.parts > 1 ? w.part : (u32)round_up(depth ? depth : 1, 64);
     PartOut parts = {(float*)workspace, round_up(a.cols, 4), 0, nullptr, a.rows, a.parts};
     parts.step = a.rows * parts.stride;
     bool row_sums = false;

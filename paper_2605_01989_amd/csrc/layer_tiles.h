@@ -408,7 +408,7 @@ __device__ __forceinline__ void put_all(const Out& out, u32 matrix, u32 part, u3
 
 // PAIRS: P has rows of 16-bit values an odd number of elements apart, so that no more than every other one begins at a multiple of four bytes, and Q lies by k.  The
 // others do so one element earlier.  Even and odd rows are two matrices, each with rows at multiples of four bytes that can be copied; of the shifted one k is one more
-// than the sum's, its first value, an element of another row, is set to zero, and Q's rows are taken one earlier.
+// than the sum's, its first value, an element of another row, is set to zero, and Q's rows are taken one earlier: the parts have to cover that one as well.
 // WR x WC waves, each 16 NM x 16 NN of the tile.
 template <int WR_, int WC_, int NM_, int NN_, int RING_> struct Waves { static constexpr int WR = WR_, WC = WC_, NM = NM_, NN = NN_, RING = RING_, BM = 16 * NM * WR, BN = 16 * NN * WC, ALL = WR * WC; };
 
