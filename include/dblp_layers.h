@@ -16,7 +16,7 @@
  * place" says so.  Every result is a function of the arguments alone: no floating-point atomics, sums cut by the sizes alone.
  * Rows whose address and stride are multiples of 16 bytes are fastest.
  *
- * Products are summed in fp32 (of 16-bit values each product is exact, of fp32 values it is within 2^-24 of itself), everything behind them is computed in fp32, and a result
+ * Products are summed in fp32 (of 16-bit values each product is exact, of fp32 values it is within 2^-23 of itself), everything behind them is computed in fp32, and a result
  * is rounded once, to nearest even, when it is stored.  NaN and infinities go through the formulas.
  * Limits: tokens, columns and rows below 2^31, those of dblp_orthogonalize below 2^24.  Zero tokens, columns or rows are allowed: a sum of nothing is zero.
  * A workspace is DEVICE memory of the size that dblp_*_workspace gives, 256-byte aligned, of any contents; it is free

@@ -35,12 +35,13 @@ template <> __device__ __forceinline__ u4v ones<BF16>() { return (u4v)(0x3F803F8
 template <> __device__ __forceinline__ u4v ones<F16>() { return (u4v)(0x3C003C00u); }
 template <> __device__ __forceinline__ u4v ones<F32>() { return (u4v)(0x3F800000u); }
 
-// Floats as sums of three bf16 values: the upper half of the bits, rounded, that of what is left, and the rest, which has eight bits at most.  A product of two such sums is taken as the
-// six of its nine products that are above 2^-24 of it, each exact, on units of sixteen times the rate: what is left out is no more than the rounding of a product to fp32.  Of values that
-// are not finite, or whose upper half is rounded to infinity, it is NaN.  (The bits' arithmetic runs at the full rate, conversions do not.)
+// Floats as sums of three bf16 values: the upper half of the bits, rounded, that of what is left, cut off, and the rest, which has eight bits at most.  A product of two such sums is taken as
+// the six of its nine products that are above 2^-24 of it, each exact, on units of sixteen times the rate.  With |x| in 1..2 what is left of it is at most 2^-8 and the rest below 2^-16:
+// middle by rest, twice, and rest by rest are below 2^-23 of the product, one step of fp32.  Of values that are not finite, or whose upper half is rounded to infinity, it is NaN.  Below
+// 2^-110 the rest may have bits below 2^-133, where bf16 ends: `cut` gets them, in its lower half.  (The bits' arithmetic runs at the full rate, conversions do not.)
 struct Thirds { u4v high, middle, low; };
 __device__ __forceinline__ u32 upper_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }       // of b, of a
-__device__ __forceinline__ Thirds thirds_of(u4v a, u4v b) {
+__device__ __forceinline__ Thirds thirds_of(u4v a, u4v b, u32& cut) {
     const u32 x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     u32 h[8], m[8], l[8];
 #pragma unroll
@@ -51,6 +52,9 @@ __device__ __forceinline__ Thirds thirds_of(u4v a, u4v b) {
         l[i] = __builtin_bit_cast(u32, r - __builtin_bit_cast(float, m[i]));
     }
     const auto pack = [](const u32 (&v)[8]) { return (u4v){upper_halves(v[0], v[1]), upper_halves(v[2], v[3]), upper_halves(v[4], v[5]), upper_halves(v[6], v[7])}; };
+    // (assembly that the values go through: the compiler would keep them in registers until it comes to `cut`)
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) asm("v_or3_b32 %0, %1, %2, %0" : "+v"(cut), "+v"(l[i]), "+v"(l[i + 1]));
     return {pack(h), pack(m), pack(l)};
 }
 // For several b, whose sums then need not wait for each other.
@@ -476,14 +480,16 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
         fp.trim(ring + slot * STAGE, end);
         fq.trim(ring + slot * STAGE + FP::BYTES, end);
     };
-    // Floats in thirds: a stage is one step of 32 k, of which a lane holds chunks `group` and 4 + group.  Bound by the making of the thirds, 6.5 instructions a value and wave.  A tile with a
-    // result that is not finite is made again of floats.  4096 x 4096 x 4096: 685 us (200 TFLOP/s), of floats 1050 and by the library 915.
+    // Floats in thirds: a stage is one step of 32 k, of which a lane holds chunks `group` and 4 + group.  Bound by the making of the thirds, seven instructions a value and wave.  A tile is
+    // made again of floats where a result is not finite or an operand of its own results is no sum of three: 4096 x 4096 x 4096: 738 us (186 TFLOP/s), 1.5 % of it for the looking; 1770 where all are
+    // made again, of floats alone 1050, by the library 920.
     constexpr bool THIRDS = sizeof(elem) == 4 && NM * NN == 16;
     if constexpr (THIRDS) {
         const auto all = [&](auto plain) {
             constexpr bool PLAIN = decltype(plain)::value;
             FP p = fp;
             FQ q = fq;
+            u32 cut_p[NM] = {}, cut_q[NN] = {};
             const auto copy_all = [&](u32 to) {
 #pragma unroll
                 for (u32 e = 0; e < FP::COPIES; ++e) p.copy(e, ring_at + to * STAGE);
@@ -504,7 +510,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 for (int i = 0; i < NM; ++i) {
                     b[i][0] = rp.get(ring, at, 0, i);
                     b[i][1] = rp.get(ring, at, 1, i);
-                    if (!PLAIN) t[i] = thirds_of(b[i][0], b[i][1]);
+                    if (!PLAIN) t[i] = thirds_of(b[i][0], b[i][1], cut_p[i]);
                 }
                 u4v c[NN][2];
 #pragma unroll
@@ -513,7 +519,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                     c[j][1] = rq.get(ring, at + FP::BYTES, 1, j);
                 }
                 Thirds u = {};
-                if (!PLAIN) u = thirds_of(c[0][0], c[0][1]);
+                if (!PLAIN) u = thirds_of(c[0][0], c[0][1], cut_q[0]);
 #pragma unroll
                 for (int j = 0; j < NN; ++j) {
                     if (PLAIN) {
@@ -522,7 +528,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                     } else {
                         // the next thirds are made while these are multiplied
                         Thirds next = {};
-                        if (j + 1 < NN) next = thirds_of(c[j + 1 < NN ? j + 1 : j][0], c[j + 1 < NN ? j + 1 : j][1]);
+                        if (j + 1 < NN) next = thirds_of(c[j + 1 < NN ? j + 1 : j][0], c[j + 1 < NN ? j + 1 : j][1], cut_q[j + 1 < NN ? j + 1 : j]);
                         f4* const to[4] = {&acc[0][j], &acc[1][j], &acc[2][j], &acc[3][j]};
                         mfma_thirds<4>(u, t, to);
                         u = next;
@@ -539,17 +545,23 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 copy_all(slot);
                 slot = slot + 1 == RING ? 0 : slot + 1;
             }
+            // (rows and columns past the ends are anything)
+            u32 cut = 0;
+#pragma unroll
+            for (int i = 0; i < NM; ++i) cut |= m0 + wm + 16 * i + in_group < rows ? cut_p[i] : 0;
+#pragma unroll
+            for (int j = 0; j < NN; ++j) cut |= n0 + wn + 16 * j + in_group < a.cols ? cut_q[j] : 0;
+            return (cut & 0xFFFFu) == 0;
         };
         if (stages) {
-            all(Int<0>());
-            bool finite = true;
+            bool good = all(Int<0>());
 #pragma unroll
             for (int i = 0; i < NM; ++i)
 #pragma unroll
                 for (int j = 0; j < NN; ++j)
-                    for (int e = 0; e < 4; ++e) finite &= fabsf(acc[i][j][e]) <= FLT_MAX || m0 + wm + 16 * i + in_group >= rows || n0 + wn + 16 * j + group * 4 + e >= a.cols;
+                    for (int e = 0; e < 4; ++e) good &= fabsf(acc[i][j][e]) <= FLT_MAX || m0 + wm + 16 * i + in_group >= rows || n0 + wn + 16 * j + group * 4 + e >= a.cols;
             arrived_and_barrier<0>();
-            if (__syncthreads_or(!finite)) {
+            if (__syncthreads_or(!good)) {
 #pragma unroll
                 for (int i = 0; i < NM; ++i)
 #pragma unroll
