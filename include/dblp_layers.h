@@ -83,7 +83,7 @@ int dblp_activation_grad(int device, void* stream, uint64_t rows, uint32_t cols,
  * with a, b, c = h_coefficients[3 k ...] in step k (NULL: 3.4445, -4.7750, 2.0315 in each, which take singular values of 0.01 and
  * above to 0.7 to 1.2 in five steps), and out = base_scale base + scale X (d_base NULL: scale X).  The orthogonalised update
  * of the Muon optimiser is this call on a momentum of gradients, with the weights as base and out.  G is of g_type, base and out of out_type.
- * X, A and a + b A + c A A are held with 22 significant bits, or to 2^-40 of the largest value that they can have, and multiplied so.  Refused are
+ * X, A and a + b A + c A A are held with 22 significant bits, or to 2^-50 of the largest value that they can have, and multiplied so.  Refused are
  * steps above 16 and coefficients under which a singular value could pass 32.  In place: out may be the base or G, with the same stride and step; out's matrices do not overlap. */
 int dblp_orthogonalize(int device, void* stream, uint64_t count, uint32_t rows, uint32_t cols, const void* d_g, uint64_t g_stride,
                        uint64_t g_step, int g_type, const double* h_coefficients, uint32_t steps, float scale, const void* d_base,

@@ -75,8 +75,11 @@ __device__ __forceinline__ void mfma_thirds(const Thirds& a, const Thirds (&b)[N
 }
 
 // One operand of a batch of products: element (row, k) at row * stride + k, or at k * stride + row where it lies by k.  An operand in halves is two such matrices of
-// fp16, `low` elements apart, whose sum it is: 22 significant bits.  A product of two of those is three of the halves', low by high, high by low and high by high, one behind the
-// other in one sum over 3 k (the small ones first: they are rounded as what they are); what is left out is below the halves' own rounding.
+// fp16, `low` elements apart, the second times 2^-11: 22 significant bits, also where a half without that factor would be below fp16's normal numbers.  A product of two of those is three of
+// the halves', low by high, high by low and high by high, one behind the other in one sum over 3 k, which is multiplied by 2^-11 before the third (the small ones first: they are rounded as
+// what they are); what is left out is below the halves' own rounding.
+#define LOW_UP 2048.0f
+#define LOW_DOWN (1.0f / LOW_UP)
 struct Operand { const void* p; u64 stride, step, low; };
 
 // What a launch computes: rows x cols results of sums over `depth` k, of which block z takes part z % parts of matrix z / parts.
@@ -617,8 +620,17 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
                 for (int i = 0; i < NM; ++i) sum[i] = mfma<T>(ones<T>(), b[i], sum[i]);
             }
         };
+        // (of halves: the stages that hold low ones)
+        const u32 two = 2 * (a.depth / 3), low_stages = !HALVES || two <= k_first ? 0 : (two - k_first) / KS < stages ? (two - k_first) / KS : stages;
+        const auto lower = [&] {
+#pragma unroll
+            for (int i = 0; i < NM; ++i)
+#pragma unroll
+                for (int j = 0; j < NN; ++j) acc[i][j] *= LOW_DOWN;
+        };
         u32 slot = 0;
         for (u32 s = 0; s < stages; ++s) {
+            if (HALVES && s == low_stages) lower();
             const u32 then = slot + 1 == RING ? 0 : slot + 1;
             half(Int<0>(), b[0], b[1], slot, 1, 0);
             if (s + 2 == stages) trim(then);
@@ -629,6 +641,7 @@ __global__ __launch_bounds__(64 * W::ALL, 2) void ring_products(Product a, Out o
             next_copied();
             slot = then;
         }
+        if (HALVES && low_stages == stages) lower();
     }
     // the result's tile through LDS, some of a wave's rows at a time: rows leave whole, and what is done with them stands here once
     arrived_and_barrier<0>();

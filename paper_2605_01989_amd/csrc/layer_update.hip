@@ -67,18 +67,19 @@ __device__ __forceinline__ double one_over_norm(const double* parts, u32 n) {
     return sum == 0.0 ? 0.0 : sum <= DBL_MAX ? 1.0 / sqrt(sum) : NAN;
 }
 
-// A value in halves: the nearest fp16 value, and the nearest one to what that leaves.  Both are of the value times a power of two that takes the largest one possible to 2^15, so that
-// a value keeps 22 bits, or 2^-40 of that largest one.
+// A value in halves: the nearest fp16 value, and the nearest one to 2^11 times what that leaves, which is no larger than the value.  Both are of the value times a power of two that takes the
+// largest one possible to 2^14 and more, below 2^15, so that a value keeps 22 bits, or 2^-50 of that largest one (without the factor 2^-39: a row 2^-24 as large as the rest was off by 2^-7 to 2^-10).
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 struct Halves { half4 high, low; };
 __device__ __forceinline__ Halves halves_of(const float (&v)[4]) {
     Halves h;
     for (int i = 0; i < 4; ++i) {
         h.high[i] = (_Float16)v[i];
-        h.low[i] = (_Float16)(v[i] - (float)h.high[i]);
+        h.low[i] = (_Float16)fmaf((float)h.high[i], -LOW_UP, v[i] * LOW_UP);
     }
     return h;
 }
+__device__ __forceinline__ float value_of(_Float16 high, _Float16 low) { return (float)high + (float)low * LOW_DOWN; }
 struct HalvesAt {
     _Float16* p;
     u64 stride, step, low;       // of rows, of matrices, from the high halves to the low ones
@@ -156,7 +157,7 @@ struct PolyOut {
     __device__ __forceinline__ Halves get(u32 matrix, u32 m, u32 n, u32) const { return gram.get(matrix0 + matrix, m, n); }
     __device__ __forceinline__ void put(u32 matrix, u32, u32 m, u32 n, u32, f4 acc, const Halves& g) const {
         float v[4];
-        for (int i = 0; i < 4; ++i) v[i] = b * ((float)g.high[i] + (float)g.low[i]) + c * acc[i] + (n + i == m && m < rows ? a : 0.0f);
+        for (int i = 0; i < 4; ++i) v[i] = b * value_of(g.high[i], g.low[i]) + c * acc[i] + (n + i == m && m < rows ? a : 0.0f);
         poly.put(matrix0 + matrix, m, n, v);
     }
     __device__ __forceinline__ void sums(u32, u32, u32, float) const {}
@@ -183,7 +184,7 @@ struct UpdateOut {
 
 // ------------------------------------------------------------------------------------------
 // Small matrices, X of at most 64 R x 64 N: a block takes one through all of its steps, X and then A, then a + b A + c A A, in halves in LDS.  Eight waves, four by two, each 16 R x
-// 32 R columns of A and 16 R x 32 N of X.  What bounds it is the way from one product to the next: reading, multiplying, a barrier, writing.  128 x 128 in five steps 53 us (four and
+// 32 R columns of A and 16 R x 32 N of X.  What bounds it is the way from one product to the next: reading, multiplying, a barrier, writing.  128 x 128 in five steps 51 us (four and
 // sixteen waves are slower), 91 as products of tiles through memory.
 // A row in LDS is 128 bytes for each 64 values, chunk c of 16 bytes of row r at c ^ (r & 7).
 // ------------------------------------------------------------------------------------------
@@ -210,18 +211,25 @@ __device__ __forceinline__ void small_put(uint8_t* m, u32 low, u32 row, u32 col,
     *(half4*)(m + low + small_at<WIDTH>(row, col)) = h.low;
 }
 
-// low by high, high by low, high by high: each a round over the results, whose sums wait for each other.  TURNED: a result's rows and columns change places.
+// low by high and high by low to sums of their own, high by high: each a round over the results, whose sums wait for each other.  TURNED: a result's rows and columns change places.
 template <int R, int C, bool TURNED = false>
-__device__ __forceinline__ void add_halves(f4 (&acc)[R][C], const u4v (&bh)[R], const u4v (&bl)[R], const u4v (&ch)[C], const u4v (&cl)[C]) {
-    const auto round = [&](const u4v (&b)[R], const u4v (&c)[C]) {
+__device__ __forceinline__ void add_halves(f4 (&acc)[R][C], f4 (&low)[R][C], const u4v (&bh)[R], const u4v (&bl)[R], const u4v (&ch)[C], const u4v (&cl)[C]) {
+    const auto round = [&](f4 (&to)[R][C], const u4v (&b)[R], const u4v (&c)[C]) {
 #pragma unroll
         for (int j = 0; j < C; ++j)
 #pragma unroll
-            for (int e = 0; e < R; ++e) acc[e][j] = TURNED ? mfma<F16>(b[e], c[j], acc[e][j]) : mfma<F16>(c[j], b[e], acc[e][j]);
+            for (int e = 0; e < R; ++e) to[e][j] = TURNED ? mfma<F16>(b[e], c[j], to[e][j]) : mfma<F16>(c[j], b[e], to[e][j]);
     };
-    round(bl, ch);
-    round(bh, cl);
-    round(bh, ch);
+    round(low, bl, ch);
+    round(low, bh, cl);
+    round(acc, bh, ch);
+}
+template <int R, int C>
+__device__ __forceinline__ void join_halves(f4 (&acc)[R][C], const f4 (&low)[R][C]) {
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int e = 0; e < R; ++e) acc[e][j] += low[e][j] * LOW_DOWN;
 }
 
 struct SmallSteps { float gram[STEPS_MOST], a[STEPS_MOST], b[STEPS_MOST], c[STEPS_MOST], next[STEPS_MOST]; u32 n; };
@@ -281,7 +289,7 @@ struct Small {
                     for (int e = 0; e < 4; ++e) {
                         const _Float16 high = (_Float16)v[e];
                         *(_Float16*)(x + small_at<COLS>(col + e, row)) = high;
-                        *(_Float16*)(x + X_LOW + small_at<COLS>(col + e, row)) = (_Float16)(v[e] - (float)high);
+                        *(_Float16*)(x + X_LOW + small_at<COLS>(col + e, row)) = (_Float16)fmaf((float)high, -LOW_UP, v[e] * LOW_UP);
                     }
             }
         }
@@ -289,15 +297,17 @@ struct Small {
     // acc += M M^T of a matrix of WIDTH columns
     template <int WIDTH>
     __device__ __forceinline__ void square(f4 (&acc)[R][2 * R], const uint8_t* of, u32 low) const {
-#pragma unroll 2
+        f4 small[R][2 * R] = {};
+#pragma unroll
         for (u32 k0 = 0; k0 < WIDTH; k0 += 32) {
             u4v bh[R], bl[R], ch[2 * R], cl[2 * R];
 #pragma unroll
             for (int e = 0; e < R; ++e) { bh[e] = small_rows<WIDTH>(of, m0 + 16 * e, k0); bl[e] = small_rows<WIDTH>(of + low, m0 + 16 * e, k0); }
 #pragma unroll
             for (int j = 0; j < 2 * R; ++j) { ch[j] = small_rows<WIDTH>(of, an0 + 16 * j, k0); cl[j] = small_rows<WIDTH>(of + low, an0 + 16 * j, k0); }
-            add_halves<R, 2 * R>(acc, bh, bl, ch, cl);
+            add_halves<R, 2 * R>(acc, small, bh, bl, ch, cl);
         }
+        join_halves<R, 2 * R>(acc, small);
     }
     // From A's sums a + b A + c A A to m, A by the way there too; a wave's part of A A is at the same places as its part of A.
     __device__ __forceinline__ void poly(f4 (&acc)[R][2 * R], uint8_t* m, u32 rows, float gram, float a, float b, float c) const {
@@ -323,23 +333,29 @@ struct Small {
             for (int j = 0; j < 2 * R; ++j) {
                 const u32 row = m0 + 16 * e + in_group, col = an0 + 16 * j + group * 4;
                 float v[4];
-                for (int t = 0; t < 4; ++t) v[t] = b * ((float)own[e][j].high[t] + (float)own[e][j].low[t]) + c * acc[e][j][t] + (col + t == row && row < rows ? a : 0.0f);
+                for (int t = 0; t < 4; ++t) v[t] = b * value_of(own[e][j].high[t], own[e][j].low[t]) + c * acc[e][j][t] + (col + t == row && row < rows ? a : 0.0f);
                 small_put<ROWS>(m, A_LOW, row, col, v);
             }
         __syncthreads();
     }
-    // next = m x; turned: a result's rows and columns change places
-    __device__ __forceinline__ void apply(f4 (&next)[R][2 * N], const uint8_t* m, const uint8_t* x, bool turned) const {
-#pragma unroll 2
+    // next = m x; TURNED: a result's rows and columns change places
+    template <bool TURNED>
+    __device__ __forceinline__ void apply_as(f4 (&next)[R][2 * N], const uint8_t* m, const uint8_t* x) const {
+        f4 small[R][2 * N] = {};
+#pragma unroll
         for (u32 k0 = 0; k0 < ROWS; k0 += 32) {
             u4v bh[R], bl[R], ch[2 * N], cl[2 * N];
 #pragma unroll
             for (int e = 0; e < R; ++e) { bh[e] = small_rows<ROWS>(m, m0 + 16 * e, k0); bl[e] = small_rows<ROWS>(m + A_LOW, m0 + 16 * e, k0); }
 #pragma unroll
             for (int j = 0; j < 2 * N; ++j) { ch[j] = small_columns<COLS>(x, xn0 + 16 * j, k0); cl[j] = small_columns<COLS>(x + X_LOW, xn0 + 16 * j, k0); }
-            if (turned) add_halves<R, 2 * N, true>(next, bh, bl, ch, cl);
-            else add_halves<R, 2 * N>(next, bh, bl, ch, cl);
+            add_halves<R, 2 * N, TURNED>(next, small, bh, bl, ch, cl);
         }
+        join_halves<R, 2 * N>(next, small);
+    }
+    __device__ __forceinline__ void apply(f4 (&next)[R][2 * N], const uint8_t* m, const uint8_t* x, bool turned) const {
+        if (turned) apply_as<true>(next, m, x);
+        else apply_as<false>(next, m, x);
     }
     __device__ __forceinline__ void keep(const f4 (&next)[R][2 * N], float by, uint8_t* x) const {
 #pragma unroll
@@ -392,7 +408,7 @@ __global__ __launch_bounds__(512) void small_steps(const typename T::elem* g, u6
 // ------------------------------------------------------------------------------------------
 // Long ones of at most 128 rows: the same by many blocks, each with some pieces of 128 columns of X.  A step is two launches: blocks multiply their pieces and add up their part of the
 // next A from them, as they lie in LDS, and one block a matrix joins the parts and makes a + b A + c A A.  What bounds it is the launches, 5 to 7 us each with a block's few products
-// in a row: 40 x 64 x 1536 in 104 us, 152 as products of tiles that go through memory; X's reads and writes where the matrices are many (300 x 64 x 3000 1040 us, 2.3 TB/s).
+// in a row: 40 x 64 x 1536 in 112 us, 153 as products of tiles that go through memory; X's reads and writes where the matrices are many (300 x 64 x 3000 1193 us, 2.3 TB/s).
 // ------------------------------------------------------------------------------------------
 // 16 bytes a thread between LDS and a piece of a matrix in halves.
 template <int ROWS, int WIDTH, bool OUT>
@@ -500,7 +516,7 @@ __global__ __launch_bounds__(256) void update_plain(HalvesAt x, Shape s, UpdateO
         for (u32 e = 0; e < 4; ++e)
             if (c + e < cols) {
                 const _Float16* const at = x.p + matrix * x.step + (s.tall ? (c + e) * x.stride + m : m * x.stride + c + e);
-                v[e] = (float)at[0] + (float)at[x.low];
+                v[e] = value_of(at[0], at[x.low]);
             }
         out.put(blockIdx.z, 0, m, c, cols, v, out.get(blockIdx.z, m, c, cols));
     }
@@ -639,8 +655,8 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
         return launched(call, launch);
     }
     // Long ones of at most 128 rows by thin_first and what follows it, where they are many or not too long (the first of two times, in us): one block a matrix joins A's parts, and few
-    // blocks hold a single long one up.  Of 64 rows as many blocks as two fit a CU, 12 x 64 x 1671 72 and 124, 1 x 64 x 5297 84 and 112, 1 x 64 x 1000000 3129 and 2683; of 128 one a CU
-    // and 16 parts, 128 x 128 x 2048 509 and 918, 16 x 128 x 4096 226 and 279, 1 x 128 x 512 95 and 106, 1 x 128 x 5297 212 and 140.  A's parts lie where the others' do, a single one where A would.
+    // blocks hold a single long one up.  Of 64 rows as many blocks as two fit a CU, 12 x 64 x 1671 78 and 124, 1 x 64 x 5297 87 and 121, 1 x 64 x 1000000 3321 and 2837; of 128 one a CU
+    // and 16 parts, 128 x 128 x 2048 565 and 762, 16 x 128 x 4096 244 and 237, 1 x 128 x 512 97 and 110, 1 x 128 x 5297 218 and 150.  A's parts lie where the others' do, a single one where A would.
     const bool few_rows = at.rows == 64;
     const u32 pieces = (u32)(at.cols / 128);
     u32 blocks = (u32)((few_rows ? 512 : 256) / count);
