@@ -1,4 +1,4 @@
-"""GPU: the gradient of a layer's input where dy's rows lie at odd places.  Operands are whole numbers of at most 8, so that products and sums are exact in fp32 (4097 x 64 < 2^24) in
+"""GPU: products of operands whose rows lie at odd places.  Operands are whole numbers of at most 8, so that products and sums are exact in fp32 (4097 x 64 < 2^24) in
 any order: results have to be equal to the definition's in 64 bits, with no tolerance."""
 import pytest
 import torch
@@ -41,3 +41,19 @@ def test_every_term_counts(t, n, inner, outer):
             narrow = torch.empty(n, inner, dtype=t, device="cuda")
             dblp.linear_grad_input(dy, w, narrow, ws)
             assert torch.equal(narrow, want.float().to(t))
+
+
+@pytest.mark.parametrize("n, inner, outer", [(1, 64, 70), (5, 1024, 65), (16, 4096, 300), (300, 64, 131), (300, 65, 256), (1024, 320, 129), (64, 300, 131), (4096, 64, 67), (1023, 768, 1025), (2048, 1025, 640)])
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
+def test_every_term_of_the_other_products_counts(t, n, inner, outer):
+    """Forward, and the weight's and the bias' gradients, whose sums are over the input's width and over the tokens."""
+    import paper_2605_01989_amd as dblp
+    g = gen(n + inner + outer)
+    ws = torch.full((dblp.linear_workspace(n, inner, outer),), 255, dtype=torch.uint8, device="cuda")
+    for shift, pad in ((0, 0), (1, 1), (1, 0), (2, 2), (3, 1), (0, 5)):
+        x, w, dy = (whole(g, r, c, t, c + pad, shift) for r, c in ((n, inner), (outer, inner), (n, outer)))
+        y, dw, db = (torch.full(s, 5.0, device="cuda") for s in ((n, outer), (outer, inner), (outer,)))
+        dblp.linear(x, w, y, ws)
+        assert torch.equal(y.double(), x.double() @ w.double().T), (shift, pad)
+        dblp.linear_grad_weight(dy, x, dw, ws, bias_grad=db)
+        assert torch.equal(dw.double(), dy.double().T @ x.double()) and torch.equal(db.double(), dy.double().sum(0)), (shift, pad)
