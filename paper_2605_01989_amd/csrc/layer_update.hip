@@ -581,8 +581,10 @@ static double poly_bound(const double* k, double most) {
     if (turn > 0 && turn < end) best = fmax(best, value(turn));
     return best;
 }
+// Bounds are held to this and more (coefficients may be any small ones): powers of two of them, and products of those, stay in fp64's range.
+#define BOUND_LEAST 0x1p-300
 // The power of two that takes values up to `most` to 2^15 and less: fp16 reaches past it.
-static double power_for(double most) { return most > 0 ? exp2(floor(15 - log2(most * (1 + 1e-5)))) : 1.0; }
+static double power_for(double most) { return exp2(floor(15 - log2(fmax(most, BOUND_LEAST) * (1 + 1e-5)))); }
 
 extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint32_t rows, uint32_t cols, const void* d_g, uint64_t g_stride,
                                   uint64_t g_step, int g_type, const double* h_coefficients, uint32_t steps, float scale, const void* d_base,
@@ -597,6 +599,7 @@ extern "C" int dblp_orthogonalize(int device, void* stream, uint64_t count, uint
     for (u32 i = 0; i < steps; ++i) {
         const double* k = h_coefficients ? h_coefficients + 3 * i : USUAL;
         bounds[i + 1] = bound_after(k, bounds[i] * (1 + 1e-6));
+        if (bounds[i + 1] < BOUND_LEAST) bounds[i + 1] = BOUND_LEAST;
         REFUSE_IF(!(fabs(k[0]) <= FLT_MAX && fabs(k[1]) <= FLT_MAX && fabs(k[2]) <= FLT_MAX && bounds[i + 1] <= BOUND_MOST), "coefficients under which a singular value could pass 32");
     }
     const bool some = count && rows && cols;
