@@ -304,7 +304,7 @@ struct Way { Kind kind; u32 parts, part; double us, stages_us; };     // (stages
 
 // Chosen by an estimate of the time, in microseconds: rounds of tiles over the 256 CUs, each a fixed time and one for each stage of 128 bytes of k, which is longer with more blocks on a CU
 // (of the largest tiles, with more CUs at work); parts are written, read and added up at 5 TB/s.  As measured with each kind alone over 27 sizes; the choice is within 15 % of the best
-// kind and number of parts on them (8192 x 1024 x 4096 in tiles of 64, 128, 256: 118, 79, 68 us; 8192 x 768 x 2304: 18, 18, 26; its weight's gradient in 1, 4, 8 parts: 85, 44, 46).
+// kind and number of parts on them (8192 x 1024 x 4096 in tiles of 64, 128, 256: 118, 79, 68 us; 2048 x 768 x 2304: 18, 18, 26; the weight's gradient of 8192 x 768 x 2304 in 1 and 4 parts of tiles of 128 85 and 44, in 8 of 256 46).
 static Way way_of(u64 rows, u64 cols, u64 depth, u32 elem) {
     static const struct { u32 tile, blocks; double fixed, stage[2][3]; } K[KINDS] = {
         {64, 3, 3.5, {{0.28, 0.40, 0.50}, {0.65, 0.90, 1.10}}}, {128, 2, 5.0, {{0.64, 0.98, 0}, {1.85, 2.65, 0}}}, {256, 1, 10.0, {{1.15, 0, 0}, {0, 0, 0}}}};

@@ -218,7 +218,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_products(Product a, Out out
 //            four values each, lane i gets value i % 4 of lanes i / 4, i / 4 + 4, ...), floats are read one by one.
 // Bound by the matrix instructions and by LDS' reads beside them (the instructions at work 65 % of the time in the largest products), small products by the rounds of tiles.  The largest
 // tile, 256 x 256 of eight waves with 128 x 64 results each, reads 96 KiB of LDS for 32 k, four of 128 x 128 128 KiB; four waves' results do not fit the registers.  8192 x 8192 x 8192 of
-// bf16: 806 us (1.36 PFLOP/s) by rows and rows, 797 by rows and k, 817 by k and k into floats; 4096 x 4096 x 4096 110, 114, 115; the library's 751 to 912 and 94 to 120.
+// bf16: 815 us (1.35 PFLOP/s) by rows and rows, 782 by rows and k, 802 by k and k into floats; 4096 x 4096 x 4096 105, 106, 107; the library's 694, 808, 908 and 109, 116, 130.
 // ------------------------------------------------------------------------------------------
 #define STAGE_BYTES 128
 
@@ -227,10 +227,10 @@ __device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_rea
 #define PAST_ALL 0x80000000u                     // an offset that no buffer here reaches: a copy of it writes zeros
 
 // 64 lanes' 16 bytes at `offset` of a buffer to 1024 bytes of LDS at `to`.  No register is written, so nothing can be overwritten by it, and the compiler waits
-// for it nowhere: by a builtin it would before each read of LDS.  Nor does it look into these lines for the wait states that a copy needs behind a write of m0, one, and
-// behind a vector instruction's write of a register of `from`, five, of which the write of m0 is one.
+// for it nowhere: by a builtin it would before each read of LDS.  m0 is nobody's else in these kernels.  Nor does the compiler look into these lines for the wait states
+// that a copy needs behind a write of m0, one, and behind a vector instruction's write of a register of `from`, five, of which the write of m0 is one.
 __device__ __forceinline__ void copy_to_lds(rsrc_t from, u32 offset, u32 to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from));
 }
 template <int N> __device__ __forceinline__ void arrived_and_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
