@@ -13,7 +13,8 @@
  * checked on the host before the device is touched, everything enqueued on `stream` of `device`, nothing allocated, nothing
  * waited for, calls that can be recorded into a HIP graph, types DBLP_F32, DBLP_BF16 and DBLP_F16, pointers aligned to one
  * element, row strides in ELEMENTS, an input's rows may overlap, an output overlaps no other argument except where "in
- * place" says so.  Every result is a function of the arguments alone: no floating-point atomics, sums cut by the sizes alone.
+ * place" says so.  Every result is a function of the arguments alone: no floating-point atomics, sums cut by sizes, types, strides and the alignment of addresses.  Where a value
+ * is not finite, or a float lies below 2^-110, other results of a large product of floats (those of its tile, at most 128 x 128) may differ in their last bits from what they are without it.
  * Rows whose address and stride are multiples of 16 bytes are fastest.
  *
  * Products are summed in fp32 (of 16-bit values each product is exact, of fp32 values it is within 2^-23 of itself), everything behind them is computed in fp32, and a result
